@@ -21,6 +21,12 @@
  *                       the full-precision layers a network keeps around its
  *                       two-bit layers (first convolution, global average
  *                       pool, last fully-connected layer)
+ *   tbn_adapter_fwd, tbn_adapter_bwd   low-rank adapters of many requests
+ *                       beside a shared (two-bit) projection
+ *   tbn_layernorm_fwd, tbn_layernorm_bwd   layer norm with its gradients
+ *   tbn_adamw_step      AdamW over many tensors (real-valued weights before
+ *                       their quantization, or adapters), moments in 32 or
+ *                       in 8 bits
  *
  * Conventions shared by every call
  * --------------------------------
@@ -500,6 +506,83 @@ tbn_status tbn_avgpool2d_global_nhwc(const void *x, tbn_dtype xdt, int64_t N, in
 tbn_status tbn_dense_linear_fwd(const float *x, int64_t B, int64_t K_in, const float *w,
                                 int64_t K_out, void *y, tbn_dtype ydt, int relu,
                                 tbn_stream stream);
+
+/* ------------------------------------------------------------------------
+ * Layer norm over the last dimension of x [rows][D], rows ldx elements apart
+ * (any ldx >= D; elements of a row are contiguous):
+ *   mean = sum x / D, rstd = (sum (x - mean)^2 / D + eps)^-1/2,
+ *   y = (x - mean) rstd gamma + beta.
+ * xdt: type of x; ydt: of y (rows ldy apart), which is xdt or TBN_BF16.
+ * gamma, beta [D] of type wdt, either may be NULL (1 and 0).  mean and rstd
+ * [rows] fp32 are written where not NULL; the backward pass needs them.
+ * rows = 0 does nothing.  y may be x where types and strides are the same.
+ * Statistics and sums are held in fp32; results are rounded once. */
+tbn_status tbn_layernorm_fwd(const void *x, tbn_dtype xdt, int64_t rows, int64_t D, int64_t ldx,
+                             const void *gamma, const void *beta, tbn_dtype wdt, float eps,
+                             void *y, tbn_dtype ydt, int64_t ldy, float *mean, float *rstd,
+                             tbn_stream stream);
+
+/* Workspace bytes of tbn_layernorm_bwd; 0 for sizes that it refuses. */
+size_t tbn_layernorm_bwd_workspace_bytes(int64_t rows, int64_t D);
+
+/* Gradients of tbn_layernorm_fwd: with w = gamma dy and xh = (x - mean) rstd,
+ *   dx = dres + rstd (w - sum w / D - xh sum (w xh) / D),
+ *   dgamma = sum over rows of dy xh, dbeta = sum over rows of dy.
+ * dy has type ydt and rows lddy apart; dx and dres (NULL: none; the gradient
+ * of a residual branch around the norm) have type xdt and rows lddx and lddres
+ * apart; dgamma and dbeta [D] fp32 (either NULL: not computed) are written,
+ * not added to, with zeros for rows = 0.  dx may be x, dy or dres where type
+ * and stride are the same.  The sums over rows are taken in a fixed order:
+ * equal inputs give equal bits.  `workspace`: as many bytes as
+ * tbn_layernorm_bwd_workspace_bytes says, 16-byte aligned. */
+tbn_status tbn_layernorm_bwd(const void *dy, tbn_dtype ydt, int64_t lddy, const void *x,
+                             tbn_dtype xdt, int64_t rows, int64_t D, int64_t ldx,
+                             const float *mean, const float *rstd, const void *gamma,
+                             tbn_dtype wdt, const void *dres, int64_t lddres, void *dx,
+                             int64_t lddx, float *dgamma, float *dbeta, void *workspace,
+                             size_t workspace_bytes, tbn_stream stream);
+
+/* ------------------------------------------------------------------------
+ * AdamW.  One tensor of a step; n = 0 is left out.  With TBN_ADAMW_STATE_32BIT
+ * m and v are fp32 [n].  With TBN_ADAMW_STATE_8BIT they are one byte an
+ * element and a scale for each 256 consecutive ones: the first moment is
+ * m_scale[i / 256] times the e4m3 number (no infinities) in m[i], the second
+ * v_scale[i / 256] times the e5m2 number in v[i], the scales fp32
+ * [ceil(n / 256)].  Zeros in all of them are the state before the first step.
+ * Tensors of one call do not overlap. */
+typedef enum { TBN_ADAMW_STATE_32BIT = 0, TBN_ADAMW_STATE_8BIT = 1 } tbn_adamw_state;
+
+typedef struct {
+  void *param;        /* updated in place */
+  const void *grad;
+  void *m, *v;        /* updated in place */
+  float *m_scale, *v_scale;   /* 8-bit moments only */
+  void *copy;         /* NULL, or bf16 [n]: the rounded new parameters */
+  int64_t n;
+  float weight_decay; /* decoupled: p loses lr * lr_scale * weight_decay of itself */
+  float lr_scale;     /* this tensor's factor on lr */
+  int32_t param_dtype, grad_dtype;   /* tbn_dtype */
+  int32_t state;                     /* tbn_adamw_state */
+} tbn_adamw_tensor;
+
+typedef struct {
+  double lr, beta1, beta2, eps;
+  int64_t step;       /* number of this step, from 1 */
+  const float *grad_scale;   /* NULL, or a DEVICE scalar that every gradient is multiplied by */
+  uint32_t seed;      /* of the 8-bit moments' rounding; another one in every step */
+} tbn_adamw_hyper;
+
+/* One AdamW step of all tensors (a HOST array, read before the call returns),
+ * in one launch for up to 352 of them:
+ *   g = grad * grad_scale, m = beta1 m + (1 - beta1) g,
+ *   v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr' wd) - lr' / (1 - beta1^step) * m
+ *                        / (sqrt(v / (1 - beta2^step)) + eps), lr' = lr lr_scale,
+ * in fp32, with 8-bit moments rounded up or down at random afterwards (16 bits
+ * of a mix of seed and element: equal arguments give equal bits).  What is not
+ * finite spoils its own element only. */
+tbn_status tbn_adamw_step(const tbn_adamw_tensor *tensors, int count, const tbn_adamw_hyper *hyper,
+                          tbn_stream stream);
 
 #ifdef __cplusplus
 }

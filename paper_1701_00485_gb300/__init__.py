@@ -33,7 +33,8 @@ __all__ = [
     "TBN_REPACK_PLANAR_TO_CANONICAL", "tbn_dense_conv2d_fwd", "tbn_avgpool2d_global_nhwc",
     "tbn_dense_linear_fwd", "tbn_space_to_depth", "space_to_depth_shape", "TBN_S2D_NHWC",
     "tbn_linear_prepare_f8", "tbn_linear_f8_workspace_bytes", "tbn_linear_fwd_f8",
-    "tbn_linear_f8_prepared_words", "tbn_conv2d_fwd_quant",
+    "tbn_linear_f8_prepared_words", "tbn_conv2d_fwd_quant", "tbn_layernorm_fwd",
+    "tbn_layernorm_bwd", "tbn_layernorm_bwd_workspace_bytes", "AdamWPlan", "tbn_adamw_step",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -61,6 +62,8 @@ EXPORTED = [
     "tbn_avgpool2d_global_nhwc", "tbn_dense_linear_fwd", "tbn_space_to_depth_elems",
     "tbn_space_to_depth", "tbn_linear_prepare_f8", "tbn_linear_f8_workspace_bytes",
     "tbn_linear_fwd_f8", "tbn_linear_f8_prepared_words", "tbn_conv2d_fwd_quant",
+    "tbn_layernorm_fwd", "tbn_layernorm_bwd_workspace_bytes", "tbn_layernorm_bwd",
+    "tbn_adamw_step",
 ]
 
 
@@ -151,6 +154,12 @@ def lib():
                                       ctypes.c_size_t, P], I32),
             "tbn_linear_fwd_f8": ([P, I32, I64, I64, U32P, P, I64, P, I32,
                                    ctypes.POINTER(Epilogue), P, ctypes.c_size_t, P], I32),
+            "tbn_layernorm_fwd": ([P, I32, I64, I64, I64, P, P, I32, ctypes.c_float, P, I32, I64,
+                                   P, P, P], I32),
+            "tbn_layernorm_bwd_workspace_bytes": ([I64, I64], ctypes.c_size_t),
+            "tbn_layernorm_bwd": ([P, I32, I64, P, I32, I64, I64, I64, P, P, P, I32, P, I64, P,
+                                   I64, P, P, P, ctypes.c_size_t, P], I32),
+            "tbn_adamw_step": ([P, I32, P, P], I32),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -705,3 +714,7 @@ def tbn_selftest_wait_timeout(limit_us: int, stream=None) -> None:
     after limit_us and sets TBN_DEVERR_TIMEOUT in the device error word."""
     _check(lib().tbn_selftest_wait_timeout(limit_us, _stream(stream)),
            "tbn_selftest_wait_timeout")
+
+
+from ._train import (AdamWPlan, AdamWTensor, AdamWHyper, tbn_adamw_step,  # noqa: E402
+                     tbn_layernorm_bwd, tbn_layernorm_bwd_workspace_bytes, tbn_layernorm_fwd)

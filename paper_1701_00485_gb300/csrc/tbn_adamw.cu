@@ -1,0 +1,339 @@
+// tbn_adamw.cu -- one AdamW step over many tensors in one launch, with the
+// two moments in 32 bits or in 8.
+//
+//   g = grad * grad_scale
+//   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+//   p = p (1 - lr wd) - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+//
+// Bound by HBM: 24 bytes a parameter with 32-bit moments, 12 with 8-bit ones,
+// and the gradient's.  A warp takes 256 consecutive elements of a tensor, the
+// length that shares a scale, so the block's largest value is a warp reduction
+// and no thread waits for another warp.
+//
+// 8-bit moments.  m = s_m * e4m3, v = s_v * e5m2 (v's range is that of m
+// squared), with s the least power of two that brings the block's largest
+// finite value into the format's range.  Values are rounded up or down at
+// random, in proportion to their distance (16 random bits for each moment, a
+// mix of the seed and the element's number): rounded to nearest, v would not
+// move at all, since a step changes it by 1 - beta2 = 0.1 % or so and the
+// format's values lie 12 to 25 % apart.  A scale that is a power of two keeps
+// the grid of values where it was, so that a stored value that does not change
+// is stored as it is.  v > 0 is never stored as 0, which would let m / sqrt(v)
+// run away.  The step itself uses the moments before they are rounded.
+// Infinite or NaN moments are stored as such (e4m3 has no infinity: NaN) and
+// leave their neighbours' scale alone.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include <cmath>
+
+#include "tbn_device.cuh"
+#include "tbn_internal.h"
+
+namespace tbn {
+namespace {
+
+constexpr int kBlock = 256;                    // elements of a scale, and of a warp's turn
+constexpr int kLane = kBlock / 32;             // consecutive elements of a lane
+constexpr int kThreads = 256;
+constexpr int kChunk = kBlock * kThreads / 32; // elements of a thread block
+
+enum : uint32_t { kParam16 = 1u, kGrad16 = 2u, kState8 = 4u, kAligned = 8u };
+
+struct Tensor {
+  void* p;
+  const void* g;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  __nv_bfloat16* copy;
+  int64_t n;
+  float lr, decay;         // lr / (1 - beta1^t), 1 - lr wd
+  uint32_t first_random;   // the number of the first element
+  uint32_t flags;
+};
+
+struct Hyper {
+  float beta1, one_beta1, beta2, one_beta2, root_fix2, eps;
+  const float* grad_scale;
+  uint32_t salt;
+  int count;
+};
+
+template <int N>
+struct Batch {
+  Hyper h;
+  uint32_t chunk_end[N];   // chunks of this tensor and those before it
+  Tensor t[N];
+};
+
+__device__ __forceinline__ uint32_t random_bits(uint32_t salt, uint32_t i) {
+  // an invertible mix of 32 bits: xor with its own shift, odd multiplications
+  uint32_t h = i + salt;
+  h = (h ^ (h >> 16)) * 0x7FEB352Du;
+  h = (h ^ (h >> 15)) * 0x846CA68Bu;
+  return h ^ (h >> 16);
+}
+
+__device__ __forceinline__ void load8(const void* base, bool bf16, bool aligned, int64_t at,
+                                      int there, float (&v)[kLane]) {
+  if (aligned && there == kLane) {
+    if (bf16) {
+      const uint4 r = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) + at);
+      const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      }
+    } else {
+      const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
+      const float4 a = f[0], b = f[1];
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kLane; ++i) {
+    v[i] = 0.0f;
+    if (i < there)
+      v[i] = bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(base)[at + i])
+                  : static_cast<const float*>(base)[at + i];
+  }
+}
+
+__device__ __forceinline__ void store8(void* base, bool bf16, bool aligned, int64_t at, int there,
+                                       const float (&v)[kLane]) {
+  if (aligned && there == kLane) {
+    if (bf16) {
+      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(base) + at) =
+          make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                     pack_bf16x2(v[6], v[7]));
+    } else {
+      float4* f = reinterpret_cast<float4*>(static_cast<float*>(base) + at);
+      f[0] = make_float4(v[0], v[1], v[2], v[3]);
+      f[1] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kLane; ++i)
+    if (i < there) {
+      if (bf16)
+        static_cast<__nv_bfloat16*>(base)[at + i] = __float2bfloat16_rn(v[i]);
+      else
+        static_cast<float*>(base)[at + i] = v[i];
+    }
+}
+
+__device__ __forceinline__ uint2 load_codes(const void* base, bool aligned, int64_t at, int there) {
+  const uint8_t* c = static_cast<const uint8_t*>(base) + at;
+  if (aligned && there == kLane) return *reinterpret_cast<const uint2*>(c);
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int i = 0; i < kLane; ++i)
+    if (i < there) w[i / 4] |= static_cast<uint32_t>(c[i]) << (8 * (i % 4));
+  return make_uint2(w[0], w[1]);
+}
+
+__device__ __forceinline__ void store_codes(void* base, bool aligned, int64_t at, int there,
+                                            const uint32_t (&w)[2]) {
+  uint8_t* c = static_cast<uint8_t*>(base) + at;
+  if (aligned && there == kLane) {
+    *reinterpret_cast<uint2*>(c) = make_uint2(w[0], w[1]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kLane; ++i)
+    if (i < there) c[i] = static_cast<uint8_t>(w[i / 4] >> (8 * (i % 4)));
+}
+
+// Eight codes of a block to values: code * scale.
+template <__nv_fp8_interpretation_t kFormat>
+__device__ __forceinline__ void decode(uint2 codes, float scale, float (&v)[kLane]) {
+  const uint32_t w[2] = {codes.x, codes.y};
+#pragma unroll
+  for (int i = 0; i < kLane / 2; ++i) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(
+        static_cast<__nv_fp8x2_storage_t>(w[i / 2] >> (16 * (i % 2))), kFormat);
+    const float2 f = __half22float2(__half2(h));
+    v[2 * i] = f.x * scale;
+    v[2 * i + 1] = f.y * scale;
+  }
+}
+
+// The block's scale for moments up to `most` (the bits of its largest finite
+// magnitude): the least 2^(f - 127), f >= 1, with 1.75 * 2^kTop times it >= most.
+template <int kTop>
+__device__ __forceinline__ int scale_field(uint32_t most) {
+  const int f = static_cast<int>((most + 0x1FFFFFu) >> 23) - kTop;
+  return f > 1 ? f : 1;
+}
+
+__device__ __forceinline__ uint32_t finite_bits(float v) {
+  const uint32_t b = __float_as_uint(v) & 0x7FFFFFFFu;
+  return b < 0x7F800000u ? b : 0u;
+}
+
+// |v| / scale in a format of exponent bias kBias and 23 - kDrop mantissa bits,
+// rounded at random: the multiplication by 2^(kBias - 127) brings the format's
+// exponent field, subnormal numbers included, to that of the 32-bit number,
+// whose kDrop low bits and as many random ones then carry or do not.
+template <int kBias, int kDrop>
+__device__ __forceinline__ uint32_t encode(float v, float inv_scale, uint32_t random16) {
+  const float u = fabsf(v) * inv_scale * __uint_as_float(static_cast<uint32_t>(kBias) << 23);
+  return (__float_as_uint(u) + (random16 << (kDrop - 16))) >> kDrop;
+}
+
+template <int N>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Batch<N> b) {
+  // the tensor of this chunk: the first whose chunks end beyond it
+  int lo = 0, hi = b.h.count - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (b.chunk_end[mid] > blockIdx.x) hi = mid;
+    else lo = mid + 1;
+  }
+  const Tensor& t = b.t[lo];
+  const uint32_t chunk = blockIdx.x - (lo > 0 ? b.chunk_end[lo - 1] : 0u);
+  const int64_t block = static_cast<int64_t>(chunk) * (kThreads / 32) + (threadIdx.x >> 5);
+  const int64_t at = block * kBlock + (threadIdx.x & 31) * kLane;
+  if (block * kBlock >= t.n) return;   // whole warps
+  const int there = t.n - at >= kLane ? kLane : t.n > at ? static_cast<int>(t.n - at) : 0;
+  const bool p16 = t.flags & kParam16, g16 = t.flags & kGrad16, s8 = t.flags & kState8;
+  const bool al = t.flags & kAligned;
+  grid_dependency_wait();
+  grid_dependents_launch();
+  float p[kLane], g[kLane], m[kLane], v[kLane];
+  load8(t.g, g16, al, at, there, g);
+  load8(t.p, p16, al, at, there, p);
+  if (s8) {
+    decode<__NV_E4M3>(load_codes(t.m, al, at, there), t.m_scale[block], m);
+    decode<__NV_E5M2>(load_codes(t.v, al, at, there), t.v_scale[block], v);
+  } else {
+    load8(t.m, false, al, at, there, m);
+    load8(t.v, false, al, at, there, v);
+  }
+  const float gs = b.h.grad_scale != nullptr ? *b.h.grad_scale : 1.0f;
+#pragma unroll
+  for (int i = 0; i < kLane; ++i) {
+    // each operation rounded by itself, as the definition has them
+    const float gi = __fmul_rn(g[i], gs);
+    m[i] = __fadd_rn(__fmul_rn(b.h.beta1, m[i]), __fmul_rn(b.h.one_beta1, gi));
+    v[i] = __fadd_rn(__fmul_rn(b.h.beta2, v[i]), __fmul_rn(__fmul_rn(b.h.one_beta2, gi), gi));
+    const float den = sqrtf(v[i]) * b.h.root_fix2 + b.h.eps;
+    p[i] = p[i] * t.decay - t.lr * (m[i] / den);
+  }
+  store8(t.p, p16, al, at, there, p);
+  if (t.copy != nullptr) store8(t.copy, true, al, at, there, p);
+  if (!s8) {
+    store8(t.m, false, al, at, there, m);
+    store8(t.v, false, al, at, there, v);
+    return;
+  }
+  uint32_t m_most = 0u, v_most = 0u;
+#pragma unroll
+  for (int i = 0; i < kLane; ++i)
+    if (i < there) {
+      m_most = max(m_most, finite_bits(m[i]));
+      v_most = max(v_most, finite_bits(v[i]));
+    }
+  m_most = __reduce_max_sync(0xffffffffu, m_most);
+  v_most = __reduce_max_sync(0xffffffffu, v_most);
+  const int mf = scale_field<8>(m_most), vf = scale_field<15>(v_most);
+  const float m_inv = __uint_as_float(static_cast<uint32_t>(254 - mf) << 23);
+  const float v_inv = __uint_as_float(static_cast<uint32_t>(254 - vf) << 23);
+  uint32_t mw[2] = {0u, 0u}, vw[2] = {0u, 0u};
+#pragma unroll
+  for (int i = 0; i < kLane; ++i) {
+    const uint32_t r = random_bits(b.h.salt, t.first_random + static_cast<uint32_t>(at) + i);
+    uint32_t mc = encode<7, 20>(m[i], m_inv, r >> 16);
+    uint32_t vc = encode<15, 21>(v[i], v_inv, r & 0xFFFFu);
+    if (vc == 0u && v[i] > 0.0f) vc = 1u;
+    if (!(fabsf(m[i]) < INFINITY)) mc = 0x7Fu;
+    if (!(v[i] < INFINITY)) vc = v[i] > 0.0f ? 0x7Cu : 0x7Fu;   // infinity, NaN
+    mc |= (__float_as_uint(m[i]) >> 24) & 0x80u;
+    mw[i / 4] |= mc << (8 * (i % 4));
+    vw[i / 4] |= vc << (8 * (i % 4));
+  }
+  store_codes(t.m, al, at, there, mw);
+  store_codes(t.v, al, at, there, vw);
+  if ((threadIdx.x & 31) == 0) {
+    t.m_scale[block] = __uint_as_float(static_cast<uint32_t>(mf) << 23);
+    t.v_scale[block] = __uint_as_float(static_cast<uint32_t>(vf) << 23);
+  }
+}
+
+// Tensors of one launch: what the 32764 bytes of a kernel's parameters hold.
+constexpr int kMost = 352;
+static_assert(sizeof(Batch<kMost>) <= 32764, "kernel parameters");
+
+template <int N>
+cudaError_t launch(const Batch<kMost>& all, cudaStream_t s) {
+  Batch<N> b;
+  b.h = all.h;
+  for (int i = 0; i < all.h.count; ++i) {
+    b.chunk_end[i] = all.chunk_end[i];
+    b.t[i] = all.t[i];
+  }
+  return launch_dependent(adamw_kernel<N>, dim3(b.chunk_end[b.h.count - 1]), dim3(kThreads), 0, s, b);
+}
+
+cudaError_t launch_batch(const Batch<kMost>& b, cudaStream_t s) {
+  if (b.h.count == 0) return cudaSuccess;
+  if (b.h.count <= 8) return launch<8>(b, s);
+  if (b.h.count <= 64) return launch<64>(b, s);
+  return launch_dependent(adamw_kernel<kMost>, dim3(b.chunk_end[b.h.count - 1]), dim3(kThreads), 0, s,
+                          b);
+}
+
+}  // namespace
+
+tbn_status launch_adamw(const tbn_adamw_tensor* tensors, int count, const tbn_adamw_hyper& h,
+                        cudaStream_t s) {
+  static thread_local Batch<kMost> b;   // 30 KB: off the stack
+  const double fix1 = 1.0 - std::pow(h.beta1, static_cast<double>(h.step));
+  const double fix2 = 1.0 - std::pow(h.beta2, static_cast<double>(h.step));
+  b.h.beta1 = static_cast<float>(h.beta1);
+  b.h.one_beta1 = static_cast<float>(1.0 - h.beta1);
+  b.h.beta2 = static_cast<float>(h.beta2);
+  b.h.one_beta2 = static_cast<float>(1.0 - h.beta2);
+  b.h.root_fix2 = static_cast<float>(1.0 / std::sqrt(fix2));
+  b.h.eps = static_cast<float>(h.eps);
+  b.h.grad_scale = h.grad_scale;
+  b.h.salt = h.seed * 0x9E3779B9u;
+  b.h.count = 0;
+  uint32_t random = 0;
+  uint64_t chunks = 0;
+  for (int i = 0; i < count; ++i) {
+    const tbn_adamw_tensor& t = tensors[i];
+    const uint32_t first = random;
+    random += static_cast<uint32_t>((t.n + kBlock - 1) / kBlock * kBlock);
+    if (t.n == 0) continue;
+    const uint64_t mine = static_cast<uint64_t>((t.n + kChunk - 1) / kChunk);
+    if (b.h.count == kMost || chunks + mine > 0x7FFFFFFFull) {
+      const cudaError_t e = launch_batch(b, s);
+      if (e != cudaSuccess) return cuda_fail(e, "adamw_kernel");
+      b.h.count = 0;
+      chunks = 0;
+    }
+    chunks += mine;
+    const bool state8 = t.state == TBN_ADAMW_STATE_8BIT;
+    const size_t state_align = state8 ? 8 : 16;
+    const bool al = is_aligned(t.param, 16) && is_aligned(t.grad, 16) &&
+                    is_aligned(t.m, state_align) && is_aligned(t.v, state_align) &&
+                    is_aligned(t.copy, 16);
+    Tensor& d = b.t[b.h.count];
+    d = {t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, static_cast<__nv_bfloat16*>(t.copy), t.n,
+         static_cast<float>(h.lr * t.lr_scale / fix1),
+         static_cast<float>(1.0 - h.lr * t.lr_scale * t.weight_decay), first,
+         (t.param_dtype == TBN_BF16 ? kParam16 : 0u) | (t.grad_dtype == TBN_BF16 ? kGrad16 : 0u) |
+             (state8 ? kState8 : 0u) | (al ? kAligned : 0u)};
+    b.chunk_end[b.h.count++] = static_cast<uint32_t>(chunks);
+  }
+  const cudaError_t e = launch_batch(b, s);
+  return e == cudaSuccess ? TBN_OK : cuda_fail(e, "adamw_kernel");
+}
+
+}  // namespace tbn

@@ -830,6 +830,17 @@ extern "C" tbn_status tbn_packed_call(int op, const int64_t* v) {
       return tbn_conv2d_bwd_filter(ptr(0), ptr(1), v[2], v[3], v[4], v[5], v[6], v[7], v[8], v[9],
                                    v[10], v[11], v[12], f32(13), ptr(14),
                                    static_cast<size_t>(v[15]), ptr(16));
+    case 5: {
+      double eps;
+      std::memcpy(&eps, &v[8], sizeof(eps));
+      return tbn_layernorm_fwd(ptr(0), dt(1), v[2], v[3], v[4], ptr(5), ptr(6), dt(7),
+                               static_cast<float>(eps), ptr(9), dt(10), v[11], f32(12), f32(13),
+                               ptr(14));
+    }
+    case 6:
+      return tbn_layernorm_bwd(ptr(0), dt(1), v[2], ptr(3), dt(4), v[5], v[6], v[7], f32(8), f32(9),
+                               ptr(10), dt(11), ptr(12), v[13], ptr(14), v[15], f32(16), f32(17),
+                               ptr(18), static_cast<size_t>(v[19]), ptr(20));
   }
   return fail(TBN_ERR_INVALID_ARG, "packed call: unknown operation %d", op);
 }

@@ -1,0 +1,141 @@
+// tbn_api_train.cu -- extern "C" entry points (include/tbn.h) of the operators
+// beside the two-bit layers: layer norm, the AdamW step and low-rank adapters.
+// Argument validation on the host, dispatch to the kernels.
+#include <cuda_runtime.h>
+
+#include "tbn.h"
+#include "tbn_internal.h"
+
+using namespace tbn;
+
+namespace {
+
+constexpr int64_t kLim31 = int64_t(1) << 31;
+constexpr int64_t kLim46 = int64_t(1) << 46;
+
+bool dtype_ok(int d) { return d == TBN_F32 || d == TBN_BF16; }
+
+// rows x ld elements stay below 2^46 (no address computation overflows)
+bool span_ok(int64_t rows, int64_t ld) { return rows == 0 || ld < kLim46 / (rows > 0 ? rows : 1); }
+
+tbn_status norm_sizes(const char* what, int64_t rows, int64_t D) {
+  if (rows < 0 || D < 1) return fail(TBN_ERR_INVALID_ARG, "%s: needs rows >= 0 and D >= 1", what);
+  if (rows >= kLim31 || D > (1 << 28))
+    return fail(TBN_ERR_UNSUPPORTED, "%s: 2^31 rows or more, or D above 2^28", what);
+  return TBN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+tbn_status tbn_layernorm_fwd(const void* x, tbn_dtype xdt, int64_t rows, int64_t D, int64_t ldx,
+                             const void* gamma, const void* beta, tbn_dtype wdt, float eps,
+                             void* y, tbn_dtype ydt, int64_t ldy, float* mean, float* rstd,
+                             tbn_stream stream) {
+  const char* what = "layernorm_fwd";
+  if (!dtype_ok(xdt) || !dtype_ok(ydt) || !dtype_ok(wdt))
+    return fail(TBN_ERR_INVALID_ARG, "%s: bad dtype", what);
+  if (ydt != xdt && ydt != TBN_BF16)
+    return fail(TBN_ERR_UNSUPPORTED, "%s: y has x's type or bf16", what);
+  if (const tbn_status st = norm_sizes(what, rows, D)) return st;
+  if (!(eps >= 0.0f)) return fail(TBN_ERR_INVALID_ARG, "%s: eps must be >= 0", what);
+  if (ldx < D || ldy < D) return fail(TBN_ERR_INVALID_ARG, "%s: a row stride is below D", what);
+  if (!span_ok(rows, ldx) || !span_ok(rows, ldy))
+    return fail(TBN_ERR_UNSUPPORTED, "%s: tensor too large", what);
+  if (rows == 0) return TBN_OK;
+  if (!x || !y) return fail(TBN_ERR_INVALID_ARG, "%s: null pointer", what);
+  if (!is_aligned(x, dtype_size(xdt)) || !is_aligned(y, dtype_size(ydt)) ||
+      !is_aligned(gamma, dtype_size(wdt)) || !is_aligned(beta, dtype_size(wdt)) ||
+      !is_aligned(mean, 4) || !is_aligned(rstd, 4))
+    return fail(TBN_ERR_MISALIGNED, "%s: pointer not aligned to its element size", what);
+  LayerNormProblem p{};
+  p.rows = rows; p.D = D; p.ldx = ldx; p.ldy = ldy;
+  p.xdt = xdt; p.ydt = ydt; p.wdt = wdt;
+  p.x = x; p.gamma = gamma; p.beta = beta; p.y = y;
+  p.mean_out = mean; p.rstd_out = rstd; p.eps = eps;
+  return launch_layernorm_fwd(p, as_stream(stream));
+}
+
+size_t tbn_layernorm_bwd_workspace_bytes(int64_t rows, int64_t D) {
+  if (norm_sizes("layernorm_bwd_workspace_bytes", rows, D) != TBN_OK) return 0;
+  return layernorm_bwd_workspace_bytes(rows, D);
+}
+
+tbn_status tbn_layernorm_bwd(const void* dy, tbn_dtype ydt, int64_t lddy, const void* x,
+                             tbn_dtype xdt, int64_t rows, int64_t D, int64_t ldx,
+                             const float* mean, const float* rstd, const void* gamma,
+                             tbn_dtype wdt, const void* dres, int64_t lddres, void* dx,
+                             int64_t lddx, float* dgamma, float* dbeta, void* workspace,
+                             size_t workspace_bytes, tbn_stream stream) {
+  const char* what = "layernorm_bwd";
+  if (!dtype_ok(xdt) || !dtype_ok(ydt) || !dtype_ok(wdt))
+    return fail(TBN_ERR_INVALID_ARG, "%s: bad dtype", what);
+  if (ydt != xdt && ydt != TBN_BF16)
+    return fail(TBN_ERR_UNSUPPORTED, "%s: dy has x's type or bf16", what);
+  if (const tbn_status st = norm_sizes(what, rows, D)) return st;
+  if (ldx < D || lddy < D || lddx < D || (dres && lddres < D))
+    return fail(TBN_ERR_INVALID_ARG, "%s: a row stride is below D", what);
+  if (!span_ok(rows, ldx) || !span_ok(rows, lddy) || !span_ok(rows, lddx) ||
+      (dres && !span_ok(rows, lddres)))
+    return fail(TBN_ERR_UNSUPPORTED, "%s: tensor too large", what);
+  if (rows > 0 && (!dy || !x || !mean || !rstd || !dx))
+    return fail(TBN_ERR_INVALID_ARG, "%s: null pointer", what);
+  if (!is_aligned(dy, dtype_size(ydt)) || !is_aligned(x, dtype_size(xdt)) ||
+      !is_aligned(dx, dtype_size(xdt)) || !is_aligned(dres, dtype_size(xdt)) ||
+      !is_aligned(gamma, dtype_size(wdt)) || !is_aligned(mean, 4) || !is_aligned(rstd, 4) ||
+      !is_aligned(dgamma, 4) || !is_aligned(dbeta, 4))
+    return fail(TBN_ERR_MISALIGNED, "%s: pointer not aligned to its element size", what);
+  if (dgamma || dbeta) {
+    const size_t need = layernorm_bwd_workspace_bytes(rows, D);
+    if (!workspace || workspace_bytes < need)
+      return fail(TBN_ERR_INVALID_ARG, "%s: workspace of %zu bytes needed", what, need);
+    if (!is_aligned(workspace, 16))
+      return fail(TBN_ERR_MISALIGNED, "%s: workspace must be 16-byte aligned", what);
+  } else if (rows == 0) {
+    return TBN_OK;
+  }
+  LayerNormProblem p{};
+  p.rows = rows; p.D = D; p.ldx = ldx; p.ldy = lddy; p.lddres = lddres; p.lddx = lddx;
+  p.xdt = xdt; p.ydt = ydt; p.wdt = wdt;
+  p.x = x; p.dy = dy; p.dres = dres; p.gamma = gamma; p.dx = dx;
+  p.mean = mean; p.rstd = rstd;
+  p.dgamma = dgamma; p.dbeta = dbeta; p.part = static_cast<float*>(workspace);
+  return launch_layernorm_bwd(p, as_stream(stream));
+}
+
+tbn_status tbn_adamw_step(const tbn_adamw_tensor* tensors, int count, const tbn_adamw_hyper* hyper,
+                          tbn_stream stream) {
+  const char* what = "adamw_step";
+  if (count < 0 || (count > 0 && !tensors) || !hyper)
+    return fail(TBN_ERR_INVALID_ARG, "%s: null pointer or negative count", what);
+  const tbn_adamw_hyper& h = *hyper;
+  if (!(h.lr >= 0.0) || !(h.beta1 >= 0.0 && h.beta1 < 1.0) || !(h.beta2 >= 0.0 && h.beta2 < 1.0) ||
+      !(h.eps >= 0.0) || h.step < 1)
+    return fail(TBN_ERR_INVALID_ARG, "%s: needs lr, eps >= 0, betas in [0, 1) and step >= 1", what);
+  if (!is_aligned(h.grad_scale, 4))
+    return fail(TBN_ERR_MISALIGNED, "%s: grad_scale not aligned to its element size", what);
+  for (int i = 0; i < count; ++i) {
+    const tbn_adamw_tensor& t = tensors[i];
+    if (t.n < 0 || !dtype_ok(t.param_dtype) || !dtype_ok(t.grad_dtype) ||
+        (t.state != TBN_ADAMW_STATE_32BIT && t.state != TBN_ADAMW_STATE_8BIT))
+      return fail(TBN_ERR_INVALID_ARG, "%s: tensor %d has a bad size, dtype or state", what, i);
+    if (t.n > (int64_t(1) << 40))
+      return fail(TBN_ERR_UNSUPPORTED, "%s: tensor %d is too large", what, i);
+    if (t.n == 0) continue;
+    const bool state8 = t.state == TBN_ADAMW_STATE_8BIT;
+    if (!t.param || !t.grad || !t.m || !t.v || (state8 && (!t.m_scale || !t.v_scale)))
+      return fail(TBN_ERR_INVALID_ARG, "%s: tensor %d has a null pointer", what, i);
+    if (!(t.weight_decay >= 0.0f) || !(t.lr_scale >= 0.0f))
+      return fail(TBN_ERR_INVALID_ARG, "%s: tensor %d needs weight_decay, lr_scale >= 0", what, i);
+    const size_t state_size = state8 ? 1 : 4;
+    if (!is_aligned(t.param, t.param_dtype == TBN_BF16 ? 2 : 4) ||
+        !is_aligned(t.grad, t.grad_dtype == TBN_BF16 ? 2 : 4) || !is_aligned(t.m, state_size) ||
+        !is_aligned(t.v, state_size) || !is_aligned(t.m_scale, 4) || !is_aligned(t.v_scale, 4) ||
+        !is_aligned(t.copy, 2))
+      return fail(TBN_ERR_MISALIGNED, "%s: tensor %d is not aligned to its element size", what, i);
+  }
+  return launch_adamw(tensors, count, h, as_stream(stream));
+}
+
+}  // extern "C"

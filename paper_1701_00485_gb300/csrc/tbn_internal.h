@@ -220,6 +220,26 @@ tbn_status launch_avgpool_global_nhwc(const void* x, tbn_dtype xdt, int64_t N, i
 tbn_status launch_dense_linear(const float* x, int64_t B, int64_t K_in, const float* w,
                                int64_t K_out, void* y, tbn_dtype ydt, int relu,
                                cudaStream_t s);
+// Layer norm after validation (tbn_layernorm.cu).  xdt is the type of x, dx
+// and dres, ydt that of y and dy (with stride ldy both), wdt that of gamma and
+// beta; what a direction does not use stays null.
+struct LayerNormProblem {
+  int64_t rows, D, ldx, ldy, lddres, lddx;
+  tbn_dtype xdt, ydt, wdt;
+  const void *x, *dy, *dres, *gamma, *beta;
+  const float *mean, *rstd;
+  void *y, *dx;
+  float *mean_out, *rstd_out, *dgamma, *dbeta, *part;
+  float eps;
+};
+tbn_status launch_layernorm_fwd(const LayerNormProblem& p, cudaStream_t s);
+size_t layernorm_bwd_workspace_bytes(int64_t rows, int64_t D);
+tbn_status launch_layernorm_bwd(const LayerNormProblem& p, cudaStream_t s);
+
+// AdamW over validated tensors (tbn_adamw.cu).
+tbn_status launch_adamw(const tbn_adamw_tensor* tensors, int count, const tbn_adamw_hyper& h,
+                        cudaStream_t s);
+
 tbn_status launch_nchw_to_nhwc(const void* x, tbn_dtype dt, int64_t N, int64_t C, int64_t H,
                                int64_t W, int64_t C_pad, void* y, cudaStream_t s);
 
