@@ -584,6 +584,65 @@ typedef struct {
 tbn_status tbn_adamw_step(const tbn_adamw_tensor *tensors, int count, const tbn_adamw_hyper *hyper,
                           tbn_stream stream);
 
+/* ------------------------------------------------------------------------
+ * Low-rank adapters of many requests beside a shared projection (the two-bit
+ * one of tbn_linear_fwd, or any other): each of T tokens has at most one of n
+ * adapters, of rank r or less.
+ *   a [n][r][K_in], b [n][r][K_out]   bf16, both rank by rank
+ *   ids [T]      the tokens' adapters, in any order; outside 0 .. n - 1: none.
+ *                NULL: all 0
+ *   ranks [n]    NULL, or the adapters' own ranks (cut to 0 .. r): what a and b
+ *                hold past them is not read
+ *   scale [n]    NULL (1), or the adapters' factors
+ * n <= 1023, r <= 128, T < 2^31, widths up to 2^22.  ids, ranks and scale are
+ * read on the device, in the call's place on the stream. */
+typedef struct {
+  const void *a, *b;
+  int64_t n, r, K_in, K_out;
+  const int32_t *ids;
+  const int32_t *ranks;
+  const float *scale;
+} tbn_adapters;
+
+/* Workspace bytes of the two calls below (backward != 0: of tbn_adapter_bwd);
+ * 0 for sizes that they refuse. */
+size_t tbn_adapter_workspace_bytes(int64_t T, int64_t K_in, int64_t K_out, int64_t n, int64_t r,
+                                   int backward);
+
+/* y_t = base_t + scale_i (a_i x_t) b_i with i = ids[t]; y_t = base_t (or 0)
+ * where there is none.  x [T][K_in] of type xdt, rows ldx elements apart;
+ * y [T][K_out] of type ydt, rows ldy apart; base NULL or of y's type and shape,
+ * rows ldbase apart: the shared projection's output, which y may overwrite
+ * (base = y, ldbase = ldy).  To put an activation or a residual behind the sum
+ * instead, give y to the projection as its epilogue's residual.
+ * v: NULL, or fp32 [T][r] that receives a_i x_t (0 past the rank and for tokens
+ * without adapter), which tbn_adapter_bwd can use.  T = 0 does nothing.
+ * Products of bf16 values are exact, sums are fp32; fp32 activations take part
+ * with all their bits, a_i x_t with 16 bits for a bf16 y and all for an fp32
+ * one.  A token's result depends on its own activations and adapter only.
+ * `workspace`: tbn_adapter_workspace_bytes(.., 0) bytes, 256-byte aligned. */
+tbn_status tbn_adapter_fwd(const tbn_adapters *adapters, const void *x, tbn_dtype xdt, int64_t T,
+                           int64_t ldx, const void *base, int64_t ldbase, void *y, tbn_dtype ydt,
+                           int64_t ldy, float *v, void *workspace, size_t workspace_bytes,
+                           tbn_stream stream);
+
+/* Gradients of tbn_adapter_fwd, with du_t = scale_i b_i dy_t:
+ *   dx_t = base_t + du_t a_i, da_i = sum over i's tokens of du_t x_t^T,
+ *   db_i = sum over i's tokens of scale_i v_t dy_t^T.
+ * dy [T][K_out] of type ydt, x, dx and base (NULL, or the gradient through the
+ * shared projection; may be dx) [T][K_in] of type xdt; da [n][r][K_in] and
+ * db [n][r][K_out] fp32 are written, not added to, with zeros past an adapter's
+ * rank and for adapters without tokens.  dx, da, db: any may be NULL and is
+ * then not computed.  v: what tbn_adapter_fwd wrote, or NULL to have it
+ * computed again.  Sums over tokens are taken in a fixed order: equal inputs
+ * give equal bits.  `workspace`: tbn_adapter_workspace_bytes(.., 1) bytes,
+ * 256-byte aligned. */
+tbn_status tbn_adapter_bwd(const tbn_adapters *adapters, const void *dy, tbn_dtype ydt,
+                           int64_t lddy, const void *x, tbn_dtype xdt, int64_t T, int64_t ldx,
+                           const float *v, const void *base, int64_t ldbase, void *dx,
+                           int64_t lddx, float *da, float *db, void *workspace,
+                           size_t workspace_bytes, tbn_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -35,6 +35,7 @@ __all__ = [
     "tbn_linear_prepare_f8", "tbn_linear_f8_workspace_bytes", "tbn_linear_fwd_f8",
     "tbn_linear_f8_prepared_words", "tbn_conv2d_fwd_quant", "tbn_layernorm_fwd",
     "tbn_layernorm_bwd", "tbn_layernorm_bwd_workspace_bytes", "AdamWPlan", "tbn_adamw_step",
+    "tbn_adapter_fwd", "tbn_adapter_bwd", "tbn_adapter_workspace_bytes",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -63,7 +64,7 @@ EXPORTED = [
     "tbn_space_to_depth", "tbn_linear_prepare_f8", "tbn_linear_f8_workspace_bytes",
     "tbn_linear_fwd_f8", "tbn_linear_f8_prepared_words", "tbn_conv2d_fwd_quant",
     "tbn_layernorm_fwd", "tbn_layernorm_bwd_workspace_bytes", "tbn_layernorm_bwd",
-    "tbn_adamw_step",
+    "tbn_adamw_step", "tbn_adapter_workspace_bytes", "tbn_adapter_fwd", "tbn_adapter_bwd",
 ]
 
 
@@ -160,6 +161,11 @@ def lib():
             "tbn_layernorm_bwd": ([P, I32, I64, P, I32, I64, I64, I64, P, P, P, I32, P, I64, P,
                                    I64, P, P, P, ctypes.c_size_t, P], I32),
             "tbn_adamw_step": ([P, I32, P, P], I32),
+            "tbn_adapter_workspace_bytes": ([I64] * 5 + [I32], ctypes.c_size_t),
+            "tbn_adapter_fwd": ([P, P, I32, I64, I64, P, I64, P, I32, I64, P, P, ctypes.c_size_t,
+                                 P], I32),
+            "tbn_adapter_bwd": ([P, P, I32, I64, P, I32, I64, I64, P, P, I64, P, I64, P, P, P,
+                                 ctypes.c_size_t, P], I32),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -716,5 +722,6 @@ def tbn_selftest_wait_timeout(limit_us: int, stream=None) -> None:
            "tbn_selftest_wait_timeout")
 
 
-from ._train import (AdamWPlan, AdamWTensor, AdamWHyper, tbn_adamw_step,  # noqa: E402
+from ._train import (AdamWHyper, AdamWPlan, AdamWTensor, Adapters, tbn_adamw_step,  # noqa: E402
+                     tbn_adapter_bwd, tbn_adapter_fwd, tbn_adapter_workspace_bytes,
                      tbn_layernorm_bwd, tbn_layernorm_bwd_workspace_bytes, tbn_layernorm_fwd)

@@ -1,5 +1,5 @@
-"""Binding of the operators beside the two-bit layers: layer norm and the
-AdamW step (``tbn.h``).  The names are exported by the package."""
+"""Binding of the operators beside the two-bit layers: layer norm, the AdamW
+step and low-rank adapters (``tbn.h``).  The names are exported by the package."""
 from __future__ import annotations
 
 import ctypes
@@ -9,9 +9,11 @@ import torch
 
 from . import TBN_F32, _check, _dt, _raw_stream, lib
 
-_OP_NORM_FWD, _OP_NORM_BWD = 5, 6
+_OP_NORM_FWD, _OP_NORM_BWD, _OP_ADAPTER_FWD, _OP_ADAPTER_BWD = range(5, 9)
 _pack_norm_fwd = struct.Struct("=8qd6q").pack
 _pack_norm_bwd = struct.Struct("=21q").pack
+_pack_adapter_fwd = struct.Struct("=22q").pack
+_pack_adapter_bwd = struct.Struct("=26q").pack
 _STATE_32BIT, _STATE_8BIT = 0, 1
 _ADAMW_BLOCK = 256
 
@@ -29,6 +31,12 @@ class AdamWHyper(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
                 ("eps", ctypes.c_double), ("step", ctypes.c_int64),
                 ("grad_scale", ctypes.c_void_p), ("seed", ctypes.c_uint32)]
+
+
+class Adapters(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("r", ctypes.c_int64), ("K_in", ctypes.c_int64), ("K_out", ctypes.c_int64),
+                ("ids", ctypes.c_void_p), ("ranks", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
 
 
 def _rows(t, name, shape=None):
@@ -59,6 +67,8 @@ def _flat(t, name, n, dtypes):
 
 _F32 = (torch.float32,)
 _FLOATS = (torch.float32, torch.bfloat16)
+_BF16 = (torch.bfloat16,)
+_I32 = (torch.int32,)
 
 
 def _weights(gamma, beta, D):
@@ -219,6 +229,101 @@ def tbn_adamw_step(plan: AdamWPlan, step: int, lr: float, betas=(0.9, 0.999), ep
     h.seed = seed & 0xFFFFFFFF
     _check(lib().tbn_adamw_step(plan._array, plan.count, ctypes.byref(h), _raw_stream(stream)),
            "tbn_adamw_step")
+
+
+def tbn_adapter_workspace_bytes(T: int, K_in: int, K_out: int, n: int, r: int,
+                                backward: bool = False) -> int:
+    """Scratch bytes of tbn_adapter_fwd, or with backward of tbn_adapter_bwd."""
+    return int(lib().tbn_adapter_workspace_bytes(T, K_in, K_out, n, r, 1 if backward else 0))
+
+
+def _adapters(a, b, T, ids, scale, ranks):
+    """The first nine arguments of a packed adapter call."""
+    if a.dim() != 3 or b.dim() != 3 or a.shape[:2] != b.shape[:2]:
+        raise ValueError("a must be [n, r, K_in] and b [n, r, K_out]")
+    n, r, K_in = a.shape
+    return (_flat(a, "a", n * r * K_in, _BF16), _flat(b, "b", b.numel(), _BF16), n, r, K_in,
+            b.shape[2], _flat(ids, "ids", T, _I32), _flat(ranks, "ranks", n, _I32),
+            _flat(scale, "scale", n, _F32))
+
+
+def _base(base, like, name):
+    if base is None:
+        return 0, 0
+    if base.dtype != like.dtype:
+        raise ValueError("base must have %s's dtype" % name)
+    return base.data_ptr(), _rows(base, "base", like.shape)
+
+
+def tbn_adapter_fwd(x, a, b, ids=None, scale=None, ranks=None, base=None, out_dtype=None,
+                    out=None, v=None, workspace=None, stream=None):
+    """Low-rank adapters of many requests: y_t = base_t + scale_i (a_i x_t) b_i
+    with i = ids[t].
+
+    x [T, K_in] (bf16 or fp32; rows contiguous, any stride between them),
+    a [n, r, K_in] and b [n, r, K_out] bf16, both rank by rank; ids [T] int32 in
+    any order, values outside 0 .. n - 1 for tokens without an adapter, None for
+    adapter 0 everywhere; scale [n] fp32; ranks [n] int32 (what a and b hold past
+    them is not read); base [T, K_out] of y's dtype, the shared projection's
+    output, which `out` may be.  v: None, or fp32 [T, r] that receives a_i x_t
+    for tbn_adapter_bwd.  y has base's, out's, out_dtype's or x's dtype."""
+    ldx = _rows(x, "x")
+    T = x.shape[0]
+    ad = _adapters(a, b, T, ids, scale, ranks)
+    if x.shape[1] != ad[4]:
+        raise ValueError("x has %d columns, a expects %d" % (x.shape[1], ad[4]))
+    if out is None:
+        dt = out_dtype or (x if base is None else base).dtype
+        out = torch.empty((T, ad[5]), dtype=dt, device=x.device)
+    if workspace is None:
+        workspace = _scratch(tbn_adapter_workspace_bytes(T, ad[4], ad[5], ad[2], ad[3]), x.device,
+                             stream)
+    ldy = _rows(out, "out", (T, ad[5]))
+    _call_packed(_OP_ADAPTER_FWD, "tbn_adapter_fwd", _pack_adapter_fwd(
+        *ad, x.data_ptr(), _dt(x), T, ldx, *_base(base, out, "y"), out.data_ptr(), _dt(out), ldy,
+        _flat(v, "v", T * ad[3], _F32), workspace.data_ptr(), _bytes(workspace, "workspace"),
+        _raw_stream(stream)))
+    return out
+
+
+def tbn_adapter_bwd(dy, x, a, b, ids=None, scale=None, ranks=None, v=None, base=None, dx=None,
+                    da=None, db=None, need=(True, True, True), workspace=None, stream=None):
+    """Gradients of tbn_adapter_fwd for dy [T, K_out]: (dx, da, db).
+
+    dx has x's dtype and is added to base, the gradient through the shared
+    projection, where one is given (`dx` may be it); da and db are fp32 of a's and
+    b's shape, zero past an adapter's rank and for adapters without tokens.  v:
+    what tbn_adapter_fwd wrote, or None to compute it again.  need: which of the
+    three are wanted; the others come back as None."""
+    ldx, lddy = _rows(x, "x"), _rows(dy, "dy")
+    T = x.shape[0]
+    ad = _adapters(a, b, T, ids, scale, ranks)
+    if x.shape[1] != ad[4] or tuple(dy.shape) != (T, ad[5]):
+        raise ValueError("x must be [T, K_in] and dy [T, K_out] of a and b")
+    if not need[0]:
+        dx = None
+    elif dx is None:
+        dx = torch.empty((T, ad[4]), dtype=x.dtype, device=x.device)
+    elif dx.dtype != x.dtype:
+        raise ValueError("dx must have x's dtype")
+    if not need[1]:
+        da = None
+    elif da is None:
+        da = torch.empty(a.shape, dtype=torch.float32, device=x.device)
+    if not need[2]:
+        db = None
+    elif db is None:
+        db = torch.empty(b.shape, dtype=torch.float32, device=x.device)
+    if workspace is None:
+        workspace = _scratch(tbn_adapter_workspace_bytes(T, ad[4], ad[5], ad[2], ad[3], True),
+                             x.device, stream)
+    _call_packed(_OP_ADAPTER_BWD, "tbn_adapter_bwd", _pack_adapter_bwd(
+        *ad, dy.data_ptr(), _dt(dy), lddy, x.data_ptr(), _dt(x), T, ldx,
+        _flat(v, "v", T * ad[3], _F32), *(_base(base, x, "x") if dx is not None else (0, 0)),
+        0 if dx is None else dx.data_ptr(), 0 if dx is None else _rows(dx, "dx", x.shape),
+        _flat(da, "da", a.numel(), _F32), _flat(db, "db", b.numel(), _F32), workspace.data_ptr(),
+        _bytes(workspace, "workspace"), _raw_stream(stream)))
+    return dx, da, db
 
 
 def _call_packed(op, where, block):

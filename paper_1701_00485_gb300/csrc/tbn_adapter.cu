@@ -1,0 +1,926 @@
+// tbn_adapter.cu -- low-rank adapters of many requests beside a shared
+// projection.  Token t of adapter i = ids[t], with a_i [r][K_in] and
+// b_i [r][K_out] both stored rank by rank:
+//
+//   v_t = a_i x_t,                 y_t = base_t + scale_i v_t b_i
+// and backward
+//   du_t = scale_i b_i dy_t,       dx_t = base_t + du_t a_i
+//   da_i = sum over i's tokens of du_t x_t^T,   db_i = sum of scale_i v_t dy_t^T
+//
+// With that storage forward and backward are three products: "shrink" (a
+// contraction over a layer's width), "expand" (over the rank) and "grad" (over
+// an adapter's tokens).  A call first sorts its tokens by adapter (route_kernel,
+// stable, so that sums over tokens have a fixed order) and cuts each adapter's
+// into tiles; every tile reads its own adapter only, so that nothing of one
+// request's adapter, not even an infinity, reaches another's tokens.
+//
+// All three run on the tensor cores in bf16 with 32-bit sums.  What has 32 bits
+// enters as a sum of bf16 terms, each the leading eight bits of what the ones
+// before leave: three terms are the value exactly, and two (16 bits) are used
+// where the result is rounded to bf16.
+#include <cuda_bf16.h>
+
+#include <type_traits>
+
+#include "tbn_device.cuh"
+#include "tbn_internal.h"
+
+namespace tbn {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTile = 64;          // tokens of a tile
+constexpr int kChunk = 64;         // elements of a contraction's step
+constexpr int kCols = 128;         // output columns of expand and grad
+constexpr int kHalf = kTile * 128; // bytes of 64 rows x 64 bf16
+
+// ------------------------------------------------------------- primitives
+// Rows of 64 bf16 as eight 16-byte chunks, chunk c of row r at c ^ (r & 7):
+// conflict-free for ldmatrix.
+__device__ __forceinline__ uint32_t tile_off(int row, int chunk) {
+  return static_cast<uint32_t>(row * 128 + ((chunk ^ (row & 7)) << 4));
+}
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+
+__device__ __forceinline__ void ldsm4_trans(uint32_t (&r)[4], uint32_t addr) {
+  ldmatrix_x4_trans(addr, r[0], r[1], r[2], r[3]);
+}
+
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
+                                    uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 "
+      "{%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// The leading kTerms bf16 terms of v: all but the last cut off (so that no
+// finite value becomes infinite), the last rounded to nearest.  Infinities and
+// NaN go into the first term alone.
+template <int kTerms>
+__device__ __forceinline__ void split(float v, float (&t)[kTerms]) {
+  const bool finite = (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u;
+#pragma unroll
+  for (int i = 0; i < kTerms; ++i) {
+    t[i] = i + 1 < kTerms && finite ? __uint_as_float(__float_as_uint(v) & 0xFFFF0000u) : v;
+    v = finite ? v - t[i] : 0.0f;
+  }
+}
+
+// Two neighbouring values into the kTerms tiles at `tile`, `stride` bytes apart.
+template <int kTerms>
+__device__ __forceinline__ void store_pair(uint8_t* tile, uint32_t stride, uint32_t off, float v0,
+                                           float v1) {
+  float a[kTerms], b[kTerms];
+  split(v0, a);
+  split(v1, b);
+#pragma unroll
+  for (int i = 0; i < kTerms; ++i)
+    *reinterpret_cast<uint32_t*>(tile + i * stride + off) = pack_bf16x2(a[i], b[i]);
+}
+
+// Sixteen consecutive elements of a row, held as they come.
+template <typename T>
+struct Piece;
+template <>
+struct Piece<__nv_bfloat16> {
+  uint4 q[2];
+};
+template <>
+struct Piece<float> {
+  float4 q[4];
+};
+
+// Elements [at, at + 16) of the row at p, of which K exist; zeros past the end
+// and for p = nullptr.
+__device__ __forceinline__ void load_piece(Piece<__nv_bfloat16>& d, const __nv_bfloat16* p, int at,
+                                           int K, bool aligned) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int e = at + 8 * i;
+    d.q[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (p == nullptr || e >= K) continue;
+    if (aligned) {
+      d.q[i] = __ldg(reinterpret_cast<const uint4*>(p + e));
+    } else {
+      uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (e + j < K)
+          w[j / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(p[e + j])) << (16 * (j % 2));
+      d.q[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
+__device__ __forceinline__ void load_piece(Piece<float>& d, const float* p, int at, int K,
+                                           bool aligned) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int e = at + 4 * i;
+    d.q[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (p == nullptr || e >= K) continue;
+    if (aligned) {
+      d.q[i] = __ldg(reinterpret_cast<const float4*>(p + e));
+    } else {
+      d.q[i].x = p[e];
+      if (e + 1 < K) d.q[i].y = p[e + 1];
+      if (e + 2 < K) d.q[i].z = p[e + 2];
+      if (e + 3 < K) d.q[i].w = p[e + 3];
+    }
+  }
+}
+
+// Into chunks c and c + 1 of a row of the tile (fp32: of its three terms).
+__device__ __forceinline__ void store_piece(uint8_t* tile, uint32_t, int row, int c,
+                                            const Piece<__nv_bfloat16>& d) {
+  *reinterpret_cast<uint4*>(tile + tile_off(row, c)) = d.q[0];
+  *reinterpret_cast<uint4*>(tile + tile_off(row, c + 1)) = d.q[1];
+}
+
+__device__ __forceinline__ void store_piece(uint8_t* tile, uint32_t stride, int row, int c,
+                                            const Piece<float>& d) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t off = tile_off(row, c + i / 2) + 8 * (i % 2);
+    store_pair<3>(tile, stride, off, d.q[i].x, d.q[i].y);
+    store_pair<3>(tile, stride, off + 4, d.q[i].z, d.q[i].w);
+  }
+}
+
+template <typename T>
+constexpr int kTermsOf = sizeof(T) == 2 ? 1 : 3;
+
+// ------------------------------------------------------------------ route
+struct Route {
+  int* counts;     // [0] tiles, [1] grad items
+  int* perm;       // [T] tokens sorted by adapter; those of none last
+  int4* tiles;     // adapter (-1: none), first position, tokens
+  int4* items;     // grad items: adapter, first position, tokens, 0
+  int* item_begin; // [n + 1] grad items of adapters 0 .. i - 1
+};
+
+// One block.  Warp w owns the w-th of 32 runs of tokens; it counts each
+// adapter's (lanes of equal ids find each other, so that no two add at once),
+// the counts are summed over adapters and warps, and the warp goes through its
+// run once more to place the tokens: the order within an adapter is kept.
+__global__ void __launch_bounds__(1024) route_kernel(const int32_t* ids, int T, int n,
+                                                     int tokens_per_item, Route r) {
+  extern __shared__ int sh[];          // counts [32][n + 1], then starts [n + 2]
+  __shared__ int warp_sum[32][2], total[2];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int groups = n + 1;            // the last: no adapter
+  int* start = sh + 32 * groups;
+  grid_dependency_wait();
+  grid_dependents_launch();
+  for (int i = tid; i < 32 * groups; i += 1024) sh[i] = 0;
+  __syncthreads();
+  const int run = (T + 31) / 32;
+  const int beg = min(T, warp * run), end = min(T, beg + run);
+  const auto group_of = [&](int t) {
+    const int id = ids != nullptr ? ids[t] : 0;
+    return id >= 0 && id < n ? id : n;
+  };
+  for (int t0 = beg; t0 < end; t0 += 32) {
+    const int t = t0 + lane;
+    const int g = t < end ? group_of(t) : -1;
+    const uint32_t same = __match_any_sync(0xffffffffu, g);
+    if (g >= 0 && lane == __ffs(same) - 1) sh[warp * groups + g] += __popc(same);
+    __syncwarp();
+  }
+  __syncthreads();
+  // thread g: adapter g's tokens, tiles and items; exclusive sums over adapters
+  int tokens = 0;
+  if (tid < groups) {
+    for (int w = 0; w < 32; ++w) {
+      const int c = sh[w * groups + tid];
+      sh[w * groups + tid] = tokens;
+      tokens += c;
+    }
+  }
+  const int tiles = (tokens + kTile - 1) / kTile;
+  const int items = tid < n ? (tokens + tokens_per_item - 1) / tokens_per_item : 0;
+  const auto exclusive = [&](int v, int* sum_all) {
+    int s = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, s, o);
+      if (lane >= o) s += u;
+    }
+    if (lane == 31) warp_sum[warp][0] = s;
+    __syncthreads();
+    if (warp == 0) {
+      int w = warp_sum[lane][0], x = w;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += u;
+      }
+      warp_sum[lane][1] = x - w;
+      if (lane == 31) *sum_all = x;
+    }
+    __syncthreads();
+    return s - v + warp_sum[warp][1];
+  };
+  __shared__ int unused;
+  const int first = exclusive(tokens, &unused);
+  const int first_tile = exclusive(tiles, &total[0]);
+  const int first_item = exclusive(items, &total[1]);
+  if (tid < groups) {
+    start[tid] = first;
+    const int adapter = tid < n ? tid : -1;
+    for (int i = 0; i < tiles; ++i)
+      r.tiles[first_tile + i] =
+          make_int4(adapter, first + i * kTile, min(kTile, tokens - i * kTile), 0);
+    for (int i = 0; i < items; ++i)
+      r.items[first_item + i] = make_int4(adapter, first + i * tokens_per_item,
+                                          min(tokens_per_item, tokens - i * tokens_per_item), 0);
+    r.item_begin[tid] = first_item;
+  }
+  if (tid == 0) {
+    r.counts[0] = total[0];
+    r.counts[1] = total[1];
+  }
+  __syncthreads();
+  for (int t0 = beg; t0 < end; t0 += 32) {
+    const int t = t0 + lane;
+    const int g = t < end ? group_of(t) : -1;
+    const uint32_t same = __match_any_sync(0xffffffffu, g);
+    if (g >= 0) {
+      const int at = start[g] + sh[warp * groups + g] + __popc(same & ((1u << lane) - 1u));
+      r.perm[at] = t;
+    }
+    __syncwarp();
+    if (g >= 0 && lane == __ffs(same) - 1) sh[warp * groups + g] += __popc(same);
+    __syncwarp();
+  }
+}
+
+struct Adapters {
+  const int32_t* ranks;
+  const float* scale;
+  int r;
+  __device__ __forceinline__ int rank(int i) const {
+    return ranks != nullptr ? max(0, min(ranks[i], r)) : r;
+  }
+  __device__ __forceinline__ float factor(int i) const {
+    return scale != nullptr ? scale[i] : 1.0f;
+  }
+};
+
+// ----------------------------------------------------------------- shrink
+struct ShrinkArgs {
+  Route route;
+  Adapters ad;
+  const void* x;
+  const __nv_bfloat16* w;    // [n][r][K]
+  float* part;               // [splits][T][r], by sorted position
+  int64_t ldx;
+  int T, K, chunks, chunks_per;
+  int x_aligned, w_aligned;
+};
+
+// CTA (tile, split): 64 tokens x the ranks over a range of K.  Warp w takes 16
+// tokens and every other 32 of a chunk's 64 elements; the two halves are added
+// at the end.
+template <typename T, int RP>
+__global__ void __launch_bounds__(kThreads) shrink_kernel(const ShrinkArgs a) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  constexpr int kTerms = kTermsOf<T>;
+  constexpr int kStage = kTerms * kHalf + RP * 128;
+  constexpr int kPieces = (RP * 8 + kThreads - 1) / kThreads;   // 16-byte pieces of w a thread
+  grid_dependency_wait();
+  grid_dependents_launch();
+  if (static_cast<int>(blockIdx.x) >= a.route.counts[0]) return;
+  const int4 tile = a.route.tiles[blockIdx.x];
+  if (tile.x < 0) return;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = a.ad.rank(tile.x);
+  const int c0 = blockIdx.y * a.chunks_per, c1 = min(a.chunks, c0 + a.chunks_per);
+  const int row = tid >> 2, q = tid & 3;
+  const T* xrow = nullptr;
+  if (row < tile.z)
+    xrow = static_cast<const T*>(a.x) + a.route.perm[tile.y + row] * a.ldx;
+  const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * a.ad.r * a.K;
+  Piece<T> px;
+  uint4 pw[kPieces];
+  const auto load = [&](int c) {
+    load_piece(px, xrow, c * kChunk + 16 * q, a.K, a.x_aligned);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int p = tid + i * kThreads, wr = p >> 3, e = c * kChunk + 8 * (p & 7);
+      pw[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (wr < rank && e < a.K) {
+        const __nv_bfloat16* src = w + static_cast<int64_t>(wr) * a.K + e;
+        if (a.w_aligned) {
+          pw[i] = __ldg(reinterpret_cast<const uint4*>(src));
+        } else {
+          uint32_t u[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (e + j < a.K)
+              u[j / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(src[j])) << (16 * (j % 2));
+          pw[i] = make_uint4(u[0], u[1], u[2], u[3]);
+        }
+      }
+    }
+  };
+  float acc[RP / 8][4];
+#pragma unroll
+  for (int i = 0; i < RP / 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = 0.0f;
+  const int tg = 16 * (warp & 3), kh = warp >> 2, mi = lane >> 3, lr = lane & 7;
+  load(c0);
+  for (int c = c0; c < c1; ++c) {
+    uint8_t* st = smem + ((c - c0) & 1) * kStage;
+    uint8_t* sw = st + kTerms * kHalf;
+    store_piece(st, kHalf, row, 2 * q, px);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int p = tid + i * kThreads;
+      if (p < RP * 8) *reinterpret_cast<uint4*>(sw + tile_off(p >> 3, p & 7)) = pw[i];
+    }
+    __syncthreads();   // two stages: the one written next was read before this
+    if (c + 1 < c1) load(c + 1);
+    const uint32_t sx = smem_addr(st), sww = smem_addr(sw);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int ks = 2 * kh + s;
+      uint32_t bf[RP / 16][4];
+#pragma unroll
+      for (int nt = 0; nt < RP / 16; ++nt)
+        ldsm4(bf[nt], sww + tile_off(16 * nt + 8 * (mi >> 1) + lr, 2 * ks + (mi & 1)));
+#pragma unroll
+      for (int t = 0; t < kTerms; ++t) {
+        uint32_t af[4];
+        ldsm4(af, sx + t * kHalf + tile_off(tg + 8 * (mi & 1) + lr, 2 * ks + (mi >> 1)));
+#pragma unroll
+        for (int nt = 0; nt < RP / 16; ++nt) {
+          mma(acc[2 * nt], af, bf[nt][0], bf[nt][1]);
+          mma(acc[2 * nt + 1], af, bf[nt][2], bf[nt][3]);
+        }
+      }
+    }
+  }
+  __syncthreads();
+  float* sum = reinterpret_cast<float*>(smem);   // [64][RP]
+  const int g = lane >> 2, t2 = 2 * (lane & 3);
+  if (kh == 1) {
+#pragma unroll
+    for (int nt = 0; nt < RP / 8; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        sum[(tg + g + 8 * (i >> 1)) * RP + 8 * nt + t2 + (i & 1)] = acc[nt][i];
+  }
+  __syncthreads();
+  if (kh == 0) {
+    float* part = a.part + (static_cast<int64_t>(blockIdx.y) * a.T + tile.y) * a.ad.r;
+#pragma unroll
+    for (int nt = 0; nt < RP / 8; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int m = tg + g + 8 * (i >> 1), col = 8 * nt + t2 + (i & 1);
+        if (m < tile.z && col < a.ad.r)
+          part[static_cast<int64_t>(m) * a.ad.r + col] = acc[nt][i] + sum[m * RP + col];
+      }
+  }
+}
+
+// ------------------------------------------------- the low-rank activations
+// Where expand and grad find them: partial sums by sorted position, added in
+// order, or (by_token) one value by token.
+struct LowRank {
+  const float* p;
+  int64_t split_stride;
+  int splits, by_token;
+  __device__ __forceinline__ float get(int64_t row, int r, int col) const {
+    const float* s = p + row * r + col;
+    float v = *s;
+    for (int i = 1; i < splits; ++i) v += s[i * split_stride];
+    return v;
+  }
+};
+
+// ----------------------------------------------------------------- expand
+struct ExpandArgs {
+  Route route;
+  Adapters ad;
+  LowRank v;
+  const __nv_bfloat16* w;   // [n][r][K]
+  const void* base;         // or nullptr
+  void* y;
+  float* v_out;             // or nullptr: [T][r] by token, unscaled
+  int64_t ldbase, ldy;
+  int K, cols_per;          // column tiles of a CTA
+  int y_bf16, w_aligned, y_aligned;
+};
+
+// CTA (tile, column group): 64 tokens x cols_per * 128 columns.  Warp w takes 16
+// tokens and 64 of the 128 columns; the sums leave through shared memory so that
+// a warp reads the base and writes the result in whole rows.
+template <int RP, int kTerms>
+__global__ void __launch_bounds__(kThreads) expand_kernel(const ExpandArgs a) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  constexpr int kV = (RP + 63) / 64 * kHalf;          // bytes of one term of V
+  constexpr int kW = RP * 128;                        // bytes of 64 columns of w
+  constexpr int kStride = kCols + 4;
+  uint8_t* sv = smem;
+  uint8_t* sw = sv + kTerms * kV;
+  float* out = reinterpret_cast<float*>(sw + 2 * kW);  // [64][kStride]
+  grid_dependency_wait();
+  grid_dependents_launch();
+  if (static_cast<int>(blockIdx.x) >= a.route.counts[0]) return;
+  const int4 tile = a.route.tiles[blockIdx.x];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int mi = lane >> 3, lr = lane & 7;
+  const bool none = tile.x < 0;
+  const int rank = none ? 0 : a.ad.rank(tile.x), r = a.ad.r;
+  const __nv_bfloat16* w = a.w + static_cast<int64_t>(none ? 0 : tile.x) * r * a.K;
+  if (!none) {
+    const float factor = a.ad.factor(tile.x);
+    for (int i = tid; i < kTile * RP / 2; i += kThreads) {
+      const int m = i / (RP / 2), col = 2 * (i % (RP / 2));
+      float v[2] = {0.0f, 0.0f};
+      if (m < tile.z) {
+        const int64_t at = a.v.by_token ? a.route.perm[tile.y + m] : tile.y + m;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          if (col + j < rank) v[j] = a.v.get(at, r, col + j);
+        if (a.v_out != nullptr && blockIdx.y == 0) {
+          float* o = a.v_out + static_cast<int64_t>(a.route.perm[tile.y + m]) * r;
+          if (col < r) o[col] = v[0];
+          if (col + 1 < r) o[col + 1] = v[1];
+        }
+      }
+      store_pair<kTerms>(sv, kV, (col >> 6) * kHalf + tile_off(m, (col & 63) >> 3) + 2 * (col & 7),
+                         v[0] * factor, v[1] * factor);
+    }
+  } else if (a.v_out != nullptr && blockIdx.y == 0) {
+    for (int i = tid; i < tile.z * r; i += kThreads)
+      a.v_out[static_cast<int64_t>(a.route.perm[tile.y + i / r]) * r + i % r] = 0.0f;
+  }
+  const uint32_t sv_s = smem_addr(sv), sw_s = smem_addr(sw);
+  const int tg = 16 * (warp & 3), ch = warp >> 2;
+  const int col_beg = blockIdx.y * a.cols_per * kCols;
+  const int col_end = min(a.K, col_beg + a.cols_per * kCols);
+  for (int c0 = col_beg; c0 < col_end; c0 += kCols) {
+    if (!none) {
+      for (int p = tid; p < RP * 16; p += kThreads) {
+        const int wr = p >> 4, pc = p & 15, e = c0 + 8 * pc;
+        uint32_t u[4] = {0u, 0u, 0u, 0u};
+        if (wr < rank && e < a.K) {
+          const __nv_bfloat16* src = w + static_cast<int64_t>(wr) * a.K + e;
+          if (a.w_aligned) {
+            const uint4 v4 = __ldg(reinterpret_cast<const uint4*>(src));
+            u[0] = v4.x; u[1] = v4.y; u[2] = v4.z; u[3] = v4.w;
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (e + j < a.K)
+                u[j / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(src[j])) << (16 * (j % 2));
+          }
+        }
+        *reinterpret_cast<uint4*>(sw + (pc >> 3) * kW + tile_off(wr, pc & 7)) =
+            make_uint4(u[0], u[1], u[2], u[3]);
+      }
+      __syncthreads();
+      float acc[8][4];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < RP / 16; ++ks) {
+        uint32_t af[kTerms][4];
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t)
+          ldsm4(af[t], sv_s + t * kV + (ks >> 2) * kHalf +
+                           tile_off(tg + 8 * (mi & 1) + lr, 2 * (ks & 3) + (mi >> 1)));
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt) {
+          uint32_t bf[4];
+          ldsm4_trans(bf, sw_s + ch * kW + tile_off(16 * ks + 8 * (mi & 1) + lr, 2 * nt + (mi >> 1)));
+#pragma unroll
+          for (int t = 0; t < kTerms; ++t) {
+            mma(acc[2 * nt], af[t], bf[0], bf[1]);
+            mma(acc[2 * nt + 1], af[t], bf[2], bf[3]);
+          }
+        }
+      }
+      const int g = lane >> 2, t2 = 2 * (lane & 3);
+#pragma unroll
+      for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          *reinterpret_cast<float2*>(out + (tg + g + 8 * h) * kStride + 64 * ch + 8 * nt + t2) =
+              make_float2(acc[nt][2 * h], acc[nt][2 * h + 1]);
+    }
+    __syncthreads();
+    // a warp: eight rows, four columns a lane
+    const int e = c0 + 4 * lane;
+    for (int j = 0; j < 8; ++j) {
+      const int m = 8 * warp + j;
+      if (m >= tile.z || e >= a.K) continue;
+      const int64_t token = a.route.perm[tile.y + m];
+      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (!none) v = *reinterpret_cast<const float4*>(out + m * kStride + 4 * lane);
+      if (a.y_aligned) {
+        if (a.y_bf16) {
+          if (a.base != nullptr) {
+            const uint2 b = *reinterpret_cast<const uint2*>(
+                static_cast<const __nv_bfloat16*>(a.base) + token * a.ldbase + e);
+            v.x += __uint_as_float(b.x << 16);
+            v.y += __uint_as_float(b.x & 0xFFFF0000u);
+            v.z += __uint_as_float(b.y << 16);
+            v.w += __uint_as_float(b.y & 0xFFFF0000u);
+          }
+          *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.y) + token * a.ldy + e) =
+              make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+        } else {
+          if (a.base != nullptr) {
+            const float4 b = *reinterpret_cast<const float4*>(
+                static_cast<const float*>(a.base) + token * a.ldbase + e);
+            v.x += b.x;
+            v.y += b.y;
+            v.z += b.z;
+            v.w += b.w;
+          }
+          *reinterpret_cast<float4*>(static_cast<float*>(a.y) + token * a.ldy + e) = v;
+        }
+      } else {
+        const float s[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (e + i >= a.K) break;
+          if (a.y_bf16) {
+            const float b = a.base == nullptr
+                                ? 0.0f
+                                : __bfloat162float(static_cast<const __nv_bfloat16*>(
+                                      a.base)[token * a.ldbase + e + i]);
+            static_cast<__nv_bfloat16*>(a.y)[token * a.ldy + e + i] = __float2bfloat16_rn(s[i] + b);
+          } else {
+            const float b = a.base == nullptr
+                                ? 0.0f
+                                : static_cast<const float*>(a.base)[token * a.ldbase + e + i];
+            static_cast<float*>(a.y)[token * a.ldy + e + i] = s[i] + b;
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------- grad
+struct GradArgs {
+  Route route;
+  Adapters ad;
+  LowRank u;
+  const void* x;
+  float* part;    // [items][r][K]
+  float* out;     // [n][r][K]
+  int64_t ldx;
+  int K, x_aligned;
+};
+
+// CTA (item, 128 columns): the ranks x 128 columns of scale_i sum_t u_t x_t^T
+// over the item's tokens, in steps of 64.  Both operands come token by token and
+// are transposed by ldmatrix.  Warp w takes 16 columns.
+template <typename T, int RP>
+__global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  constexpr int kTerms = kTermsOf<T>;
+  constexpr int kU = (RP + 63) / 64 * kHalf;    // bytes of one term of u
+  uint8_t* su = smem;                           // three terms
+  uint8_t* sx = smem + 3 * kU;                  // [terms][2 halves]
+  grid_dependency_wait();
+  grid_dependents_launch();
+  if (static_cast<int>(blockIdx.x) >= a.route.counts[1]) return;
+  const int4 item = a.route.items[blockIdx.x];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int mi = lane >> 3, lr = lane & 7, r = a.ad.r;
+  const int rank = a.ad.rank(item.x);
+  const float factor = a.ad.factor(item.x);
+  const int c0 = blockIdx.y * kCols;
+  const int row = tid >> 2, q = tid & 3;
+  Piece<T> px[2];
+  const auto load = [&](int t0) {
+    const T* p = nullptr;
+    if (t0 + row < item.z)
+      p = static_cast<const T*>(a.x) + a.route.perm[item.y + t0 + row] * a.ldx;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load_piece(px[h], p, c0 + 64 * h + 16 * q, a.K, a.x_aligned);
+  };
+  float acc[RP / 16][2][4];
+#pragma unroll
+  for (int i = 0; i < RP / 16; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.0f;
+  const uint32_t su_s = smem_addr(su), sx_s = smem_addr(sx);
+  load(0);
+  for (int t0 = 0; t0 < item.z; t0 += kTile) {
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) store_piece(sx + h * kHalf, 2 * kHalf, row, 2 * q, px[h]);
+    for (int i = tid; i < kTile * RP / 2; i += kThreads) {
+      const int m = i / (RP / 2), col = 2 * (i % (RP / 2));
+      float v[2] = {0.0f, 0.0f};
+      if (t0 + m < item.z) {
+        const int64_t at = a.u.by_token ? a.route.perm[item.y + t0 + m] : item.y + t0 + m;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          if (col + j < rank) v[j] = a.u.get(at, r, col + j) * factor;
+      }
+      store_pair<3>(su, kU, (col >> 6) * kHalf + tile_off(m, (col & 63) >> 3) + 2 * (col & 7), v[0],
+                    v[1]);
+    }
+    __syncthreads();
+    if (t0 + kTile < item.z) load(t0 + kTile);
+#pragma unroll
+    for (int ks = 0; ks < kTile / 16; ++ks) {
+      uint32_t bf[kTerms][4];
+#pragma unroll
+      for (int t = 0; t < kTerms; ++t)
+        ldsm4_trans(bf[t], sx_s + (2 * t + (warp >> 2)) * kHalf +
+                               tile_off(16 * ks + 8 * (mi & 1) + lr, 2 * (warp & 3) + (mi >> 1)));
+#pragma unroll
+      for (int mt = 0; mt < RP / 16; ++mt)
+#pragma unroll
+        for (int tu = 0; tu < 3; ++tu) {
+          uint32_t af[4];
+          ldsm4_trans(af, su_s + tu * kU + (mt >> 2) * kHalf +
+                              tile_off(16 * ks + 8 * (mi >> 1) + lr, 2 * (mt & 3) + (mi & 1)));
+#pragma unroll
+          for (int t = 0; t < kTerms; ++t)
+            if (tu + t <= 2) {   // what is left out is below 2^-24 of the product
+              mma(acc[mt][0], af, bf[t][0], bf[t][1]);
+              mma(acc[mt][1], af, bf[t][2], bf[t][3]);
+            }
+        }
+    }
+  }
+  const bool alone = a.route.item_begin[item.x + 1] - a.route.item_begin[item.x] == 1;
+  float* out = alone ? a.out + static_cast<int64_t>(item.x) * r * a.K
+                     : a.part + static_cast<int64_t>(blockIdx.x) * r * a.K;
+  const int g = lane >> 2, t2 = 2 * (lane & 3);
+#pragma unroll
+  for (int mt = 0; mt < RP / 16; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int m = 16 * mt + g + 8 * (i >> 1), e = c0 + 16 * warp + 8 * nt + t2 + (i & 1);
+        // rows past the adapter's rank are zero whatever x holds
+        if (m < r && e < a.K) out[static_cast<int64_t>(m) * a.K + e] = m < rank ? acc[mt][nt][i] : 0.0f;
+      }
+}
+
+// Adapters of several items: their sums in order; of none: zeros.
+__global__ void __launch_bounds__(256) grad_reduce_kernel(Route route, const float* part,
+                                                          float* out, int64_t size) {
+  grid_dependency_wait();
+  grid_dependents_launch();
+  const int beg = route.item_begin[blockIdx.y], end = route.item_begin[blockIdx.y + 1];
+  if (end - beg == 1) return;
+  const int64_t i = blockIdx.x * 256ll + threadIdx.x;
+  if (i >= size) return;
+  float s = 0.0f;
+  for (int k = beg; k < end; ++k) s += part[k * size + i];
+  out[blockIdx.y * size + i] = s;
+}
+
+// -------------------------------------------------------------- host side
+size_t up(size_t n) { return (n + 255) / 256 * 256; }
+
+// Everything that a call cuts its work into, from its sizes alone.
+struct Plan {
+  int max_tiles, max_items, tokens_per_item;
+  int splits_in, per_in, splits_out, per_out;   // shrink over K_in, over K_out
+  size_t counts, perm, tiles, items, begin, v, du, part, total;
+};
+
+void cut(int64_t K, int tiles, int most, int* splits, int* per) {
+  const int chunks = static_cast<int>((K + kChunk - 1) / kChunk);
+  int want = (2 * device_sm_count() + tiles - 1) / tiles;
+  if (want > most) want = most;
+  if (want > chunks) want = chunks;
+  if (want < 1) want = 1;
+  *per = (chunks + want - 1) / want;
+  *splits = (chunks + *per - 1) / *per;
+}
+
+Plan make_plan(int64_t T, int64_t n, int64_t r, int64_t K_in, int64_t K_out, bool backward) {
+  Plan p{};
+  const int64_t used = n < T ? n : T;
+  p.max_tiles = static_cast<int>((T + kTile - 1) / kTile + used + 1);
+  const int most = T <= 64 ? 32 : 8;
+  cut(K_in, p.max_tiles, most, &p.splits_in, &p.per_in);
+  cut(K_out, p.max_tiles, most, &p.splits_out, &p.per_out);
+  // grad: at least two CTAs an SM over the narrower of the two widths
+  const int64_t K = K_in < K_out ? K_in : K_out;
+  const int64_t want = (2 * device_sm_count() * kCols + K - 1) / K;
+  int64_t per = (T + want - 1) / want;
+  per = (per + kTile - 1) / kTile * kTile;
+  if (per < kTile) per = kTile;
+  p.tokens_per_item = static_cast<int>(per);
+  p.max_items = static_cast<int>((T + per - 1) / per + used);
+  size_t at = 0;
+  const auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += up(bytes);
+    return here;
+  };
+  p.counts = take(64);
+  p.perm = take(sizeof(int) * static_cast<size_t>(T));
+  p.tiles = take(sizeof(int4) * static_cast<size_t>(p.max_tiles));
+  p.items = take(sizeof(int4) * static_cast<size_t>(p.max_items));
+  p.begin = take(sizeof(int) * static_cast<size_t>(n + 1));
+  const size_t row = sizeof(float) * static_cast<size_t>(T) * static_cast<size_t>(r);
+  p.v = take(row * p.splits_in);
+  if (backward) {
+    p.du = take(row * p.splits_out);
+    p.part = take(sizeof(float) * static_cast<size_t>(p.max_items) * static_cast<size_t>(r) *
+                  static_cast<size_t>(K_in > K_out ? K_in : K_out));
+  }
+  p.total = at;
+  return p;
+}
+
+Route route_at(const Plan& p, void* ws) {
+  uint8_t* b = static_cast<uint8_t*>(ws);
+  return {reinterpret_cast<int*>(b + p.counts), reinterpret_cast<int*>(b + p.perm),
+          reinterpret_cast<int4*>(b + p.tiles), reinterpret_cast<int4*>(b + p.items),
+          reinterpret_cast<int*>(b + p.begin)};
+}
+
+cudaError_t allow(const void* kernel, size_t smem) {
+  if (smem <= 48 * 1024) return cudaSuccess;
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              static_cast<int>(smem));
+}
+
+template <typename... P, typename... A>
+cudaError_t go(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s,
+               const A&... args) {
+  const cudaError_t e = allow(reinterpret_cast<const void*>(kernel), smem);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kernel, grid, dim3(threads), smem, s, args...);
+}
+
+// f(std::integral_constant<int, RP>) for the padded rank of r.
+template <typename F>
+cudaError_t by_rank(int64_t r, F f) {
+  if (r <= 16) return f(std::integral_constant<int, 16>{});
+  if (r <= 32) return f(std::integral_constant<int, 32>{});
+  if (r <= 64) return f(std::integral_constant<int, 64>{});
+  return f(std::integral_constant<int, 128>{});
+}
+
+bool rows_aligned(const void* p, int64_t ld, int64_t K, size_t elem, size_t bytes) {
+  return is_aligned(p, bytes) && (ld * elem) % bytes == 0 && (K * elem) % bytes == 0;
+}
+
+cudaError_t run_route(const AdapterProblem& p, const Plan& pl, const Route& r, cudaStream_t s) {
+  const size_t smem = sizeof(int) * (33 * static_cast<size_t>(p.n + 1) + 1);
+  return go(route_kernel, dim3(1), 1024, smem, s, p.ids, static_cast<int>(p.T),
+            static_cast<int>(p.n), pl.tokens_per_item, r);
+}
+
+cudaError_t run_shrink(const AdapterProblem& p, const Plan& pl, const Route& route, const void* x,
+                       tbn_dtype dt, int64_t ldx, const void* w, int64_t K, int splits, int per,
+                       float* part, cudaStream_t s) {
+  const int chunks = static_cast<int>((K + kChunk - 1) / kChunk);
+  ShrinkArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, x,
+               static_cast<const __nv_bfloat16*>(w), part, ldx, static_cast<int>(p.T),
+               static_cast<int>(K), chunks, per, rows_aligned(x, ldx, K, dtype_size(dt), 16),
+               rows_aligned(w, K, K, 2, 16)};
+  const dim3 grid(pl.max_tiles, splits);
+  return by_rank(p.r, [&](auto rp) {
+    constexpr int RP = decltype(rp)::value;
+    const int terms = dt == TBN_BF16 ? 1 : 3;
+    size_t smem = 2 * (terms * static_cast<size_t>(kHalf) + RP * 128);
+    if (smem < sizeof(float) * kTile * RP) smem = sizeof(float) * kTile * RP;
+    if (dt == TBN_BF16) return go(shrink_kernel<__nv_bfloat16, RP>, grid, kThreads, smem, s, a);
+    return go(shrink_kernel<float, RP>, grid, kThreads, smem, s, a);
+  });
+}
+
+cudaError_t run_expand(const AdapterProblem& p, const Plan& pl, const Route& route,
+                       const LowRank& v, const void* w, int64_t K, const void* base,
+                       int64_t ldbase, void* y, tbn_dtype dt, int64_t ldy, float* v_out,
+                       cudaStream_t s) {
+  const size_t e = dtype_size(dt);
+  const int tiles = static_cast<int>((K + kCols - 1) / kCols);
+  int groups = (4 * device_sm_count() + pl.max_tiles - 1) / pl.max_tiles;
+  if (groups > tiles) groups = tiles;
+  const int per = (tiles + groups - 1) / groups;
+  groups = (tiles + per - 1) / per;
+  ExpandArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, v,
+               static_cast<const __nv_bfloat16*>(w), base, y, v_out, ldbase, ldy,
+               static_cast<int>(K), per, dt == TBN_BF16, rows_aligned(w, K, K, 2, 16),
+               rows_aligned(y, ldy, K, e, 4 * e) &&
+                   (base == nullptr || rows_aligned(base, ldbase, K, e, 4 * e))};
+  const dim3 grid(pl.max_tiles, groups);
+  return by_rank(p.r, [&](auto rp) {
+    constexpr int RP = decltype(rp)::value;
+    const int terms = dt == TBN_BF16 ? 2 : 3;
+    const size_t smem = static_cast<size_t>(terms) * ((RP + 63) / 64 * kHalf) + 2 * RP * 128 +
+                        sizeof(float) * kTile * (kCols + 4);
+    if (dt == TBN_BF16) return go(expand_kernel<RP, 2>, grid, kThreads, smem, s, a);
+    return go(expand_kernel<RP, 3>, grid, kThreads, smem, s, a);
+  });
+}
+
+cudaError_t run_grad(const AdapterProblem& p, const Plan& pl, const Route& route, const LowRank& u,
+                     const void* x, tbn_dtype dt, int64_t ldx, int64_t K, float* part, float* out,
+                     cudaStream_t s) {
+  cudaError_t e = cudaSuccess;
+  if (p.T > 0) {
+    GradArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, u, x, part, out, ldx,
+               static_cast<int>(K), rows_aligned(x, ldx, K, dtype_size(dt), 16)};
+    const dim3 grid(pl.max_items, static_cast<unsigned>((K + kCols - 1) / kCols));
+    e = by_rank(p.r, [&](auto rp) {
+      constexpr int RP = decltype(rp)::value;
+      const int terms = dt == TBN_BF16 ? 1 : 3;
+      const size_t smem = 3 * static_cast<size_t>((RP + 63) / 64 * kHalf) + terms * 2 * kHalf;
+      if (dt == TBN_BF16) return go(grad_kernel<__nv_bfloat16, RP>, grid, kThreads, smem, s, a);
+      return go(grad_kernel<float, RP>, grid, kThreads, smem, s, a);
+    });
+  }
+  if (e != cudaSuccess) return e;
+  const int64_t size = p.r * K;
+  return launch_dependent(grad_reduce_kernel,
+                          dim3(static_cast<unsigned>((size + 255) / 256), static_cast<unsigned>(p.n)),
+                          dim3(256), 0, s, route, part, out, size);
+}
+
+}  // namespace
+
+size_t adapter_workspace_bytes(int64_t T, int64_t K_in, int64_t K_out, int64_t n, int64_t r,
+                               bool backward) {
+  return make_plan(T, n, r, K_in, K_out, backward).total;
+}
+
+tbn_status launch_adapter_fwd(const AdapterProblem& p, void* ws, cudaStream_t s) {
+  if (p.T == 0) return TBN_OK;
+  const Plan pl = make_plan(p.T, p.n, p.r, p.K_in, p.K_out, false);
+  const Route route = route_at(pl, ws);
+  float* part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + pl.v);
+  cudaError_t e = run_route(p, pl, route, s);
+  if (e != cudaSuccess) return cuda_fail(e, "adapter route_kernel");
+  e = run_shrink(p, pl, route, p.x, p.xdt, p.ldx, p.a, p.K_in, pl.splits_in, pl.per_in, part, s);
+  if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_kernel");
+  const LowRank v{part, p.T * p.r, pl.splits_in, 0};
+  e = run_expand(p, pl, route, v, p.b, p.K_out, p.base, p.ldbase, p.y, p.ydt, p.ldy, p.v_out, s);
+  return e == cudaSuccess ? TBN_OK : cuda_fail(e, "adapter expand_kernel");
+}
+
+tbn_status launch_adapter_bwd(const AdapterProblem& p, void* ws, cudaStream_t s) {
+  const Plan pl = make_plan(p.T, p.n, p.r, p.K_in, p.K_out, true);
+  const Route route = route_at(pl, ws);
+  uint8_t* b = static_cast<uint8_t*>(ws);
+  float* vpart = reinterpret_cast<float*>(b + pl.v);
+  float* du = reinterpret_cast<float*>(b + pl.du);
+  float* part = reinterpret_cast<float*>(b + pl.part);
+  cudaError_t e = run_route(p, pl, route, s);
+  if (e != cudaSuccess) return cuda_fail(e, "adapter route_kernel");
+  LowRank v{p.v, 0, 1, 1};
+  if (p.T > 0) {
+    if (p.dx != nullptr || p.da != nullptr) {
+      e = run_shrink(p, pl, route, p.dy, p.ydt, p.lddy, p.b, p.K_out, pl.splits_out, pl.per_out, du, s);
+      if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_kernel");
+    }
+    if (p.db != nullptr && p.v == nullptr) {
+      e = run_shrink(p, pl, route, p.x, p.xdt, p.ldx, p.a, p.K_in, pl.splits_in, pl.per_in, vpart, s);
+      if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_kernel");
+      v = {vpart, p.T * p.r, pl.splits_in, 0};
+    }
+  }
+  const LowRank u{du, p.T * p.r, pl.splits_out, 0};
+  if (p.da != nullptr) {
+    e = run_grad(p, pl, route, u, p.x, p.xdt, p.ldx, p.K_in, part, p.da, s);
+    if (e != cudaSuccess) return cuda_fail(e, "adapter grad_kernel");
+  }
+  if (p.db != nullptr) {
+    e = run_grad(p, pl, route, v, p.dy, p.ydt, p.lddy, p.K_out, part, p.db, s);
+    if (e != cudaSuccess) return cuda_fail(e, "adapter grad_kernel");
+  }
+  // last: dx may be written over x or over the base
+  if (p.dx != nullptr && p.T > 0) {
+    e = run_expand(p, pl, route, u, p.a, p.K_in, p.base, p.ldbase, p.dx, p.xdt, p.lddx, nullptr, s);
+    if (e != cudaSuccess) return cuda_fail(e, "adapter expand_kernel");
+  }
+  return TBN_OK;
+}
+
+}  // namespace tbn

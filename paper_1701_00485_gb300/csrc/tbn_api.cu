@@ -841,6 +841,17 @@ extern "C" tbn_status tbn_packed_call(int op, const int64_t* v) {
       return tbn_layernorm_bwd(ptr(0), dt(1), v[2], ptr(3), dt(4), v[5], v[6], v[7], f32(8), f32(9),
                                ptr(10), dt(11), ptr(12), v[13], ptr(14), v[15], f32(16), f32(17),
                                ptr(18), static_cast<size_t>(v[19]), ptr(20));
+    case 7:
+    case 8: {
+      const tbn_adapters ad{ptr(0), ptr(1), v[2], v[3], v[4], v[5], static_cast<int32_t*>(ptr(6)),
+                            static_cast<int32_t*>(ptr(7)), f32(8)};
+      if (op == 7)
+        return tbn_adapter_fwd(&ad, ptr(9), dt(10), v[11], v[12], ptr(13), v[14], ptr(15), dt(16),
+                               v[17], f32(18), ptr(19), static_cast<size_t>(v[20]), ptr(21));
+      return tbn_adapter_bwd(&ad, ptr(9), dt(10), v[11], ptr(12), dt(13), v[14], v[15], f32(16),
+                             ptr(17), v[18], ptr(19), v[20], f32(21), f32(22), ptr(23),
+                             static_cast<size_t>(v[24]), ptr(25));
+    }
   }
   return fail(TBN_ERR_INVALID_ARG, "packed call: unknown operation %d", op);
 }

@@ -25,6 +25,41 @@ tbn_status norm_sizes(const char* what, int64_t rows, int64_t D) {
   return TBN_OK;
 }
 
+const char* adapter_size_reason(int64_t T, int64_t K_in, int64_t K_out, int64_t n, int64_t r) {
+  if (T >= kLim31) return "2^31 tokens or more";
+  if (K_in > (1 << 22) || K_out > (1 << 22)) return "a width above 2^22";
+  if (n > 1023) return "more than 1023 adapters";
+  if (r > 128) return "a rank above 128";
+  return "";
+}
+
+// What both directions check of the adapters and their sizes.
+tbn_status check_adapters(const char* what, const tbn_adapters* ad, int64_t T, bool backward,
+                          const void* workspace, size_t workspace_bytes) {
+  if (!ad) return fail(TBN_ERR_INVALID_ARG, "%s: null pointer", what);
+  if (T < 0 || ad->n < 1 || ad->r < 1 || ad->K_in < 1 || ad->K_out < 1)
+    return fail(TBN_ERR_INVALID_ARG, "%s: needs T >= 0 and other sizes >= 1", what);
+  const char* why = adapter_size_reason(T, ad->K_in, ad->K_out, ad->n, ad->r);
+  if (why[0] != '\0') return fail(TBN_ERR_UNSUPPORTED, "%s: %s", what, why);
+  if (!ad->a || !ad->b) return fail(TBN_ERR_INVALID_ARG, "%s: null pointer", what);
+  if (!is_aligned(ad->a, 2) || !is_aligned(ad->b, 2) || !is_aligned(ad->ids, 4) ||
+      !is_aligned(ad->ranks, 4) || !is_aligned(ad->scale, 4))
+    return fail(TBN_ERR_MISALIGNED, "%s: pointer not aligned to its element size", what);
+  const size_t need = adapter_workspace_bytes(T, ad->K_in, ad->K_out, ad->n, ad->r, backward);
+  if (!workspace || workspace_bytes < need)
+    return fail(TBN_ERR_INVALID_ARG, "%s: workspace of %zu bytes needed", what, need);
+  if (!is_aligned(workspace, 256))
+    return fail(TBN_ERR_MISALIGNED, "%s: workspace must be 256-byte aligned", what);
+  return TBN_OK;
+}
+
+AdapterProblem adapter_problem(const tbn_adapters& ad, int64_t T) {
+  AdapterProblem p{};
+  p.T = T; p.n = ad.n; p.r = ad.r; p.K_in = ad.K_in; p.K_out = ad.K_out;
+  p.a = ad.a; p.b = ad.b; p.ids = ad.ids; p.ranks = ad.ranks; p.scale = ad.scale;
+  return p;
+}
+
 }  // namespace
 
 extern "C" {
@@ -136,6 +171,63 @@ tbn_status tbn_adamw_step(const tbn_adamw_tensor* tensors, int count, const tbn_
       return fail(TBN_ERR_MISALIGNED, "%s: tensor %d is not aligned to its element size", what, i);
   }
   return launch_adamw(tensors, count, h, as_stream(stream));
+}
+
+size_t tbn_adapter_workspace_bytes(int64_t T, int64_t K_in, int64_t K_out, int64_t n, int64_t r,
+                                   int backward) {
+  if (T < 0 || K_in < 1 || K_out < 1 || n < 1 || r < 1 ||
+      adapter_size_reason(T, K_in, K_out, n, r)[0] != '\0')
+    return 0;
+  return adapter_workspace_bytes(T, K_in, K_out, n, r, backward != 0);
+}
+
+tbn_status tbn_adapter_fwd(const tbn_adapters* adapters, const void* x, tbn_dtype xdt, int64_t T,
+                           int64_t ldx, const void* base, int64_t ldbase, void* y, tbn_dtype ydt,
+                           int64_t ldy, float* v, void* workspace, size_t workspace_bytes,
+                           tbn_stream stream) {
+  const char* what = "adapter_fwd";
+  if (const tbn_status st = check_adapters(what, adapters, T, false, workspace, workspace_bytes))
+    return st;
+  if (!dtype_ok(xdt) || !dtype_ok(ydt)) return fail(TBN_ERR_INVALID_ARG, "%s: bad dtype", what);
+  if (T == 0) return TBN_OK;
+  if (!x || !y) return fail(TBN_ERR_INVALID_ARG, "%s: null pointer", what);
+  if (ldx < adapters->K_in || ldy < adapters->K_out || (base && ldbase < adapters->K_out))
+    return fail(TBN_ERR_INVALID_ARG, "%s: a row stride is below the row's length", what);
+  if (!span_ok(T, ldx) || !span_ok(T, ldy) || (base && !span_ok(T, ldbase)))
+    return fail(TBN_ERR_UNSUPPORTED, "%s: tensor too large", what);
+  if (!is_aligned(x, dtype_size(xdt)) || !is_aligned(y, dtype_size(ydt)) ||
+      !is_aligned(base, dtype_size(ydt)) || !is_aligned(v, 4))
+    return fail(TBN_ERR_MISALIGNED, "%s: pointer not aligned to its element size", what);
+  AdapterProblem p = adapter_problem(*adapters, T);
+  p.xdt = xdt; p.ydt = ydt; p.x = x; p.ldx = ldx;
+  p.base = base; p.ldbase = ldbase; p.y = y; p.ldy = ldy; p.v_out = v;
+  return launch_adapter_fwd(p, workspace, as_stream(stream));
+}
+
+tbn_status tbn_adapter_bwd(const tbn_adapters* adapters, const void* dy, tbn_dtype ydt,
+                           int64_t lddy, const void* x, tbn_dtype xdt, int64_t T, int64_t ldx,
+                           const float* v, const void* base, int64_t ldbase, void* dx,
+                           int64_t lddx, float* da, float* db, void* workspace,
+                           size_t workspace_bytes, tbn_stream stream) {
+  const char* what = "adapter_bwd";
+  if (const tbn_status st = check_adapters(what, adapters, T, true, workspace, workspace_bytes))
+    return st;
+  if (!dtype_ok(xdt) || !dtype_ok(ydt)) return fail(TBN_ERR_INVALID_ARG, "%s: bad dtype", what);
+  if (T > 0 && (!dy || !x)) return fail(TBN_ERR_INVALID_ARG, "%s: null pointer", what);
+  if (T > 0 && (ldx < adapters->K_in || lddy < adapters->K_out || (dx && lddx < adapters->K_in) ||
+                (base && ldbase < adapters->K_in)))
+    return fail(TBN_ERR_INVALID_ARG, "%s: a row stride is below the row's length", what);
+  if (!span_ok(T, ldx) || !span_ok(T, lddy) || (dx && !span_ok(T, lddx)) ||
+      (base && !span_ok(T, ldbase)))
+    return fail(TBN_ERR_UNSUPPORTED, "%s: tensor too large", what);
+  if (!is_aligned(x, dtype_size(xdt)) || !is_aligned(dy, dtype_size(ydt)) ||
+      !is_aligned(dx, dtype_size(xdt)) || !is_aligned(base, dtype_size(xdt)) || !is_aligned(v, 4) ||
+      !is_aligned(da, 4) || !is_aligned(db, 4))
+    return fail(TBN_ERR_MISALIGNED, "%s: pointer not aligned to its element size", what);
+  AdapterProblem p = adapter_problem(*adapters, T);
+  p.xdt = xdt; p.ydt = ydt; p.x = x; p.ldx = ldx; p.dy = dy; p.lddy = lddy; p.v = v;
+  p.base = base; p.ldbase = ldbase; p.dx = dx; p.lddx = lddx; p.da = da; p.db = db;
+  return launch_adapter_bwd(p, workspace, as_stream(stream));
 }
 
 }  // extern "C"

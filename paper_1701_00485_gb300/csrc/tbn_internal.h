@@ -236,6 +236,24 @@ tbn_status launch_layernorm_fwd(const LayerNormProblem& p, cudaStream_t s);
 size_t layernorm_bwd_workspace_bytes(int64_t rows, int64_t D);
 tbn_status launch_layernorm_bwd(const LayerNormProblem& p, cudaStream_t s);
 
+// Low-rank adapters after validation (tbn_adapter.cu).  xdt is the type of x
+// and dx, ydt that of y and dy; `base` (rows ldbase apart) has the type of what
+// it is added to, y forward and dx backward.
+struct AdapterProblem {
+  int64_t T, n, r, K_in, K_out, ldx, ldbase, ldy, lddy, lddx;
+  tbn_dtype xdt, ydt;
+  const void *a, *b;
+  const int32_t *ids, *ranks;
+  const float *scale, *v;
+  const void *x, *dy, *base;
+  void *y, *dx;
+  float *v_out, *da, *db;
+};
+size_t adapter_workspace_bytes(int64_t T, int64_t K_in, int64_t K_out, int64_t n, int64_t r,
+                               bool backward);
+tbn_status launch_adapter_fwd(const AdapterProblem& p, void* workspace, cudaStream_t s);
+tbn_status launch_adapter_bwd(const AdapterProblem& p, void* workspace, cudaStream_t s);
+
 // AdamW over validated tensors (tbn_adamw.cu).
 tbn_status launch_adamw(const tbn_adamw_tensor* tensors, int count, const tbn_adamw_hyper& h,
                         cudaStream_t s);

@@ -93,3 +93,45 @@ def test_adamw_refusals(L):
     # nothing to do: no tensor, or only empty ones
     assert _adamw(L, count=0) == OK
     assert _adamw(L, n=0, param=None, grad=None, m=None, v=None) == OK
+
+
+def _adapter(L, backward=False, fields=None, **kw):
+    ad = tbn.Adapters(a=1 << 20, b=1 << 21, n=2, r=8, K_in=64, K_out=128)
+    for k, v in (fields or {}).items():
+        setattr(ad, k, v)
+    need = L.tbn_adapter_workspace_bytes(5, 64, 128, 2, 8, 1 if backward else 0)
+    if backward:
+        a = dict(dy=D, ydt=1, lddy=128, x=D, xdt=1, T=5, ldx=64, v=D, base=D, ldbase=64, dx=D, lddx=64,
+                 da=D, db=D, ws=D, nws=need)
+    else:
+        a = dict(x=D, xdt=1, T=5, ldx=64, base=D, ldbase=128, y=D, ydt=1, ldy=128, v=D, ws=D, nws=need)
+    a.update(kw)
+    call = L.tbn_adapter_bwd if backward else L.tbn_adapter_fwd
+    return call(ctypes.byref(ad), *a.values(), None)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_adapter_refusals(L, backward):
+    run = lambda fields=None, **kw: _adapter(L, backward, fields, **kw)  # noqa: E731
+    need = L.tbn_adapter_workspace_bytes(5, 64, 128, 2, 8, 1 if backward else 0)
+    for f in (dict(a=None), dict(b=None), dict(n=0), dict(r=0), dict(K_in=0), dict(K_out=-1)):
+        assert run(f) == INVALID, f
+    for f in (dict(n=1024), dict(r=129), dict(K_in=(1 << 22) + 1), dict(K_out=1 << 40)):
+        assert run(f) == UNSUPPORTED, f
+    assert run(T=1 << 31) == UNSUPPORTED and run(T=-1) == INVALID
+    for f in (dict(a=(1 << 20) + 1), dict(ids=(1 << 20) + 2), dict(ranks=(1 << 20) + 1), dict(scale=(1 << 20) + 2)):
+        assert run(f) == MISALIGNED, f
+    wrong = [dict(x=None), dict(xdt=5), dict(ydt=-1), dict(ldx=63), dict(ldbase=3), dict(ws=None),
+             dict(nws=need - 1)]
+    wrong += [dict(dy=None), dict(lddy=127), dict(lddx=1)] if backward else [dict(y=None), dict(ldy=127)]
+    for kw in wrong:
+        assert run(**kw) == INVALID, kw
+    assert run(ldx=1 << 45) == UNSUPPORTED
+    odd = ctypes.c_void_p((1 << 20) + 1)
+    for kw in (dict(x=odd), dict(base=odd), dict(v=odd), dict(ws=ctypes.c_void_p((1 << 20) + 128))):
+        assert run(**kw) == MISALIGNED, kw
+    assert L.tbn_adapter_workspace_bytes(5, 64, 128, 0, 8, 0) == 0
+    assert L.tbn_adapter_workspace_bytes(-1, 64, 128, 1, 8, 0) == 0
+    assert L.tbn_adapter_workspace_bytes(5, 64, 128, 1, 129, 1) == 0
+    if not backward:
+        assert run(T=0, x=None, y=None) == OK
