@@ -12,6 +12,13 @@
 // statistics and its result, so each tensor is touched once; the variance is
 // the sum of squared distances from the mean (no cancellation), and every sum
 // is held in 32 bits and taken in an order that depends on the sizes alone.
+//
+// Many aligned rows of 17 to 1024 vectors run on teams with rings of rows
+// (below); short rows by groups of lanes; few rows, rows of odd length or
+// alignment and longer ones by a block each.  Measured (GB300, HBM copy 6.8
+// TB/s), 16384 x 4096 bf16: forward 47.8 us (5.6 TB/s), backward with dres 82.9
+// us (6.5 TB/s); before the rings 58 and 113 us, where what the threads had
+// asked for did not cover the time until it came.
 #include <cuda_bf16.h>
 
 #include "tbn_device.cuh"
@@ -20,10 +27,20 @@
 namespace tbn {
 namespace {
 
+// Arithmetic goes by pairs (two fp32 operations in one instruction, each rounded
+// as by itself): with single ones the backward kernel issued 33 instructions an
+// element and was bound by them.
 constexpr int kVec = 8;   // consecutive elements of a thread
+constexpr int kPairs = kVec / 2;
 
-__device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
+__device__ __forceinline__ uint64_t both(float v) {
+  return f32x2(__float_as_uint(v), __float_as_uint(v));
+}
+__device__ __forceinline__ float first(uint64_t v) { return __uint_as_float(static_cast<uint32_t>(v)); }
+__device__ __forceinline__ float second(uint64_t v) {
+  return __uint_as_float(static_cast<uint32_t>(v >> 32));
+}
+
 
 // Element indexes of a row over `threads` threads: thread t's slot (j, k) is
 // its k-th element of vector j where rows are 16-byte aligned, and element
@@ -34,116 +51,173 @@ __device__ __forceinline__ int slot(int j, int k, int t, int threads) {
   return kAligned ? (j * threads + t) * kVec + k : (j * kVec + k) * threads + t;
 }
 
-template <bool kAligned, typename T, int NV>
-__device__ __forceinline__ void load_row(const T* p, int D, int t, int threads,
-                                         float (&v)[NV][kVec]) {
+// A thread's part of a row, held as it comes until it is used, so that the next
+// row's part can be on its way meanwhile in few registers.
+template <typename T, bool kAligned, int NV>
+struct Row {
+  static constexpr int kWords = kAligned ? static_cast<int>(sizeof(T)) * kVec / 4 : kVec;
+  uint32_t w[NV][kWords];
+
+  // Elements past D are zeros.  What streams through is kept out of L1, where
+  // gamma and beta stay.
+  __device__ __forceinline__ void load(const T* p, int D, int t, int threads) {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    if constexpr (kAligned) {
-      const int e = slot<true>(j, 0, t, threads);
-      if (e < D) {
-        if constexpr (sizeof(T) == 2) {
-          const uint4 r = *reinterpret_cast<const uint4*>(p + e);
-          v[j][0] = bf16_lo(r.x); v[j][1] = bf16_hi(r.x);
-          v[j][2] = bf16_lo(r.y); v[j][3] = bf16_hi(r.y);
-          v[j][4] = bf16_lo(r.z); v[j][5] = bf16_hi(r.z);
-          v[j][6] = bf16_lo(r.w); v[j][7] = bf16_hi(r.w);
-        } else {
-          const float4 a = *reinterpret_cast<const float4*>(p + e);
-          const float4 b = *reinterpret_cast<const float4*>(p + e + 4);
-          v[j][0] = a.x; v[j][1] = a.y; v[j][2] = a.z; v[j][3] = a.w;
-          v[j][4] = b.x; v[j][5] = b.y; v[j][6] = b.z; v[j][7] = b.w;
+    for (int j = 0; j < NV; ++j) {
+      if constexpr (kAligned) {
+        const int e = slot<true>(j, 0, t, threads);
+#pragma unroll
+        for (int i = 0; i < kWords; i += 4) {
+          uint4 r = make_uint4(0u, 0u, 0u, 0u);
+          if (e < D) r = load_once(reinterpret_cast<const uint4*>(p + e) + i / 4);
+          w[j][i] = r.x; w[j][i + 1] = r.y; w[j][i + 2] = r.z; w[j][i + 3] = r.w;
         }
       } else {
 #pragma unroll
-        for (int k = 0; k < kVec; ++k) v[j][k] = 0.0f;
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < kVec; ++k) {
-        const int e = slot<false>(j, k, t, threads);
-        v[j][k] = e < D ? static_cast<float>(p[e]) : 0.0f;
+        for (int k = 0; k < kVec; ++k) {
+          const int e = slot<false>(j, k, t, threads);
+          w[j][k] = e < D ? __float_as_uint(static_cast<float>(p[e])) : 0u;
+        }
       }
     }
   }
-}
 
-// gamma or beta (fp32 or bf16, any alignment that its type has), or `none`.
-template <bool kAligned, int NV>
-__device__ __forceinline__ void load_weight(const void* w, bool bf16, float none, int D, int t,
-                                            int threads, float (&v)[NV][kVec]) {
-  if (w == nullptr) {
+  // The same from a row in shared memory.
+  __device__ __forceinline__ void load_shared(const uint8_t* p, int D, int t, int threads) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int k = 0; k < kVec; ++k) v[j][k] = none;
-  } else if (bf16) {
-    load_row<kAligned>(static_cast<const __nv_bfloat16*>(w), D, t, threads, v);
-  } else {
-    load_row<kAligned>(static_cast<const float*>(w), D, t, threads, v);
-  }
-}
-
-template <bool kAligned, int NV>
-__device__ __forceinline__ void store_row(void* out, bool bf16, int64_t at, int D, int t,
-                                          int threads, const float (&v)[NV][kVec]) {
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    if constexpr (kAligned) {
+    for (int j = 0; j < NV; ++j) {
       const int e = slot<true>(j, 0, t, threads);
-      if (e < D) {
-        if (bf16) {
-          *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(out) + at + e) =
-              make_uint4(pack_bf16x2(v[j][0], v[j][1]), pack_bf16x2(v[j][2], v[j][3]),
-                         pack_bf16x2(v[j][4], v[j][5]), pack_bf16x2(v[j][6], v[j][7]));
-        } else {
-          float4* p = reinterpret_cast<float4*>(static_cast<float*>(out) + at + e);
-          p[0] = make_float4(v[j][0], v[j][1], v[j][2], v[j][3]);
-          p[1] = make_float4(v[j][4], v[j][5], v[j][6], v[j][7]);
-        }
-      }
-    } else {
 #pragma unroll
-      for (int k = 0; k < kVec; ++k) {
-        const int e = slot<false>(j, k, t, threads);
-        if (e < D) {
-          if (bf16)
-            static_cast<__nv_bfloat16*>(out)[at + e] = __float2bfloat16_rn(v[j][k]);
-          else
-            static_cast<float*>(out)[at + e] = v[j][k];
-        }
+      for (int i = 0; i < kWords; i += 4) {
+        uint4 r = make_uint4(0u, 0u, 0u, 0u);
+        if (e < D) r = reinterpret_cast<const uint4*>(p + e * sizeof(T))[i / 4];
+        w[j][i] = r.x; w[j][i + 1] = r.y; w[j][i + 2] = r.z; w[j][i + 3] = r.w;
+      }
+    }
+  }
+
+  // Elements 2 i and 2 i + 1 of vector j.
+  __device__ __forceinline__ uint64_t pair(int j, int i) const {
+    if constexpr (kAligned && sizeof(T) == 2)
+      return f32x2(w[j][i] << 16, w[j][i] & 0xFFFF0000u);
+    else
+      return f32x2(w[j][2 * i], w[j][2 * i + 1]);
+  }
+
+  static __device__ __forceinline__ uint4 load_once(const uint4* p) {
+    uint4 r;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+                 : "l"(p));
+    return r;
+  }
+};
+
+// Vector j of gamma or beta (fp32 or bf16), or `none`.
+template <bool kAligned>
+__device__ __forceinline__ void load_weight(const void* w, bool bf16, float none, int D, int j,
+                                            int t, int threads, uint64_t (&v)[kPairs]) {
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) v[i] = both(none);
+  if (w == nullptr) return;
+  if constexpr (kAligned) {
+    const int e = slot<true>(j, 0, t, threads);
+    if (e >= D) return;
+    if (bf16) {
+      const uint4 r = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(w) + e));
+      const uint32_t u[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) v[i] = f32x2(u[i] << 16, u[i] & 0xFFFF0000u);
+    } else {
+      const uint4* f = reinterpret_cast<const uint4*>(static_cast<const float*>(w) + e);
+      const uint4 a = __ldg(f), b = __ldg(f + 1);
+      v[0] = f32x2(a.x, a.y);
+      v[1] = f32x2(a.z, a.w);
+      v[2] = f32x2(b.x, b.y);
+      v[3] = f32x2(b.z, b.w);
+    }
+  } else {
+    const auto at = [&](int k) {
+      const int e = slot<false>(j, k, t, threads);
+      const float f = e >= D ? none
+                      : bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(w)[e])
+                             : static_cast<const float*>(w)[e];
+      return __float_as_uint(f);
+    };
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) v[i] = f32x2(at(2 * i), at(2 * i + 1));
+  }
+}
+
+// Vector j of a result at element `at` of `out`.
+template <bool kAligned>
+__device__ __forceinline__ void store_vec(void* out, bool bf16, int64_t at, int D, int j, int t,
+                                          int threads, const uint64_t (&v)[kPairs]) {
+  if constexpr (kAligned) {
+    const int e = slot<true>(j, 0, t, threads);
+    if (e >= D) return;
+    if (bf16) {
+      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(out) + at + e) =
+          make_uint4(pack_bf16x2(first(v[0]), second(v[0])), pack_bf16x2(first(v[1]), second(v[1])),
+                     pack_bf16x2(first(v[2]), second(v[2])), pack_bf16x2(first(v[3]), second(v[3])));
+    } else {
+      float4* p = reinterpret_cast<float4*>(static_cast<float*>(out) + at + e);
+      p[0] = make_float4(first(v[0]), second(v[0]), first(v[1]), second(v[1]));
+      p[1] = make_float4(first(v[2]), second(v[2]), first(v[3]), second(v[3]));
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
+      const int e = slot<false>(j, k, t, threads);
+      const float f = k % 2 == 0 ? first(v[k / 2]) : second(v[k / 2]);
+      if (e < D) {
+        if (bf16)
+          static_cast<__nv_bfloat16*>(out)[at + e] = __float2bfloat16_rn(f);
+        else
+          static_cast<float*>(out)[at + e] = f;
       }
     }
   }
 }
 
-// Sums of a and b over the lanes of a group of G (a power of two, <= 32).
+// The sums of a and b over the threads of a row: a group of G <= 32 lanes (a
+// power of two), or (G = 0) the block, through `red`, which the next call may
+// use again at once where the caller alternates between two of them.  The upper
+// half of the lanes takes over b and the lower a, so that each later step adds
+// both at once.
 template <int G>
-__device__ __forceinline__ void group_sum(float& a, float& b) {
+__device__ __forceinline__ void row_sum(float& a, float& b, float (*red)[32]) {
+  constexpr int kLanes = G != 0 ? G : 32, kUpper = kLanes / 2;
+  const int lane = threadIdx.x & 31;
+  const bool upper = lane & kUpper;
+  float v = (upper ? b : a) + __shfl_xor_sync(0xffffffffu, upper ? a : b, kUpper);
 #pragma unroll
-  for (int o = G / 2; o > 0; o >>= 1) {
-    a += __shfl_xor_sync(0xffffffffu, a, o);
-    b += __shfl_xor_sync(0xffffffffu, b, o);
+  for (int o = kUpper / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if constexpr (G == 0) {   // up to 16 warps
+    if ((lane & 15) == 0) (*red)[(threadIdx.x >> 5) + lane] = v;
+    __syncthreads();
+    v = (lane & 15) < (blockDim.x >> 5) ? (*red)[lane] : 0.0f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   }
+  a = __shfl_sync(0xffffffffu, v, lane & ~(kLanes - 1));
+  b = __shfl_sync(0xffffffffu, v, (lane & ~(kLanes - 1)) + kUpper);
 }
 
-// The same over a row's threads: a group of G <= 32 lanes, or (G = 0) the
-// block, through `red`, which the next call may use again at once where the
-// caller alternates between two of them.
+// One sum.
 template <int G>
-__device__ __forceinline__ void row_sum(float& a, float& b, float2* red) {
-  if constexpr (G != 0) {
-    group_sum<G>(a, b);
-  } else {
-    group_sum<32>(a, b);
+__device__ __forceinline__ float row_sum1(float a, float (*red)[32]) {
+  constexpr int kLanes = G != 0 ? G : 32;
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+  if constexpr (G == 0) {
     const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-    if (lane == 0) red[threadIdx.x >> 5] = make_float2(a, b);
+    if (lane == 0) (*red)[threadIdx.x >> 5] = a;
     __syncthreads();
-    const float2 v = lane < warps ? red[lane] : make_float2(0.0f, 0.0f);
-    a = v.x;
-    b = v.y;
-    group_sum<32>(a, b);
+    a = lane < warps ? (*red)[lane] : 0.0f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
   }
+  return a;
 }
 
 struct FwdArgs {
@@ -157,79 +231,242 @@ struct FwdArgs {
   int y_bf16, w_bf16;
 };
 
-// A row by G lanes (256 / G rows per block) or, G = 0, by the block.
-template <typename T, bool kAligned, int G, int NV>
-__global__ void __launch_bounds__(G != 0 ? 256 : 1024) layernorm_fwd_kernel(const FwdArgs a) {
-  __shared__ float2 red[2][32];
+// The sum of a row's part, and that of its squared distances from the mean.
+template <typename R, int NV>
+__device__ __forceinline__ float part_sum(const R& x) {
+  uint64_t s = 0u;   // two zeros
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) s = add_f32x2(s, x.pair(j, i));
+  return first(s) + second(s);
+}
+
+template <typename R, bool kAligned, int NV>
+__device__ __forceinline__ float part_squares(const R& x, float mean, int D, int t, int threads) {
+  const uint64_t minus_mean = both(-mean);
+  uint64_t s = 0u;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    if constexpr (kAligned) {   // vectors lie inside the row or past it
+      if (slot<true>(j, 0, t, threads) >= D) continue;
+    }
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      uint64_t d = add_f32x2(x.pair(j, i), minus_mean);
+      if constexpr (!kAligned) {
+        if (slot<false>(j, 2 * i, t, threads) >= D) d = 0u;
+        else if (slot<false>(j, 2 * i + 1, t, threads) >= D) d &= 0xFFFFFFFFull;
+      }
+      s = fma_f32x2(d, d, s);
+    }
+  }
+  return first(s) + second(s);
+}
+
+__device__ __forceinline__ void write_statistics(const FwdArgs& a, float2 st, int64_t row) {
+  if (a.mean != nullptr) a.mean[row] = st.x;
+  if (a.rstd != nullptr) a.rstd[row] = st.y;
+}
+
+// Vector j of the row's result.
+template <typename R, bool kAligned>
+__device__ __forceinline__ void write_vec(const R& x, int j, const FwdArgs& a, float2 st,
+                                          const uint64_t (&g)[kPairs], const uint64_t (&b)[kPairs],
+                                          int64_t row, int t, int threads) {
+  const uint64_t minus_mean = both(-st.x), scale = both(st.y);
+  uint64_t v[kPairs];
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i)
+    v[i] = fma_f32x2(mul_f32x2(add_f32x2(x.pair(j, i), minus_mean), scale), g[i], b[i]);
+  store_vec<kAligned>(a.y, a.y_bf16, row * a.ldy, a.D, j, t, threads, v);
+}
+
+// A row by G lanes (256 / G at a time per block, R times) or, G = 0, by the block.
+template <typename T, bool kAligned, int G, int NV, int R>
+__global__ void __launch_bounds__(G != 0 ? 256 : NV > 2 ? 512 : 1024)
+    layernorm_fwd_kernel(const FwdArgs a) {
+  __shared__ float red[2][32];
+  constexpr int kGroups = G != 0 ? 256 / (G != 0 ? G : 1) : 1;
   const int threads = G != 0 ? G : blockDim.x;
   const int t = G != 0 ? threadIdx.x % (G != 0 ? G : 1) : threadIdx.x;
-  const int64_t row = G != 0 ? blockIdx.x * static_cast<int64_t>(256 / (G != 0 ? G : 1)) +
-                                   threadIdx.x / (G != 0 ? G : 1)
-                             : blockIdx.x;
-  const bool there = G == 0 || row < a.rows;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups * R +
+                      (G != 0 ? threadIdx.x / (G != 0 ? G : 1) : 0);
   grid_dependency_wait();
   grid_dependents_launch();
-  float v[NV][kVec];
-  load_row<kAligned>(static_cast<const T*>(a.x) + (there ? row : 0) * a.ldx, there ? a.D : 0, t,
-                     threads, v);
-  float s = 0.0f, unused = 0.0f;
+  Row<T, kAligned, NV> x[R];
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
+  for (int q = 0; q < R; ++q) {
+    const int64_t at = row + q * kGroups;
+    x[q].load(static_cast<const T*>(a.x) + (at < a.rows ? at : 0) * a.ldx, at < a.rows ? a.D : 0, t,
+              threads);
+  }
+  const float n = static_cast<float>(a.D);
+  float2 st[R];
 #pragma unroll
-    for (int k = 0; k < kVec; ++k) s += v[j][k];
-  row_sum<G>(s, unused, red[0]);
-  const float mean = s / static_cast<float>(a.D);
-  float q = 0.0f;
+  for (int q = 0; q < R; ++q)
+    st[q].x = row_sum1<G>(part_sum<Row<T, kAligned, NV>, NV>(x[q]), &red[0]) / n;
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
+  for (int q = 0; q < R; ++q)
+    st[q].y = 1.0f / sqrtf(row_sum1<G>(part_squares<Row<T, kAligned, NV>, kAligned, NV>(
+                                           x[q], st[q].x, a.D, t, threads), &red[1]) / n + a.eps);
 #pragma unroll
-    for (int k = 0; k < kVec; ++k) {
-      v[j][k] -= mean;
-      if (slot<kAligned>(j, k, t, threads) < a.D) q = fmaf(v[j][k], v[j][k], q);
+  for (int j = 0; j < NV; ++j) {
+    uint64_t g[kPairs], b[kPairs];
+    load_weight<kAligned>(a.gamma, a.w_bf16, 1.0f, a.D, j, t, threads, g);
+    load_weight<kAligned>(a.beta, a.w_bf16, 0.0f, a.D, j, t, threads, b);
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      const int64_t at = row + q * kGroups;
+      if (at >= a.rows) break;
+      if (t == 0 && j == 0) write_statistics(a, st[q], at);
+      write_vec<Row<T, kAligned, NV>, kAligned>(x[q], j, a, st[q], g, b, at, t, threads);
     }
-  row_sum<G>(q, unused, red[1]);
-  const float rstd = 1.0f / sqrtf(q / static_cast<float>(a.D) + a.eps);
-  if (!there) return;
-  if (t == 0) {
-    if (a.mean != nullptr) a.mean[row] = mean;
-    if (a.rstd != nullptr) a.rstd[row] = rstd;
   }
-  float w[NV][kVec];
-  load_weight<kAligned>(a.gamma, a.w_bf16, 1.0f, a.D, t, threads, w);
-#pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int k = 0; k < kVec; ++k) v[j][k] *= rstd * w[j][k];
-  if (a.beta != nullptr) {
-    load_weight<kAligned>(a.beta, a.w_bf16, 0.0f, a.D, t, threads, w);
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int k = 0; k < kVec; ++k) v[j][k] += w[j][k];
+}
+
+// ---- many aligned rows: teams of warps that stay, each with a ring of rows --
+//
+// A team (a warp with kWarp, else the block) takes rows in turn.  Its first lane
+// keeps `stages` rows on their way by bulk copies into the team's ring, so that
+// the bytes in flight do not depend on registers or on what the team waits for.
+constexpr uint64_t kWaitLimitNs = 1000000000ull;
+constexpr int kMaxStages = 8;
+constexpr int kTeamsOfWarps = 8;   // of a block, with kWarp
+
+struct Ring {
+  uint8_t* rows;      // stages x bytes
+  uint64_t* full;     // [stages]
+  volatile int* abort;
+  uint32_t* err;
+  int stages, bytes, st;
+  uint32_t parity;
+  int issued;         // stages filled so far (first lane)
+
+  __device__ __forceinline__ uint8_t* wait() {
+    mbar_wait(&full[st], parity, abort, err, kWaitLimitNs);
+    return rows + st * bytes;
   }
-  store_row<kAligned>(a.y, a.y_bf16, row * a.ldy, a.D, t, threads, v);
+  __device__ __forceinline__ void advance() {
+    if (++st == stages) {
+      st = 0;
+      parity ^= 1u;
+    }
+  }
+  // First lane, after a wait that ran out: what is still being copied must land
+  // before the block may exit.
+  __device__ __forceinline__ void drain() {
+    if (!*abort) return;
+    for (int i = issued > stages ? issued - stages : 0; i < issued; ++i)
+      mbar_wait(&full[i % stages], static_cast<uint32_t>(i / stages) & 1u, nullptr, err, kWaitLimitNs);
+  }
+};
+
+// Sets a team's ring up: its part of the block's shared memory, barriers that
+// one arrival (the copies' announcement) and the copied bytes complete.
+template <bool kWarp>
+__device__ __forceinline__ Ring make_ring(uint8_t* smem, uint64_t (*full)[kMaxStages], int* abort,
+                                          uint32_t* err, int stages, int bytes) {
+  const int team = kWarp ? threadIdx.x >> 5 : 0;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < (kWarp ? kTeamsOfWarps : 1); ++i)
+      for (int j = 0; j < stages; ++j) mbar_init(&full[i][j], 1);
+    *abort = 0;
+    fence_mbar_init();
+  }
+  __syncthreads();
+  return {smem + static_cast<size_t>(team) * stages * bytes, full[team], abort, err, stages, bytes,
+          0, 0u, 0};
+}
+
+struct RingArgs {
+  int stages, bytes;
+  uint32_t* err;
+};
+
+// Two rows a turn: their sums go through one reduction, and gamma and beta stay
+// in registers.
+template <typename T, bool kWarp>
+__global__ void __launch_bounds__(512) layernorm_fwd_ring_kernel(const FwdArgs a, const RingArgs ra) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint64_t full[kWarp ? kTeamsOfWarps : 1][kMaxStages];
+  __shared__ float red[2][32];
+  __shared__ int abort;
+  constexpr int G = kWarp ? 32 : 0, NV = 2;
+  const int threads = kWarp ? 32 : blockDim.x, t = kWarp ? threadIdx.x & 31 : threadIdx.x;
+  Ring ring = make_ring<kWarp>(smem, full, &abort, ra.err, ra.stages, ra.bytes);
+  grid_dependency_wait();
+  grid_dependents_launch();
+  const int teams = kWarp ? gridDim.x * kTeamsOfWarps : gridDim.x;
+  const int rows = static_cast<int>(a.rows), turns = rows / 2 + rows % 2;
+  const int begin = kWarp ? blockIdx.x * kTeamsOfWarps + (threadIdx.x >> 5) : blockIdx.x;
+  const int row_bytes = ra.bytes / 2;
+  const auto fetch = [&](int64_t turn, int st) {
+    ++ring.issued;
+    const bool two = 2 * turn + 1 < rows;
+    const T* src = static_cast<const T*>(a.x) + 2 * turn * a.ldx;
+    uint8_t* dst = ring.rows + st * ra.bytes;
+    mbar_arrive_expect_tx(&ring.full[st], two ? ra.bytes : row_bytes);
+    bulk_load_1d(dst, src, row_bytes, &ring.full[st]);
+    if (two) bulk_load_1d(dst + row_bytes, src + a.ldx, row_bytes, &ring.full[st]);
+  };
+  if (t == 0)
+    for (int i = 0; i < ra.stages; ++i)
+      if (begin + static_cast<int64_t>(i) * teams < turns) fetch(begin + static_cast<int64_t>(i) * teams, i);
+  uint64_t g[NV][kPairs], b[NV][kPairs];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    load_weight<true>(a.gamma, a.w_bf16, 1.0f, a.D, j, t, threads, g[j]);
+    load_weight<true>(a.beta, a.w_bf16, 0.0f, a.D, j, t, threads, b[j]);
+  }
+  const float n = static_cast<float>(a.D);
+  using X = Row<T, true, NV>;
+  for (int64_t turn = begin; turn < turns; turn += teams, ring.advance()) {
+    const bool two = 2 * turn + 1 < rows;
+    const uint8_t* p = ring.wait();
+    X x[2];
+    x[0].load_shared(p, a.D, t, threads);
+    x[1].load_shared(p + row_bytes, two ? a.D : 0, t, threads);
+    float s0 = part_sum<X, NV>(x[0]), s1 = part_sum<X, NV>(x[1]);
+    row_sum<G>(s0, s1, &red[0]);   // every thread holds its part of the rows past this
+    const int64_t next = turn + static_cast<int64_t>(ra.stages) * teams;
+    if (t == 0 && next < turns && !*ring.abort) fetch(next, ring.st);
+    float2 st[2] = {{s0 / n, 0.0f}, {s1 / n, 0.0f}};
+    s0 = part_squares<X, true, NV>(x[0], st[0].x, a.D, t, threads);
+    s1 = part_squares<X, true, NV>(x[1], st[1].x, a.D, t, threads);
+    row_sum<G>(s0, s1, &red[1]);
+    st[0].y = 1.0f / sqrtf(s0 / n + a.eps);
+    st[1].y = 1.0f / sqrtf(s1 / n + a.eps);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      if (q == 1 && !two) break;
+      if (t == 0) write_statistics(a, st[q], 2 * turn + q);
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        write_vec<X, true>(x[q], j, a, st[q], g[j], b[j], 2 * turn + q, t, threads);
+    }
+  }
+  if (t == 0) ring.drain();
 }
 
 // Rows too long for registers: the row is read three times, the second and
 // third time from the caches.
 template <typename T>
 __global__ void __launch_bounds__(1024) layernorm_fwd_long_kernel(const FwdArgs a) {
-  __shared__ float2 red[2][32];
+  __shared__ float red[2][32];
   grid_dependency_wait();
   grid_dependents_launch();
   const int64_t row = blockIdx.x;
   const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-  float s = 0.0f, unused = 0.0f;
+  float s = 0.0f;
   for (int e = threadIdx.x; e < a.D; e += blockDim.x) s += static_cast<float>(x[e]);
-  row_sum<0>(s, unused, red[0]);
-  const float mean = s / static_cast<float>(a.D);
+  const float mean = row_sum1<0>(s, &red[0]) / static_cast<float>(a.D);
   float q = 0.0f;
   for (int e = threadIdx.x; e < a.D; e += blockDim.x) {
     const float d = static_cast<float>(x[e]) - mean;
     q = fmaf(d, d, q);
   }
-  row_sum<0>(q, unused, red[1]);
-  const float rstd = 1.0f / sqrtf(q / static_cast<float>(a.D) + a.eps);
+  const float rstd = 1.0f / sqrtf(row_sum1<0>(q, &red[1]) / static_cast<float>(a.D) + a.eps);
   if (threadIdx.x == 0) {
     if (a.mean != nullptr) a.mean[row] = mean;
     if (a.rstd != nullptr) a.rstd[row] = rstd;
@@ -261,79 +498,106 @@ struct BwdArgs {
 };
 
 // The rows blockIdx.x, blockIdx.x + gridDim.x, ... (times the groups of a
-// block); a thread keeps the sums of its own columns over all of them.
+// block); a thread keeps the sums of its own columns over all of them, and the
+// next row is on its way while this one is reduced.
 template <typename T, typename DY, bool kAligned, int G, int NV>
 __global__ void __launch_bounds__(G != 0 ? 256 : 512) layernorm_bwd_kernel(const BwdArgs a) {
   extern __shared__ float sums[];   // G != 0: [2][D]
-  __shared__ float2 red[2][32];
+  __shared__ float red[2][32];
   constexpr int kGroups = G != 0 ? 256 / (G != 0 ? G : 1) : 1;
   const int threads = G != 0 ? G : blockDim.x;
   const int t = G != 0 ? threadIdx.x % (G != 0 ? G : 1) : threadIdx.x;
   const int group = G != 0 ? threadIdx.x / (G != 0 ? G : 1) : 0;
   grid_dependency_wait();
   grid_dependents_launch();
-  float gamma[NV][kVec], dg[NV][kVec], db[NV][kVec];
-  load_weight<kAligned>(a.gamma, a.w_bf16, 1.0f, a.D, t, threads, gamma);
+  uint64_t gamma[NV][kPairs], dg[NV][kPairs], db[NV][kPairs];
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
+  for (int j = 0; j < NV; ++j) {
+    load_weight<kAligned>(a.gamma, a.w_bf16, 1.0f, a.D, j, t, threads, gamma[j]);
 #pragma unroll
-    for (int k = 0; k < kVec; ++k) dg[j][k] = db[j][k] = 0.0f;
+    for (int i = 0; i < kPairs; ++i) dg[j][i] = db[j][i] = 0u;
+  }
   const float inv_d = 1.0f / static_cast<float>(a.D);
+  // rows fit 31 bits; a block's groups go on together, since they meet in the
+  // block's sums at the end, and what lies past the last row is read as zeros
+  const int rows = static_cast<int>(a.rows), stride = gridDim.x * kGroups;
+  int row = blockIdx.x * kGroups + group;
+  const T* px = static_cast<const T*>(a.x) + row * a.ldx;
+  const T* pres = static_cast<const T*>(a.dres) + row * a.lddres;
+  const DY* pdy = static_cast<const DY*>(a.dy) + row * a.lddy;
+  int64_t out = row * a.lddx;
+  Row<T, kAligned, NV> x, res;
+  Row<DY, kAligned, NV> dy;
+  float mean = 0.0f, rstd = 0.0f;
+  const auto load = [&](int at) {
+    const int n = at < rows ? a.D : 0;
+    x.load(px, n, t, threads);
+    dy.load(pdy, n, t, threads);
+    if (a.dres != nullptr) res.load(pres, n, t, threads);
+    mean = n > 0 ? a.mean[at] : 0.0f;
+    rstd = n > 0 ? a.rstd[at] : 0.0f;
+    px += stride * a.ldx;
+    pdy += stride * a.lddy;
+    pres += stride * a.lddres;
+  };
+  if (row - group < rows) load(row);
   int turn = 0;
-  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * kGroups; r0 < a.rows;
-       r0 += static_cast<int64_t>(gridDim.x) * kGroups, turn ^= 1) {
-    const int64_t row = r0 + group;
-    const bool there = row < a.rows;
-    const int64_t at = there ? row : 0;
-    const int n = there ? a.D : 0;
-    float xh[NV][kVec], dy[NV][kVec];
-    load_row<kAligned>(static_cast<const T*>(a.x) + at * a.ldx, n, t, threads, xh);
-    load_row<kAligned>(static_cast<const DY*>(a.dy) + at * a.lddy, n, t, threads, dy);
-    const float mean = a.mean[at], rstd = a.rstd[at];
-    float s1 = 0.0f, s2 = 0.0f;
+  for (; row - group < rows; row += stride, turn ^= 1) {
+    uint64_t xh[NV][kPairs], w[NV][kPairs], p1 = 0u, p2 = 0u;
+    // past the row's end dy is zero: what stands there takes no part
+    const uint64_t minus_mean = both(-mean), by = both(rstd);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int k = 0; k < kVec; ++k) {
-        // what lies past the row's end takes no part, whatever mean and rstd are
-        const bool in = slot<kAligned>(j, k, t, threads) < n;
-        xh[j][k] = in ? (xh[j][k] - mean) * rstd : 0.0f;
-        dg[j][k] = fmaf(dy[j][k], xh[j][k], dg[j][k]);
-        db[j][k] += dy[j][k];
-        const float w = dy[j][k] * gamma[j][k];
-        s1 += w;
-        s2 = fmaf(w, xh[j][k], s2);
+      for (int i = 0; i < kPairs; ++i) {
+        const uint64_t d = dy.pair(j, i);
+        xh[j][i] = mul_f32x2(add_f32x2(x.pair(j, i), minus_mean), by);
+        dg[j][i] = fma_f32x2(d, xh[j][i], dg[j][i]);
+        db[j][i] = add_f32x2(db[j][i], d);
+        w[j][i] = mul_f32x2(d, gamma[j][i]);
+        p1 = add_f32x2(p1, w[j][i]);
+        p2 = fma_f32x2(w[j][i], xh[j][i], p2);
       }
-    row_sum<G>(s1, s2, red[turn]);
-    s1 *= inv_d;
-    s2 *= inv_d;
+    float s1 = first(p1) + second(p1), s2 = first(p2) + second(p2);
+    Row<T, kAligned, NV> add;
+    if (a.dres != nullptr) add = res;
+    if (row - group + stride < rows) load(row + stride);
+    row_sum<G>(s1, s2, &red[turn]);
+    const uint64_t m1 = both(-s1 * inv_d), m2 = both(-s2 * inv_d);
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
+      uint64_t v[kPairs];
 #pragma unroll
-      for (int k = 0; k < kVec; ++k)
-        xh[j][k] = rstd * (dy[j][k] * gamma[j][k] - s1 - xh[j][k] * s2);
-    if (a.dres != nullptr) {
-      load_row<kAligned>(static_cast<const T*>(a.dres) + at * a.lddres, n, t, threads, dy);
-#pragma unroll
-      for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) xh[j][k] += dy[j][k];
+      for (int i = 0; i < kPairs; ++i) {
+        v[i] = mul_f32x2(by, fma_f32x2(xh[j][i], m2, add_f32x2(w[j][i], m1)));
+        if (a.dres != nullptr) v[i] = add_f32x2(v[i], add.pair(j, i));
+      }
+      if (row < rows) store_vec<kAligned>(a.dx, a.x_bf16, out, a.D, j, t, threads, v);
     }
-    if (there) store_row<kAligned>(a.dx, a.x_bf16, row * a.lddx, a.D, t, threads, xh);
+    out += stride * a.lddx;
   }
   if (a.part == nullptr) return;
   float* part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.D;
+  const auto get = [](const uint64_t (&v)[kPairs], int k) {
+    return k % 2 == 0 ? first(v[k / 2]) : second(v[k / 2]);
+  };
   if constexpr (G == 0) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
+      if (kAligned) {
+        store_vec<true>(part, false, 0, a.D, j, t, threads, dg[j]);
+        store_vec<true>(part, false, a.D, a.D, j, t, threads, db[j]);
+        continue;
+      }
 #pragma unroll
       for (int k = 0; k < kVec; ++k) {
         const int e = slot<kAligned>(j, k, t, threads);
         if (e < a.D) {
-          part[e] = dg[j][k];
-          part[a.D + e] = db[j][k];
+          part[e] = get(dg[j], k);
+          part[a.D + e] = get(db[j], k);
         }
       }
+    }
   } else {
     // the groups of the block one after another
     for (int g = 0; g < kGroups; ++g) {
@@ -344,10 +608,124 @@ __global__ void __launch_bounds__(G != 0 ? 256 : 512) layernorm_bwd_kernel(const
           for (int k = 0; k < kVec; ++k) {
             const int e = slot<kAligned>(j, k, t, threads);
             if (e < a.D) {
-              sums[e] = g == 0 ? dg[j][k] : sums[e] + dg[j][k];
-              sums[a.D + e] = g == 0 ? db[j][k] : sums[a.D + e] + db[j][k];
+              sums[e] = g == 0 ? get(dg[j], k) : sums[e] + get(dg[j], k);
+              sums[a.D + e] = g == 0 ? get(db[j], k) : sums[a.D + e] + get(db[j], k);
             }
           }
+      }
+      __syncthreads();
+    }
+    for (int e = threadIdx.x; e < 2 * a.D; e += blockDim.x) part[e] = sums[e];
+  }
+}
+
+// The same with rings: a stage holds a row of x, of dy and of dres.
+template <typename T, typename DY, bool kWarp, int NV>
+__global__ void __launch_bounds__(512) layernorm_bwd_ring_kernel(const BwdArgs a, const RingArgs ra) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint64_t full[kWarp ? kTeamsOfWarps : 1][kMaxStages];
+  __shared__ float red[2][32];
+  __shared__ int abort;
+  constexpr int G = kWarp ? 32 : 0;
+  const int threads = kWarp ? 32 : blockDim.x, t = kWarp ? threadIdx.x & 31 : threadIdx.x;
+  Ring ring = make_ring<kWarp>(smem, full, &abort, ra.err, ra.stages, ra.bytes);
+  grid_dependency_wait();
+  grid_dependents_launch();
+  uint64_t gamma[NV][kPairs], dg[NV][kPairs], db[NV][kPairs];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    load_weight<true>(a.gamma, a.w_bf16, 1.0f, a.D, j, t, threads, gamma[j]);
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) dg[j][i] = db[j][i] = 0u;
+  }
+  const float inv_d = 1.0f / static_cast<float>(a.D);
+  const int teams = kWarp ? gridDim.x * kTeamsOfWarps : gridDim.x;
+  const int rows = static_cast<int>(a.rows);
+  const int begin = kWarp ? blockIdx.x * kTeamsOfWarps + (threadIdx.x >> 5) : blockIdx.x;
+  const int xb = a.D * static_cast<int>(sizeof(T)), dyb = a.D * static_cast<int>(sizeof(DY));
+  const auto fetch = [&](int64_t row, int st) {
+    ++ring.issued;
+    uint8_t* p = ring.rows + st * ra.bytes;
+    mbar_arrive_expect_tx(&ring.full[st], a.dres != nullptr ? 2 * xb + dyb : xb + dyb);
+    bulk_load_1d(p, static_cast<const T*>(a.x) + row * a.ldx, xb, &ring.full[st]);
+    bulk_load_1d(p + xb, static_cast<const DY*>(a.dy) + row * a.lddy, dyb, &ring.full[st]);
+    if (a.dres != nullptr)
+      bulk_load_1d(p + xb + dyb, static_cast<const T*>(a.dres) + row * a.lddres, xb, &ring.full[st]);
+  };
+  if (t == 0)
+    for (int i = 0; i < ra.stages; ++i)
+      if (begin + static_cast<int64_t>(i) * teams < rows) fetch(begin + static_cast<int64_t>(i) * teams, i);
+  int turn = 0;
+  float mean = begin < rows ? a.mean[begin] : 0.0f, rstd = begin < rows ? a.rstd[begin] : 0.0f;
+  for (int64_t row = begin; row < rows; row += teams, ring.advance(), turn ^= 1) {
+    const uint8_t* p = ring.wait();
+    uint64_t xh[NV][kPairs], w[NV][kPairs], p1 = 0u, p2 = 0u;
+    const uint64_t minus_mean = both(-mean), by = both(rstd);
+    Row<T, true, NV> x, res;
+    Row<DY, true, NV> dy;
+    x.load_shared(p, a.D, t, threads);
+    dy.load_shared(p + xb, a.D, t, threads);
+    if (a.dres != nullptr) res.load_shared(p + xb + dyb, a.D, t, threads);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        const uint64_t d = dy.pair(j, i);
+        xh[j][i] = mul_f32x2(add_f32x2(x.pair(j, i), minus_mean), by);
+        dg[j][i] = fma_f32x2(d, xh[j][i], dg[j][i]);
+        db[j][i] = add_f32x2(db[j][i], d);
+        w[j][i] = mul_f32x2(d, gamma[j][i]);
+        p1 = add_f32x2(p1, w[j][i]);
+        p2 = fma_f32x2(w[j][i], xh[j][i], p2);
+      }
+    float s1 = first(p1) + second(p1), s2 = first(p2) + second(p2);
+    if (row + teams < rows) {
+      mean = a.mean[row + teams];
+      rstd = a.rstd[row + teams];
+    }
+    row_sum<G>(s1, s2, &red[turn]);   // every thread holds its part of the row past this
+    const int64_t next = row + static_cast<int64_t>(ra.stages) * teams;
+    if (t == 0 && next < rows && !*ring.abort) fetch(next, ring.st);
+    const uint64_t m1 = both(-s1 * inv_d), m2 = both(-s2 * inv_d);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      uint64_t v[kPairs];
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        v[i] = mul_f32x2(by, fma_f32x2(xh[j][i], m2, add_f32x2(w[j][i], m1)));
+        if (a.dres != nullptr) v[i] = add_f32x2(v[i], res.pair(j, i));
+      }
+      store_vec<true>(a.dx, a.x_bf16, row * a.lddx, a.D, j, t, threads, v);
+    }
+  }
+  if (t == 0) ring.drain();
+  if (a.part == nullptr) return;
+  float* part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.D;
+  if constexpr (!kWarp) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      store_vec<true>(part, false, 0, a.D, j, t, threads, dg[j]);
+      store_vec<true>(part, false, a.D, a.D, j, t, threads, db[j]);
+    }
+  } else {
+    // the warps of the block one after another, in what was the rings
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(smem);
+    for (int g = 0; g < kTeamsOfWarps; ++g) {
+      if ((threadIdx.x >> 5) == g) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          const int e = slot<true>(j, 0, t, 32);
+          if (e < a.D) {
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+              uint64_t* sg = reinterpret_cast<uint64_t*>(sums + e + 2 * i);
+              uint64_t* sb = reinterpret_cast<uint64_t*>(sums + a.D + e + 2 * i);
+              *sg = g == 0 ? dg[j][i] : add_f32x2(*sg, dg[j][i]);
+              *sb = g == 0 ? db[j][i] : add_f32x2(*sb, db[j][i]);
+            }
+          }
+        }
       }
       __syncthreads();
     }
@@ -358,8 +736,8 @@ __global__ void __launch_bounds__(G != 0 ? 256 : 512) layernorm_bwd_kernel(const
 // Rows too long for registers: dx of one row per block, and the columns' sums
 // over a slice of the rows in a kernel of their own.
 template <typename T, typename DY>
-__global__ void __launch_bounds__(1024) layernorm_bwd_long_kernel(const BwdArgs a) {
-  __shared__ float2 red[32];
+__global__ void __launch_bounds__(512) layernorm_bwd_long_kernel(const BwdArgs a) {
+  __shared__ float red[1][32];
   grid_dependency_wait();
   grid_dependents_launch();
   const int64_t row = blockIdx.x;
@@ -409,64 +787,150 @@ __global__ void __launch_bounds__(256) layernorm_bwd_columns_kernel(const BwdArg
   part[a.D + e] = db;
 }
 
-// dgamma, dbeta = the partial sums of `slices` blocks, added by eight threads
-// a column (thread row q takes slices q, q + 8, ...) and then in order.
-__global__ void __launch_bounds__(256) layernorm_bwd_reduce_kernel(const float* part, int slices,
-                                                                   int D, float* dgamma,
-                                                                   float* dbeta) {
-  __shared__ float sum[8][33];
+// dgamma, dbeta = the partial sums of `slices` blocks, added by 32 threads a
+// column (thread row q takes slices q, q + 32, ...) and then in order.
+__global__ void __launch_bounds__(1024) layernorm_bwd_reduce_kernel(const float* part, int slices,
+                                                                    int D, float* dgamma,
+                                                                    float* dbeta) {
+  __shared__ float sum[32][33];
   grid_dependency_wait();
   grid_dependents_launch();
   const int c = threadIdx.x & 31, q = threadIdx.x >> 5;
   const int64_t col = static_cast<int64_t>(blockIdx.x) * 32 + c;
   float s = 0.0f;
-  if (col < 2ll * D)
-    for (int i = q; i < slices; i += 8) s += part[2ll * D * i + col];
+  if (col < 2ll * D) {
+#pragma unroll 8
+    for (int i = q; i < slices; i += 32) s += part[2ll * D * i + col];
+  }
   sum[q][c] = s;
   __syncthreads();
   if (q == 0 && col < 2ll * D) {
-    for (int i = 1; i < 8; ++i) s += sum[i][c];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) s += sum[i][c];
     float* out = col < D ? dgamma : dbeta;
     if (out != nullptr) out[col < D ? col : col - D] = s;
   }
 }
 
-// How a row is spread: lanes per row (0: the block), vectors and threads.
+// -------------------------------------------------------------- host side
+// How a row is spread without rings: lanes per row (0: the block), vectors of a
+// lane, threads of the block.
 struct Spread {
   int G, NV, threads;
-  bool fits;
 };
 
-Spread spread(int64_t D, int max_threads, int max_nv, bool wide) {
-  const int64_t u = (D + kVec - 1) / kVec;
-  if (u <= 8) return {8, 1, 256, true};
-  if (u <= 16) return {16, 1, 256, true};
-  if (u <= 32) return {32, 1, 256, true};
-  if (u <= 64 && max_nv >= 2) return {32, 2, 256, true};
-  int nv = wide ? 1 : max_nv;
-  while (nv < max_nv && u > static_cast<int64_t>(nv) * max_threads) nv *= 2;
-  while (nv > 1 && (u + nv - 1) / nv < 64) nv /= 2;
-  const int64_t threads = ((u + nv - 1) / nv + 31) / 32 * 32;
-  return {0, nv, static_cast<int>(threads < max_threads ? threads : max_threads),
-          threads <= max_threads};
+constexpr int64_t kFwdLongest = 512 * 4 * kVec;
+constexpr int64_t kFwdRingLongest = 512 * 2 * kVec;
+constexpr int64_t kBwdLongest = 512 * 2 * kVec;
+// What the rings of an SM's teams take of its shared memory: backward copies
+// three rows a turn, forward one and is no quicker with more (128 KB 47.8 us,
+// 200 KB 48.8 at 16384 x 4096).
+constexpr int kFwdRingBytes = 128 * 1024;
+constexpr int kBwdRingBytes = 200 * 1024;
+
+int block_threads(int64_t vectors, int nv) {
+  return static_cast<int>(((vectors + nv - 1) / nv + 31) / 32 * 32);
 }
 
-constexpr int64_t kFwdLongest = 1024 * 4 * kVec;
-constexpr int64_t kBwdLongest = 512 * 2 * kVec;
+Spread fwd_spread(int64_t D, bool few) {
+  const int64_t u = (D + kVec - 1) / kVec;
+  if (u <= 8) return {8, 1, 256};
+  if (u <= 16) return {16, 1, 256};
+  if (u <= 32) return {32, 1, 256};
+  if (u <= 64) return {32, 2, 256};
+  const int nv = few && u <= 1024 ? 1 : few && u <= 2048 ? 2 : 4;
+  return {0, nv, block_threads(u, nv)};
+}
+
+Spread bwd_spread(int64_t D) {
+  const int64_t u = (D + kVec - 1) / kVec;
+  if (u <= 8) return {8, 1, 256};
+  if (u <= 16) return {16, 1, 256};
+  if (u <= 32) return {32, 1, 256};
+  const int nv = u <= 512 ? 1 : 2;
+  return {0, nv, block_threads(u, nv)};
+}
+
+// How teams with rings are: warps or blocks, their blocks on an SM, the stages
+// that its shared memory holds for each.
+struct Teams {
+  bool warp;
+  int NV, threads, per_sm, stages, bytes;
+};
+
+Teams make_teams(int64_t D, int max_nv, int resident, int bytes, int budget) {
+  const int64_t u = D / kVec;
+  Teams t{};
+  t.bytes = bytes;
+  t.warp = u <= 32 * max_nv;
+  t.threads = t.warp ? 32 * kTeamsOfWarps : static_cast<int>((u + 32 * max_nv - 1) / (32 * max_nv)) * 32;
+  t.NV = static_cast<int>(t.warp ? (u + 31) / 32 : (u + t.threads - 1) / t.threads);
+  t.per_sm = resident / t.threads < 16 ? resident / t.threads : 16;
+  if (t.per_sm < 1) t.per_sm = 1;
+  const auto stages = [&] {
+    return budget / (t.per_sm * (t.warp ? kTeamsOfWarps : 1) * bytes);
+  };
+  while (stages() < 2 && t.per_sm > 1) --t.per_sm;
+  t.stages = stages() < kMaxStages ? stages() : kMaxStages;
+  return t;
+}
+
+// The blocks of a launch that stay and take `rows` in turn, at least four each.
+int staying_blocks(int64_t rows, int64_t teams, int per_sm) {
+  int64_t n = static_cast<int64_t>(device_sm_count()) * per_sm;
+  const int64_t most = (rows + 4 * teams - 1) / (4 * teams);
+  if (n > most) n = most;
+  return static_cast<int>(n < 1 ? 1 : n);
+}
+
+template <typename K, typename A>
+cudaError_t launch_ring(K kernel, const Teams& t, int grid, const A& a, cudaStream_t s) {
+  const size_t smem = static_cast<size_t>(t.stages) * t.bytes * (t.warp ? kTeamsOfWarps : 1);
+  if (smem > 40 * 1024) {   // with the static part, above the 48 KB that need no asking
+    const cudaError_t e = cudaFuncSetAttribute(
+        reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize,
+        static_cast<int>(smem));
+    if (e != cudaSuccess) return e;
+  }
+  const RingArgs r{t.stages, t.bytes, device_error_word()};
+  return launch_dependent(kernel, dim3(grid), dim3(t.threads), smem, s, a, r);
+}
+
+template <typename T>
+cudaError_t launch_fwd_ring(const FwdArgs& a, cudaStream_t s) {
+  const Teams t =
+      make_teams(a.D, 2, 512, 2 * a.D * static_cast<int>(sizeof(T)), kFwdRingBytes);
+  const int grid = staying_blocks(a.rows, t.warp ? kTeamsOfWarps : 1, t.per_sm);
+  return launch_ring(t.warp ? layernorm_fwd_ring_kernel<T, true> : layernorm_fwd_ring_kernel<T, false>,
+                     t, grid, a, s);
+}
+
+template <typename T, typename DY>
+cudaError_t launch_bwd_ring(const BwdArgs& a, const Teams& t, int grid, cudaStream_t s) {
+  if (t.warp && t.NV == 1) return launch_ring(layernorm_bwd_ring_kernel<T, DY, true, 1>, t, grid, a, s);
+  if (t.warp) return launch_ring(layernorm_bwd_ring_kernel<T, DY, true, 2>, t, grid, a, s);
+  return launch_ring(layernorm_bwd_ring_kernel<T, DY, false, 2>, t, grid, a, s);
+}
 
 template <typename T, bool kAligned>
-cudaError_t launch_fwd(const FwdArgs& a, const Spread& sp, cudaStream_t s) {
-  const auto go = [&](auto kernel, int64_t per_block) {
+cudaError_t launch_fwd(const FwdArgs& a, const Spread& sp, bool few, cudaStream_t s) {
+  const auto go = [&](auto kernel, int at_once) {
+    const int64_t per_block = (sp.G != 0 ? 256 / sp.G : 1) * at_once;
     const unsigned grid = static_cast<unsigned>((a.rows + per_block - 1) / per_block);
     return launch_dependent(kernel, dim3(grid), dim3(sp.threads), 0, s, a);
   };
-  if (sp.G == 8) return go(layernorm_fwd_kernel<T, kAligned, 8, 1>, 32);
-  if (sp.G == 16) return go(layernorm_fwd_kernel<T, kAligned, 16, 1>, 16);
-  if (sp.G == 32 && sp.NV == 1) return go(layernorm_fwd_kernel<T, kAligned, 32, 1>, 8);
-  if (sp.G == 32) return go(layernorm_fwd_kernel<T, kAligned, 32, 2>, 8);
-  if (sp.NV == 1) return go(layernorm_fwd_kernel<T, kAligned, 0, 1>, 1);
-  if (sp.NV == 2) return go(layernorm_fwd_kernel<T, kAligned, 0, 2>, 1);
-  return go(layernorm_fwd_kernel<T, kAligned, 0, 4>, 1);
+  if (kAligned && !few) {   // four short rows at once: more of them on their way
+    if (sp.G == 8) return go(layernorm_fwd_kernel<T, kAligned, 8, 1, 4>, 4);
+    if (sp.G == 16) return go(layernorm_fwd_kernel<T, kAligned, 16, 1, 4>, 4);
+    if (sp.G == 32 && sp.NV == 1) return go(layernorm_fwd_kernel<T, kAligned, 32, 1, 4>, 4);
+  }
+  if (sp.G == 8) return go(layernorm_fwd_kernel<T, kAligned, 8, 1, 1>, 1);
+  if (sp.G == 16) return go(layernorm_fwd_kernel<T, kAligned, 16, 1, 1>, 1);
+  if (sp.G == 32 && sp.NV == 1) return go(layernorm_fwd_kernel<T, kAligned, 32, 1, 1>, 1);
+  if (sp.G == 32) return go(layernorm_fwd_kernel<T, kAligned, 32, 2, 1>, 1);
+  if (sp.NV == 1) return go(layernorm_fwd_kernel<T, kAligned, 0, 1, 1>, 1);
+  if (sp.NV == 2) return go(layernorm_fwd_kernel<T, kAligned, 0, 2, 1>, 1);
+  return go(layernorm_fwd_kernel<T, kAligned, 0, 4, 1>, 1);
 }
 
 template <typename T, typename DY, bool kAligned>
@@ -477,22 +941,26 @@ cudaError_t launch_bwd(const BwdArgs& a, const Spread& sp, int grid, cudaStream_
   };
   if (sp.G == 8) return go(layernorm_bwd_kernel<T, DY, kAligned, 8, 1>);
   if (sp.G == 16) return go(layernorm_bwd_kernel<T, DY, kAligned, 16, 1>);
-  if (sp.G == 32 && sp.NV == 1) return go(layernorm_bwd_kernel<T, DY, kAligned, 32, 1>);
-  if (sp.G == 32) return go(layernorm_bwd_kernel<T, DY, kAligned, 32, 2>);
+  if (sp.G == 32) return go(layernorm_bwd_kernel<T, DY, kAligned, 32, 1>);
   if (sp.NV == 1) return go(layernorm_bwd_kernel<T, DY, kAligned, 0, 1>);
   return go(layernorm_bwd_kernel<T, DY, kAligned, 0, 2>);
 }
 
-// Blocks of the backward pass, which each leave one row of partial sums:
-// several resident on every SM, and at least four rows for each of them.
+// Blocks of the backward pass, which each leave one row of partial sums, without
+// rings (512 threads resident on an SM) and with them.
 int bwd_slices(int64_t rows, int64_t D) {
-  const Spread sp = spread(D, 512, 2, false);
-  const int64_t groups = !sp.fits ? 1 : sp.G != 0 ? 256 / sp.G : 1;
-  const int per_sm = !sp.fits ? 4 : 1024 / sp.threads < 8 ? 1024 / sp.threads : 8;
-  int64_t n = static_cast<int64_t>(device_sm_count()) * per_sm;
-  const int64_t most = (rows + 4 * groups - 1) / (4 * groups);
-  if (n > most) n = most;
-  return static_cast<int>(n < 1 ? 1 : n);
+  const bool fits = D <= kBwdLongest;
+  const Spread sp = bwd_spread(D);
+  const int64_t groups = !fits ? 1 : sp.G != 0 ? 256 / sp.G : 1;
+  return staying_blocks(rows, groups, !fits ? 4 : 512 / sp.threads);
+}
+
+int bwd_ring_slices(int64_t rows, const Teams& t) {
+  return staying_blocks(rows, t.warp ? kTeamsOfWarps : 1, t.per_sm);
+}
+
+Teams bwd_teams(int64_t D, size_t row_bytes) {
+  return make_teams(D, 2, 512, static_cast<int>(row_bytes), kBwdRingBytes);
 }
 
 bool aligned_rows(const void* p, int64_t ld, size_t elem) {
@@ -502,7 +970,12 @@ bool aligned_rows(const void* p, int64_t ld, size_t elem) {
 }  // namespace
 
 size_t layernorm_bwd_workspace_bytes(int64_t rows, int64_t D) {
-  return sizeof(float) * 2 * static_cast<size_t>(D) * static_cast<size_t>(bwd_slices(rows, D));
+  int n = bwd_slices(rows, D);
+  if (D <= kBwdLongest) {   // the most blocks that any types' rings leave room for
+    const int ring = bwd_ring_slices(rows, bwd_teams(D, 1));
+    if (ring > n) n = ring;
+  }
+  return sizeof(float) * 2 * static_cast<size_t>(D) * static_cast<size_t>(n);
 }
 
 tbn_status launch_layernorm_fwd(const LayerNormProblem& p, cudaStream_t s) {
@@ -518,18 +991,22 @@ tbn_status launch_layernorm_fwd(const LayerNormProblem& p, cudaStream_t s) {
     const bool al = p.D % kVec == 0 && aligned_rows(p.x, p.ldx, dtype_size(p.xdt)) &&
                     aligned_rows(p.y, p.ldy, dtype_size(p.ydt)) && is_aligned(p.gamma, 16) &&
                     is_aligned(p.beta, 16);
-    const Spread sp = spread(p.D, 1024, 4, p.rows < 2 * device_sm_count());
-    if (p.xdt == TBN_BF16)
-      e = al ? launch_fwd<__nv_bfloat16, true>(a, sp, s) : launch_fwd<__nv_bfloat16, false>(a, sp, s);
+    const bool few = p.rows < 8 * device_sm_count();
+    const Spread sp = fwd_spread(p.D, few);
+    if (al && !few && p.D > 32 * kVec && p.D <= kFwdRingLongest)
+      e = p.xdt == TBN_BF16 ? launch_fwd_ring<__nv_bfloat16>(a, s) : launch_fwd_ring<float>(a, s);
+    else if (p.xdt == TBN_BF16)
+      e = al ? launch_fwd<__nv_bfloat16, true>(a, sp, few, s)
+             : launch_fwd<__nv_bfloat16, false>(a, sp, few, s);
     else
-      e = al ? launch_fwd<float, true>(a, sp, s) : launch_fwd<float, false>(a, sp, s);
+      e = al ? launch_fwd<float, true>(a, sp, few, s) : launch_fwd<float, false>(a, sp, few, s);
   }
   return e == cudaSuccess ? TBN_OK : cuda_fail(e, "layernorm_fwd_kernel");
 }
 
 tbn_status launch_layernorm_bwd(const LayerNormProblem& p, cudaStream_t s) {
   const bool sums = p.dgamma != nullptr || p.dbeta != nullptr;
-  const int slices = bwd_slices(p.rows, p.D);
+  int slices = bwd_slices(p.rows, p.D);
   const bool x16 = p.xdt == TBN_BF16, dy16 = p.ydt == TBN_BF16;
   BwdArgs a{p.x, p.dy, p.dres, p.dx, p.gamma, p.mean, p.rstd, sums ? p.part : nullptr, p.rows,
             p.ldx, p.ldy, p.lddres, p.lddx, static_cast<int>(p.D), x16, p.wdt == TBN_BF16};
@@ -546,15 +1023,21 @@ tbn_status launch_layernorm_bwd(const LayerNormProblem& p, cudaStream_t s) {
       e = launch_dependent(columns, dim3(slices, static_cast<unsigned>((p.D + 255) / 256)), dim3(256),
                            0, s, a, (p.rows + slices - 1) / slices);
     if (e == cudaSuccess && p.rows > 0)
-      e = launch_dependent(rows, dim3(static_cast<unsigned>(p.rows)), dim3(1024), 0, s, a);
+      e = launch_dependent(rows, dim3(static_cast<unsigned>(p.rows)), dim3(512), 0, s, a);
   } else {
     const bool al = p.D % kVec == 0 && aligned_rows(p.x, p.ldx, dtype_size(p.xdt)) &&
                     aligned_rows(p.dy, p.ldy, dtype_size(p.ydt)) &&
                     aligned_rows(p.dx, p.lddx, dtype_size(p.xdt)) &&
                     (p.dres == nullptr || aligned_rows(p.dres, p.lddres, dtype_size(p.xdt))) &&
                     is_aligned(p.gamma, 16);
-    const Spread sp = spread(p.D, 512, 2, false);
-    if (x16)
+    const Spread sp = bwd_spread(p.D);
+    const Teams teams = bwd_teams(p.D, p.D * (dtype_size(p.xdt) * (p.dres ? 2 : 1) + dtype_size(p.ydt)));
+    if (al && p.rows >= 8 * device_sm_count() && p.D > 16 * kVec) {
+      slices = bwd_ring_slices(p.rows, teams);
+      e = x16    ? launch_bwd_ring<B, B>(a, teams, slices, s)
+          : dy16 ? launch_bwd_ring<float, B>(a, teams, slices, s)
+                 : launch_bwd_ring<float, float>(a, teams, slices, s);
+    } else if (x16)
       e = al ? launch_bwd<B, B, true>(a, sp, slices, s) : launch_bwd<B, B, false>(a, sp, slices, s);
     else if (dy16)
       e = al ? launch_bwd<float, B, true>(a, sp, slices, s)
@@ -566,7 +1049,7 @@ tbn_status launch_layernorm_bwd(const LayerNormProblem& p, cudaStream_t s) {
   if (e != cudaSuccess) return cuda_fail(e, "layernorm_bwd_kernel");
   if (!sums) return TBN_OK;
   e = launch_dependent(layernorm_bwd_reduce_kernel, dim3(static_cast<unsigned>((2 * p.D + 31) / 32)),
-                       dim3(256), 0, s, a.part, slices, static_cast<int>(p.D), p.dgamma, p.dbeta);
+                       dim3(1024), 0, s, a.part, slices, static_cast<int>(p.D), p.dgamma, p.dbeta);
   return e == cudaSuccess ? TBN_OK : cuda_fail(e, "layernorm_bwd_reduce_kernel");
 }
 

@@ -96,6 +96,33 @@ def test_forward_and_backward(rows, D, xdt, ydt, pad, offset):
     assert tbn.tbn_device_error() == 0
 
 
+# many rows: teams with rings, an odd number of rows, strides, short rows four at once
+@pytest.mark.parametrize("rows,D", [(1301, 264), (5001, 512), (1301, 520), (2600, 1000), (1219, 2056),
+                                    (1300, 4096), (1217, 8192), (1217, 8200), (9001, 64), (5003, 72),
+                                    (2447, 136), (2441, 256)])
+@pytest.mark.parametrize("xdt,ydt", [(BF16, BF16), (F32, F32), (F32, BF16)])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (24, 16)])
+def test_many_rows(rows, D, xdt, ydt, pad, offset):
+    test_forward_and_backward(rows, D, xdt, ydt, pad, offset)
+
+
+def test_many_rows_in_place_and_equal_bits():
+    rows, D = 4001, 1024
+    x, dy = _inputs(rows, D, BF16, 21), _inputs(rows, D, BF16, 22)
+    gamma = 1 + 0.2 * torch.randn(D, device="cuda")
+    y, mean, rstd = tbn.tbn_layernorm_fwd(x, gamma)
+    z = x.clone()
+    assert torch.equal(tbn.tbn_layernorm_fwd(z, gamma, out=z)[0], y)
+    first = tbn.tbn_layernorm_bwd(dy, x, mean, rstd, gamma, dres=x)
+    again = tbn.tbn_layernorm_bwd(dy, x, mean, rstd, gamma, dres=x)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    for name in ("dy", "dres"):
+        t = {"dy": dy.clone(), "dres": x.clone()}
+        got = tbn.tbn_layernorm_bwd(t["dy"], x, mean, rstd, gamma, dres=t["dres"], dx=t[name])
+        assert all(torch.equal(a, b) for a, b in zip(first, got))
+    assert tbn.tbn_device_error() == 0
+
+
 @pytest.mark.parametrize("gamma,beta", [(False, False), (True, False), (False, True)])
 @pytest.mark.parametrize("wdt", [F32, BF16])
 def test_optional_weights_of_either_type(gamma, beta, wdt):
