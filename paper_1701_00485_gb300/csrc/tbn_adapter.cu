@@ -172,7 +172,7 @@ struct Route {
 // the counts are summed over adapters and warps, and the warp goes through its
 // run once more to place the tokens: the order within an adapter is kept.
 __global__ void __launch_bounds__(1024) route_kernel(const int32_t* ids, int T, int n,
-                                                     int tokens_per_item, Route r) {
+                                                     int tile, int tokens_per_item, Route r) {
   extern __shared__ int sh[];          // counts [32][n + 1], then starts [n + 2]
   __shared__ int warp_sum[32][2], total[2];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(1024) route_kernel(const int32_t* ids, int T, 
       tokens += c;
     }
   }
-  const int tiles = (tokens + kTile - 1) / kTile;
+  const int tiles = (tokens + tile - 1) / tile;
   const int items = tid < n ? (tokens + tokens_per_item - 1) / tokens_per_item : 0;
   const auto exclusive = [&](int v, int* sum_all) {
     int s = v;
@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(1024) route_kernel(const int32_t* ids, int T, 
     const int adapter = tid < n ? tid : -1;
     for (int i = 0; i < tiles; ++i)
       r.tiles[first_tile + i] =
-          make_int4(adapter, first + i * kTile, min(kTile, tokens - i * kTile), 0);
+          make_int4(adapter, first + i * tile, min(tile, tokens - i * tile), 0);
     for (int i = 0; i < items; ++i)
       r.items[first_item + i] = make_int4(adapter, first + i * tokens_per_item,
                                           min(tokens_per_item, tokens - i * tokens_per_item), 0);
@@ -580,15 +580,21 @@ __global__ void __launch_bounds__(kThreads) expand_kernel(const ExpandArgs a) {
 }
 
 // ------------------------------------------------------------------- grad
-struct GradArgs {
-  Route route;
-  Adapters ad;
+// One of the two gradients.
+struct GradSide {
   LowRank u;
+  const __nv_bfloat16* terms;   // tensor-core kernel: [T][3 RP] by sorted position
   const void* x;
   float* part;    // [items][r][K]
   float* out;     // [n][r][K]
   int64_t ldx;
   int K, x_aligned;
+};
+
+struct GradArgs {
+  Route route;
+  Adapters ad;
+  GradSide side;
 };
 
 // CTA (item, 128 columns): the ranks x 128 columns of scale_i sum_t u_t x_t^T
@@ -615,9 +621,9 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
   const auto load = [&](int t0) {
     const T* p = nullptr;
     if (t0 + row < item.z)
-      p = static_cast<const T*>(a.x) + a.route.perm[item.y + t0 + row] * a.ldx;
+      p = static_cast<const T*>(a.side.x) + a.route.perm[item.y + t0 + row] * a.side.ldx;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) load_piece(px[h], p, c0 + 64 * h + 16 * q, a.K, a.x_aligned);
+    for (int h = 0; h < 2; ++h) load_piece(px[h], p, c0 + 64 * h + 16 * q, a.side.K, a.side.x_aligned);
   };
   float acc[RP / 16][2][4];
 #pragma unroll
@@ -636,10 +642,10 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
       const int m = i / (RP / 2), col = 2 * (i % (RP / 2));
       float v[2] = {0.0f, 0.0f};
       if (t0 + m < item.z) {
-        const int64_t at = a.u.by_token ? a.route.perm[item.y + t0 + m] : item.y + t0 + m;
+        const int64_t at = a.side.u.by_token ? a.route.perm[item.y + t0 + m] : item.y + t0 + m;
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-          if (col + j < rank) v[j] = a.u.get(at, r, col + j) * factor;
+          if (col + j < rank) v[j] = a.side.u.get(at, r, col + j) * factor;
       }
       store_pair<3>(su, kU, (col >> 6) * kHalf + tile_off(m, (col & 63) >> 3) + 2 * (col & 7), v[0],
                     v[1]);
@@ -670,8 +676,8 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
     }
   }
   const bool alone = a.route.item_begin[item.x + 1] - a.route.item_begin[item.x] == 1;
-  float* out = alone ? a.out + static_cast<int64_t>(item.x) * r * a.K
-                     : a.part + static_cast<int64_t>(blockIdx.x) * r * a.K;
+  float* out = alone ? a.side.out + static_cast<int64_t>(item.x) * r * a.side.K
+                     : a.side.part + static_cast<int64_t>(blockIdx.x) * r * a.side.K;
   const int g = lane >> 2, t2 = 2 * (lane & 3);
 #pragma unroll
   for (int mt = 0; mt < RP / 16; ++mt)
@@ -681,7 +687,7 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
       for (int i = 0; i < 4; ++i) {
         const int m = 16 * mt + g + 8 * (i >> 1), e = c0 + 16 * warp + 8 * nt + t2 + (i & 1);
         // rows past the adapter's rank are zero whatever x holds
-        if (m < r && e < a.K) out[static_cast<int64_t>(m) * a.K + e] = m < rank ? acc[mt][nt][i] : 0.0f;
+        if (m < r && e < a.side.K) out[static_cast<int64_t>(m) * a.side.K + e] = m < rank ? acc[mt][nt][i] : 0.0f;
       }
 }
 
@@ -699,14 +705,515 @@ __global__ void __launch_bounds__(256) grad_reduce_kernel(Route route, const flo
   out[blockIdx.y * size + i] = s;
 }
 
+// ==================================================================== tcgen05
+// The same three products for bf16 activations in aligned rows, on tiles of 128
+// tokens: operands come by cp.async into a ring (zero-filled where there is no
+// token, no rank or no column), one thread issues the MMAs, sums stay in tensor
+// memory.  The low-rank activations between two products are written once as
+// bf16 terms (terms_kernel), a row's terms side by side.
+constexpr int kTcTile = 128;
+constexpr int64_t kTcFrom = 128;   // tokens
+constexpr uint64_t kWaitLimitNs = 1000000000ull;
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
+               "r"(valid ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// Matrix descriptor of an operand whose rows are steps of the contraction and
+// whose 64-wide column blocks (128-byte swizzled rows) lie `block` bytes apart.
+__device__ __forceinline__ uint64_t desc_mn(uint32_t saddr, uint32_t block) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(block >> 4) << 16;   // next 64 columns
+  d |= static_cast<uint64_t>(1024u >> 4) << 32;   // next 8 steps
+  d |= static_cast<uint64_t>(1u) << 46;
+  d |= static_cast<uint64_t>(2u) << 61;           // 128-byte swizzle
+  return d;
+}
+
+// What each tensor-core kernel begins and ends with: its tensor memory (kCols
+// columns) and `bars` barriers that one arrival completes.
+template <int kTmemCols>
+__device__ __forceinline__ uint32_t tc_begin(uint32_t* slot, uint64_t* bar, int bars) {
+  if (threadIdx.x < 32) {
+    tmem_alloc(slot, kTmemCols);
+    tmem_relinquish();
+  }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < bars; ++i) mbar_init(&bar[i], 1);
+    fence_mbar_init();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  return *slot;
+}
+
+template <int kTmemCols>
+__device__ __forceinline__ void tc_end(uint32_t tmem) {
+  tc_fence_before_sync();
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+__device__ __forceinline__ uint8_t* align_1k(uint8_t* p) {
+  return p + ((1024u - (smem_addr(p) & 1023u)) & 1023u);
+}
+
+// ---- shrink: D[128 tokens][RP] over a range of K, both operands K-major
+constexpr int kShrinkStages = 4;
+template <int RP>
+constexpr int kShrinkStage = kTcTile * 128 + RP * 128;
+
+template <int RP>
+__global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const ShrinkArgs a, uint32_t* err) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t bar[kShrinkStages];
+  __shared__ uint32_t slot;
+  constexpr int kTmem = RP < 32 ? 32 : RP, S = kShrinkStages;
+  constexpr int kWPieces = (RP * 8 + kThreads - 1) / kThreads;
+  grid_dependency_wait();
+  grid_dependents_launch();
+  if (static_cast<int>(blockIdx.x) >= a.route.counts[0]) return;
+  const int4 tile = a.route.tiles[blockIdx.x];
+  if (tile.x < 0) return;
+  const uint32_t tmem = tc_begin<kTmem>(&slot, bar, S);
+  const uint32_t ring = smem_addr(align_1k(smem_raw));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, ch = tid & 7;
+  const int rank = a.ad.rank(tile.x);
+  const int c0 = blockIdx.y * a.chunks_per, n = min(a.chunks, c0 + a.chunks_per) - c0;
+  const __nv_bfloat16* xr[4];
+  uint32_t there = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = (tid >> 3) + 32 * i;
+    const bool v = row < tile.z;
+    xr[i] = static_cast<const __nv_bfloat16*>(a.x) +
+            (v ? a.route.perm[tile.y + row] * a.ldx : 0);
+    there |= static_cast<uint32_t>(v) << i;
+  }
+  const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * a.ad.r * a.K;
+  const auto issue = [&](int ci) {
+    const uint32_t st = ring + (ci % S) * kShrinkStage<RP>;
+    const int e = (c0 + ci) * kChunk + 8 * ch;
+    const bool in = e < a.K;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool v = in && ((there >> i) & 1u);
+      cp_async16(st + tile_off((tid >> 3) + 32 * i, ch), v ? xr[i] + e : xr[i], v);
+    }
+#pragma unroll
+    for (int i = 0; i < kWPieces; ++i) {
+      const int row = (tid >> 3) + 32 * i;
+      if (RP * 8 >= kThreads || row < RP) {
+        const bool v = in && row < rank;
+        cp_async16(st + kTcTile * 128 + tile_off(row, ch),
+                   v ? w + static_cast<int64_t>(row) * a.K + e : w, v);
+      }
+    }
+  };
+#pragma unroll
+  for (int ci = 0; ci < S - 1; ++ci) {
+    if (ci < n) issue(ci);
+    cp_async_commit();
+  }
+  constexpr uint32_t idesc = idesc_bf16_f32(128, RP);
+  bool ok = true;
+  for (int ci = 0; ci < n; ++ci) {
+    cp_async_wait<S - 2>();
+    fence_proxy_async_smem();   // this thread's copies, to the tensor core
+    __syncthreads();
+    if (tid == 0) {
+      tc_fence_after_sync();
+      const uint32_t st = ring + (ci % S) * kShrinkStage<RP>;
+#pragma unroll
+      for (int ks = 0; ks < kChunk / 16; ++ks)
+        tc_mma_ss(tmem, smem_desc_sw128_kmajor(st + 32 * ks),
+                  smem_desc_sw128_kmajor(st + kTcTile * 128 + 32 * ks), idesc, (ci | ks) != 0);
+      tc_commit(&bar[ci % S]);
+    }
+    if (ci + S - 1 < n) {
+      // the stage refilled held chunk ci - 1: its MMAs must have read it
+      if (ci >= 1 && tid == 0)
+        ok = mbar_wait(&bar[(ci - 1) % S], static_cast<uint32_t>((ci - 1) / S) & 1u, nullptr, err,
+                       kWaitLimitNs);
+      if (!__syncthreads_and(ok)) break;
+      issue(ci + S - 1);
+    }
+    cp_async_commit();
+  }
+  cp_async_wait<0>();
+  if (tid == 0)
+    ok = mbar_wait(&bar[(n - 1) % S], static_cast<uint32_t>((n - 1) / S) & 1u, nullptr, err,
+                   kWaitLimitNs) && ok;
+  ok = __syncthreads_and(ok);
+  tc_fence_after_sync();
+  // warp w: tokens 32 (w % 4) .., every other 16 ranks
+  const int row = 32 * (warp & 3) + lane;
+  float* out = a.part + (static_cast<int64_t>(blockIdx.y) * a.T + tile.y + row) * a.ad.r;
+#pragma unroll
+  for (int c = 16 * (warp >> 2); c < RP; c += 32) {
+    uint32_t v[16];
+    tmem_ld_32x32b_x16(tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + c, v);
+    tmem_wait_ld();
+    if (ok && row < tile.z) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (c + i < a.ad.r) out[c + i] = __uint_as_float(v[i]);
+    }
+  }
+  tc_end<kTmem>(tmem);
+}
+
+// ---- the low-rank activations as bf16 terms, by sorted position
+struct TermsArgs {
+  Route route;
+  Adapters ad;
+  LowRank v;
+  __nv_bfloat16* terms;   // [T][kTerms RP]
+  float* v_out;           // or nullptr: [T][r] by token, unscaled
+};
+
+// A tile per block.  Past the rank the terms are zero, whatever v holds there.
+template <int RP, int kTerms>
+__global__ void __launch_bounds__(kThreads) terms_kernel(const TermsArgs a) {
+  grid_dependency_wait();
+  grid_dependents_launch();
+  if (static_cast<int>(blockIdx.x) >= a.route.counts[0]) return;
+  const int4 tile = a.route.tiles[blockIdx.x];
+  const int r = a.ad.r, rank = tile.x < 0 ? 0 : a.ad.rank(tile.x);
+  if (tile.x < 0 && a.v_out == nullptr) return;
+  const float factor = tile.x < 0 ? 0.0f : a.ad.factor(tile.x);
+  for (int i = threadIdx.x + blockIdx.y * kThreads; i < tile.z * RP / 2; i += kThreads * gridDim.y) {
+    const int m = i / (RP / 2), col = 2 * (i % (RP / 2));
+    const int token = a.route.perm[tile.y + m];
+    const int64_t at = a.v.by_token ? token : tile.y + m;
+    float v[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (col + j < rank) v[j] = a.v.get(at, r, col + j);
+    if (a.v_out != nullptr) {
+      float* o = a.v_out + static_cast<int64_t>(token) * r;
+      if (col < r) o[col] = v[0];
+      if (col + 1 < r) o[col + 1] = v[1];
+    }
+    if (tile.x < 0) continue;
+    store_pair<kTerms>(reinterpret_cast<uint8_t*>(a.terms + (tile.y + m) * static_cast<int64_t>(kTerms * RP)),
+                       2 * RP, 2 * col, v[0] * factor, v[1] * factor);
+  }
+}
+
+// ---- expand: D[128 tokens][128 columns] over two terms of RP ranks
+struct ExpandTcArgs {
+  Route route;
+  Adapters ad;
+  const __nv_bfloat16* terms;   // rows of row_terms elements
+  const __nv_bfloat16* w;       // [n][r][K]
+  const __nv_bfloat16* base;    // or nullptr
+  __nv_bfloat16* y;
+  int64_t ldbase, ldy;
+  int row_terms, K, cols_per;
+  int wide;                     // rows of base and y start at multiples of 32 bytes
+  uint32_t* err;
+};
+
+// 64 bytes of a row (32 bf16, of which `left` exist) as four 16-byte words.
+__device__ __forceinline__ void load_64(uint4 (&d)[4], const __nv_bfloat16* p, bool wide, int left) {
+  if (wide && left >= 32) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(d[2 * i].x), "=r"(d[2 * i].y), "=r"(d[2 * i].z), "=r"(d[2 * i].w),
+                     "=r"(d[2 * i + 1].x), "=r"(d[2 * i + 1].y), "=r"(d[2 * i + 1].z),
+                     "=r"(d[2 * i + 1].w)
+                   : "l"(p + 16 * i)
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      d[i] = 8 * i < left ? *reinterpret_cast<const uint4*>(p + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
+__device__ __forceinline__ void store_64(__nv_bfloat16* p, const uint4 (&d)[4], bool wide, int left) {
+  if (wide && left >= 32) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + 16 * i),
+                   "r"(d[2 * i].x), "r"(d[2 * i].y), "r"(d[2 * i].z), "r"(d[2 * i].w),
+                   "r"(d[2 * i + 1].x), "r"(d[2 * i + 1].y), "r"(d[2 * i + 1].z), "r"(d[2 * i + 1].w)
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (8 * i < left) *reinterpret_cast<uint4*>(p + 8 * i) = d[i];
+  }
+}
+
+template <int RP>
+constexpr int kExpandV = (2 * RP + 63) / 64 * kTcTile * 128;
+template <int RP>
+constexpr int kExpandW = 2 * RP * 128;   // of a stage: two blocks of 64 columns
+
+// CTA (tile, column group).  V is the K-major operand, w the other, ranks as
+// steps.  A thread owns a token's row: it reads and writes 64 bytes at a time, so
+// that every 32-byte sector is moved whole without going through shared memory.
+template <int RP>
+__global__ void __launch_bounds__(kThreads, RP == 128 ? 1 : 3) expand_tc_kernel(const ExpandTcArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t bar[1];
+  __shared__ uint32_t slot;
+  grid_dependency_wait();
+  grid_dependents_launch();
+  if (static_cast<int>(blockIdx.x) >= a.route.counts[0]) return;
+  const int4 tile = a.route.tiles[blockIdx.x];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int row = 32 * (warp & 3) + lane, half = 64 * (warp >> 2);
+  const bool there = row < tile.z;
+  const int64_t token = there ? a.route.perm[tile.y + row] : 0;
+  const __nv_bfloat16* base = a.base == nullptr ? nullptr : a.base + token * a.ldbase;
+  __nv_bfloat16* y = a.y + token * a.ldy;
+  const int col_beg = blockIdx.y * a.cols_per * kCols;
+  const int col_end = min(a.K, col_beg + a.cols_per * kCols);
+  if (tile.x < 0) {   // no adapter: the base, or zeros
+    if (!there || base == y) return;
+    for (int c = col_beg + half; c < col_end; c += c % kCols == half + 32 ? kCols - 32 : 32) {
+      uint4 d[4] = {};
+      if (base != nullptr) load_64(d, base + c, a.wide, a.K - c);
+      store_64(y + c, d, a.wide, a.K - c);
+    }
+    return;
+  }
+  const uint32_t tmem = tc_begin<kCols>(&slot, bar, 1);
+  const uint32_t sv = smem_addr(align_1k(smem_raw)), sw = sv + kExpandV<RP>;
+  const int rank = a.ad.rank(tile.x);
+  const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * a.ad.r * a.K;
+  constexpr int kRow = 2 * RP / 8;   // 16-byte pieces of a row of V
+  for (int p = tid; p < kTcTile * kRow; p += kThreads) {
+    const int m = p / kRow, c = p % kRow;
+    const bool v = m < tile.z;
+    cp_async16(sv + (c >> 3) * (kTcTile * 128) + tile_off(m, c & 7),
+               a.terms + static_cast<int64_t>(tile.y + (v ? m : 0)) * a.row_terms + 8 * c, v);
+  }
+  const auto issue = [&](int c0, int st) {
+#pragma unroll
+    for (int i = 0; i < RP * 16 / kThreads; ++i) {
+      const int p = tid + i * kThreads, wr = p >> 4, pc = p & 15, e = c0 + 8 * pc;
+      const bool v = wr < rank && e < a.K;
+      cp_async16(sw + st * kExpandW<RP> + (pc >> 3) * (RP * 128) + tile_off(wr, pc & 7),
+                 v ? w + static_cast<int64_t>(wr) * a.K + e : w, v);
+    }
+    cp_async_commit();
+  };
+  issue(col_beg, 0);
+  constexpr uint32_t idesc = idesc_bf16_f32(128, kCols) | (1u << 16);   // w: columns contiguous
+  int turn = 0;
+  for (int c0 = col_beg; c0 < col_end; c0 += kCols, ++turn) {
+    const int st = turn & 1;
+    cp_async_wait<0>();
+    fence_proxy_async_smem();
+    __syncthreads();   // also: every warp has read the last tile's sums
+    if (tid == 0) {
+      tc_fence_after_sync();
+#pragma unroll
+      for (int k = 0; k < 2 * RP / 16; ++k)   // the leading terms' ranks, then the second terms'
+        tc_mma_ss(tmem,
+                  smem_desc_sw128_kmajor(sv + (k >> 2) * (kTcTile * 128) + 32 * (k & 3)),
+                  desc_mn(sw + st * kExpandW<RP> + (k % (RP / 16)) * 2048, RP * 128), idesc, k != 0);
+      tc_commit(&bar[0]);
+    }
+    if (c0 + kCols < col_end) issue(c0 + kCols, st ^ 1);   // last read by the MMAs waited for
+    const int c = c0 + half;
+    uint4 b[2][4] = {};
+    if (base != nullptr && there) {
+      load_64(b[0], base + c, a.wide, a.K - c);
+      load_64(b[1], base + c + 32, a.wide, a.K - c - 32);
+    }
+    const bool ok = mbar_wait(&bar[0], static_cast<uint32_t>(turn) & 1u, nullptr, a.err, kWaitLimitNs);
+    if (!__syncthreads_and(ok)) break;
+    tc_fence_after_sync();
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      uint32_t v[32];
+      tmem_ld_32x32b_x32(tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + half + 32 * q, v);
+      tmem_wait_ld();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t* u = reinterpret_cast<uint32_t*>(&b[q][i]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          u[j] = pack_bf16x2(__uint_as_float(v[8 * i + 2 * j]) + __uint_as_float(u[j] << 16),
+                             __uint_as_float(v[8 * i + 2 * j + 1]) + __uint_as_float(u[j] & 0xFFFF0000u));
+      }
+      if (there) store_64(y + c + 32 * q, b[q], a.wide, a.K - c - 32 * q);
+    }
+    tc_fence_before_sync();
+  }
+  cp_async_wait<0>();
+  tc_end<kCols>(tmem);
+}
+
+// ---- grad: D[columns of x][3 RP] over an item's tokens, both operands token by
+// token.  The three terms are columns of one MMA and are added at the end, the
+// smaller ones first: each term's sum loses nothing to the leading one's size.
+template <int RP>
+constexpr int kGradCols = RP == 128 ? 128 : 256;
+template <int RP>
+constexpr int kGradU = (3 * RP + 63) / 64 * kHalf;
+template <int RP>
+constexpr int kGradStage = kGradCols<RP> / 64 * kHalf + kGradU<RP>;
+constexpr int kGradStages = 3;
+
+struct GradTcArgs {
+  Route route;
+  Adapters ad;
+  GradSide side[2];
+  int tiles0;       // column tiles of side 0; the launch's others are side 1's
+  uint32_t* err;
+};
+
+template <int RP>
+__global__ void __launch_bounds__(kThreads, 1) grad_tc_kernel(const GradTcArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t bar[kGradStages];
+  __shared__ uint32_t slot;
+  constexpr int S = kGradStages, kCt = kGradCols<RP>, N = 3 * RP;
+  constexpr int kAcc = kCt / 128 * N;
+  constexpr int kTmem = kAcc <= 128 ? 128 : kAcc <= 256 ? 256 : 512;
+  constexpr int kXRows = kThreads / (kCt / 8), kXPasses = 64 / kXRows;   // rows of a pass
+  constexpr int kURow = N / 8;                                           // pieces of a row of u
+  constexpr int kUPasses = (64 * kURow + kThreads - 1) / kThreads;
+  grid_dependency_wait();
+  grid_dependents_launch();
+  if (static_cast<int>(blockIdx.x) >= a.route.counts[1]) return;
+  const int4 item = a.route.items[blockIdx.x];
+  const bool first = static_cast<int>(blockIdx.y) < a.tiles0;
+  const GradSide& sd = a.side[first ? 0 : 1];
+  const int c0 = (first ? blockIdx.y : blockIdx.y - a.tiles0) * kCt;
+  const uint32_t tmem = tc_begin<kTmem>(&slot, bar, S);
+  const uint32_t ring = smem_addr(align_1k(smem_raw));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int n = (item.z + 63) / 64;
+  const int xc = tid % (kCt / 8), xrow = tid / (kCt / 8);
+  const bool col_in = c0 + 8 * xc < sd.K;
+  const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(sd.x) + (col_in ? c0 + 8 * xc : 0);
+  const __nv_bfloat16* terms = sd.terms + static_cast<int64_t>(item.y) * N;
+  int token[kXPasses];   // of the chunk issued next (-1: none)
+  const auto find = [&](int ci) {
+#pragma unroll
+    for (int i = 0; i < kXPasses; ++i) {
+      const int t = 64 * ci + xrow + kXRows * i;
+      token[i] = t < item.z ? a.route.perm[item.y + t] : -1;
+    }
+  };
+  const auto issue = [&](int ci) {
+    const uint32_t st = ring + (ci % S) * kGradStage<RP>;
+#pragma unroll
+    for (int i = 0; i < kXPasses; ++i) {
+      const bool v = col_in && token[i] >= 0;
+      cp_async16(st + (xc >> 3) * kHalf + tile_off(xrow + kXRows * i, xc & 7),
+                 v ? x + token[i] * sd.ldx : x, v);
+    }
+#pragma unroll
+    for (int i = 0; i < kUPasses; ++i) {
+      const int p = tid + i * kThreads, m = p / kURow, c = p % kURow;
+      if (64 * kURow % kThreads == 0 || m < 64) {
+        const int t = 64 * ci + m;
+        const bool v = t < item.z;
+        cp_async16(st + kCt / 64 * kHalf + (c >> 3) * kHalf + tile_off(m, c & 7),
+                   terms + static_cast<int64_t>(v ? t : 0) * N + 8 * c, v);
+      }
+    }
+    find(ci + 1);
+  };
+  find(0);
+#pragma unroll
+  for (int ci = 0; ci < S - 1; ++ci) {
+    if (ci < n) issue(ci);
+    cp_async_commit();
+  }
+  constexpr int kN = RP == 128 ? N / 2 : N, kMmas = N / kN;   // an MMA has 256 columns at most
+  constexpr uint32_t idesc = idesc_bf16_f32(128, kN) | (1u << 15) | (1u << 16);
+  bool ok = true;
+  for (int ci = 0; ci < n; ++ci) {
+    cp_async_wait<S - 2>();
+    fence_proxy_async_smem();
+    __syncthreads();
+    if (tid == 0) {
+      tc_fence_after_sync();
+      const uint32_t st = ring + (ci % S) * kGradStage<RP>, su = st + kCt / 64 * kHalf;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int m = 0; m < kCt / 128; ++m)
+#pragma unroll
+          for (int q = 0; q < kMmas; ++q)
+            tc_mma_ss(tmem + m * N + q * kN, desc_mn(st + 2 * m * kHalf + ks * 2048, kHalf),
+                      desc_mn(su + q * (kN / 64) * kHalf + ks * 2048, kHalf), idesc, (ci | ks) != 0);
+      tc_commit(&bar[ci % S]);
+    }
+    if (ci + S - 1 < n) {
+      if (ci >= 1 && tid == 0)
+        ok = mbar_wait(&bar[(ci - 1) % S], static_cast<uint32_t>((ci - 1) / S) & 1u, nullptr, a.err,
+                       kWaitLimitNs);
+      if (!__syncthreads_and(ok)) break;
+      issue(ci + S - 1);
+    }
+    cp_async_commit();
+  }
+  cp_async_wait<0>();
+  if (tid == 0)
+    ok = mbar_wait(&bar[(n - 1) % S], static_cast<uint32_t>((n - 1) / S) & 1u, nullptr, a.err,
+                   kWaitLimitNs) && ok;
+  ok = __syncthreads_and(ok);
+  tc_fence_after_sync();
+  const int r = a.ad.r, rank = a.ad.rank(item.x);
+  const bool alone = a.route.item_begin[item.x + 1] - a.route.item_begin[item.x] == 1;
+  float* out = alone ? sd.out + static_cast<int64_t>(item.x) * r * sd.K
+                     : sd.part + static_cast<int64_t>(blockIdx.x) * r * sd.K;
+  // a warp's lanes are 32 columns of x; with 256 of them warps 4 .. 7 take the
+  // upper 128, else every other 16 ranks
+  const int m = kCt == 256 ? warp >> 2 : 0;
+  const int e = c0 + 128 * m + 32 * (warp & 3) + lane;
+  const uint32_t acc = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + m * N;
+#pragma unroll 1
+  for (int k = kCt == 256 ? 0 : 16 * (warp >> 2); k < RP; k += kCt == 256 ? 16 : 32) {
+    uint32_t v[3][16];
+#pragma unroll
+    for (int t = 0; t < 3; ++t) tmem_ld_32x32b_x16(acc + t * RP + k, v[t]);
+    tmem_wait_ld();
+    if (ok && e < sd.K) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (k + i < r)   // past the adapter's rank zeros, whatever x holds
+          out[static_cast<int64_t>(k + i) * sd.K + e] =
+              k + i < rank ? __uint_as_float(v[0][i]) + (__uint_as_float(v[1][i]) + __uint_as_float(v[2][i]))
+                           : 0.0f;
+    }
+  }
+  tc_end<kTmem>(tmem);
+}
+
 // -------------------------------------------------------------- host side
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
-// Everything that a call cuts its work into, from its sizes alone.
+// Everything that a call cuts its work into, from its sizes alone (and, for
+// `tc`, from whether the tensor-core kernels take its types and alignment).
 struct Plan {
-  int max_tiles, max_items, tokens_per_item;
+  bool tc;
+  int tile, max_tiles, max_items, tokens_per_item;
   int splits_in, per_in, splits_out, per_out;   // shrink over K_in, over K_out
-  size_t counts, perm, tiles, items, begin, v, du, part, total;
+  size_t counts, perm, tiles, items, begin, v, du, v_terms, du_terms, part_a, part_b, total;
 };
 
 void cut(int64_t K, int tiles, int most, int* splits, int* per) {
@@ -719,16 +1226,21 @@ void cut(int64_t K, int tiles, int most, int* splits, int* per) {
   *splits = (chunks + *per - 1) / *per;
 }
 
-Plan make_plan(int64_t T, int64_t n, int64_t r, int64_t K_in, int64_t K_out, bool backward) {
+int64_t padded_rank(int64_t r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }
+
+Plan make_plan(int64_t T, int64_t n, int64_t r, int64_t K_in, int64_t K_out, bool backward, bool tc) {
   Plan p{};
+  p.tc = tc;
+  p.tile = tc ? kTcTile : kTile;
   const int64_t used = n < T ? n : T;
-  p.max_tiles = static_cast<int>((T + kTile - 1) / kTile + used + 1);
+  p.max_tiles = static_cast<int>((T + p.tile - 1) / p.tile + used + 1);
   const int most = T <= 64 ? 32 : 8;
   cut(K_in, p.max_tiles, most, &p.splits_in, &p.per_in);
   cut(K_out, p.max_tiles, most, &p.splits_out, &p.per_out);
-  // grad: at least two CTAs an SM over the narrower of the two widths
-  const int64_t K = K_in < K_out ? K_in : K_out;
-  const int64_t want = (2 * device_sm_count() * kCols + K - 1) / K;
+  // grad: about two CTAs an SM over the columns of both gradients
+  const int64_t ct = tc && r <= 64 ? 256 : kCols;
+  const int64_t column_tiles = (K_in + ct - 1) / ct + (K_out + ct - 1) / ct;
+  const int64_t want = (2 * device_sm_count() + column_tiles - 1) / column_tiles;
   int64_t per = (T + want - 1) / want;
   per = (per + kTile - 1) / kTile * kTile;
   if (per < kTile) per = kTile;
@@ -746,11 +1258,15 @@ Plan make_plan(int64_t T, int64_t n, int64_t r, int64_t K_in, int64_t K_out, boo
   p.items = take(sizeof(int4) * static_cast<size_t>(p.max_items));
   p.begin = take(sizeof(int) * static_cast<size_t>(n + 1));
   const size_t row = sizeof(float) * static_cast<size_t>(T) * static_cast<size_t>(r);
+  const size_t term = sizeof(__nv_bfloat16) * static_cast<size_t>(T * padded_rank(r));
   p.v = take(row * p.splits_in);
+  if (tc) p.v_terms = take(term * (backward ? 3 : 2));
   if (backward) {
     p.du = take(row * p.splits_out);
-    p.part = take(sizeof(float) * static_cast<size_t>(p.max_items) * static_cast<size_t>(r) *
-                  static_cast<size_t>(K_in > K_out ? K_in : K_out));
+    if (tc) p.du_terms = take(term * 3);
+    const size_t part = sizeof(float) * static_cast<size_t>(p.max_items) * static_cast<size_t>(r);
+    p.part_a = take(part * static_cast<size_t>(K_in));
+    p.part_b = take(part * static_cast<size_t>(K_out));
   }
   p.total = at;
   return p;
@@ -793,7 +1309,7 @@ bool rows_aligned(const void* p, int64_t ld, int64_t K, size_t elem, size_t byte
 cudaError_t run_route(const AdapterProblem& p, const Plan& pl, const Route& r, cudaStream_t s) {
   const size_t smem = sizeof(int) * (33 * static_cast<size_t>(p.n + 1) + 1);
   return go(route_kernel, dim3(1), 1024, smem, s, p.ids, static_cast<int>(p.T),
-            static_cast<int>(p.n), pl.tokens_per_item, r);
+            static_cast<int>(p.n), pl.tile, pl.tokens_per_item, r);
 }
 
 cudaError_t run_shrink(const AdapterProblem& p, const Plan& pl, const Route& route, const void* x,
@@ -805,6 +1321,12 @@ cudaError_t run_shrink(const AdapterProblem& p, const Plan& pl, const Route& rou
                static_cast<int>(K), chunks, per, rows_aligned(x, ldx, K, dtype_size(dt), 16),
                rows_aligned(w, K, K, 2, 16)};
   const dim3 grid(pl.max_tiles, splits);
+  if (pl.tc)
+    return by_rank(p.r, [&](auto rp) {
+      constexpr int RP = decltype(rp)::value;
+      return go(shrink_tc_kernel<RP>, grid, kThreads, 1024 + kShrinkStages * kShrinkStage<RP>, s, a,
+                device_error_word());
+    });
   return by_rank(p.r, [&](auto rp) {
     constexpr int RP = decltype(rp)::value;
     const int terms = dt == TBN_BF16 ? 1 : 3;
@@ -841,63 +1363,139 @@ cudaError_t run_expand(const AdapterProblem& p, const Plan& pl, const Route& rou
   });
 }
 
-cudaError_t run_grad(const AdapterProblem& p, const Plan& pl, const Route& route, const LowRank& u,
-                     const void* x, tbn_dtype dt, int64_t ldx, int64_t K, float* part, float* out,
-                     cudaStream_t s) {
-  cudaError_t e = cudaSuccess;
-  if (p.T > 0) {
-    GradArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, u, x, part, out, ldx,
-               static_cast<int>(K), rows_aligned(x, ldx, K, dtype_size(dt), 16)};
-    const dim3 grid(pl.max_items, static_cast<unsigned>((K + kCols - 1) / kCols));
-    e = by_rank(p.r, [&](auto rp) {
-      constexpr int RP = decltype(rp)::value;
-      const int terms = dt == TBN_BF16 ? 1 : 3;
-      const size_t smem = 3 * static_cast<size_t>((RP + 63) / 64 * kHalf) + terms * 2 * kHalf;
-      if (dt == TBN_BF16) return go(grad_kernel<__nv_bfloat16, RP>, grid, kThreads, smem, s, a);
-      return go(grad_kernel<float, RP>, grid, kThreads, smem, s, a);
-    });
-  }
-  if (e != cudaSuccess) return e;
-  const int64_t size = p.r * K;
+// Low-rank activations as bf16 terms, of `kTerms` a value.
+template <int kTerms>
+cudaError_t run_terms(const AdapterProblem& p, const Plan& pl, const Route& route, const LowRank& v,
+                      __nv_bfloat16* terms, float* v_out, cudaStream_t s) {
+  const TermsArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, v, terms, v_out};
+  int parts = (2 * device_sm_count() + pl.max_tiles - 1) / pl.max_tiles;   // blocks of a tile
+  if (parts > 8) parts = 8;
+  return by_rank(p.r, [&](auto rp) {
+    return go(terms_kernel<decltype(rp)::value, kTerms>, dim3(pl.max_tiles, parts), kThreads, 0, s, a);
+  });
+}
+
+cudaError_t run_expand_tc(const AdapterProblem& p, const Plan& pl, const Route& route,
+                          const __nv_bfloat16* terms, int terms_per, const void* w, int64_t K,
+                          const void* base, int64_t ldbase, void* y, int64_t ldy, cudaStream_t s) {
+  const int tiles = static_cast<int>((K + kCols - 1) / kCols);
+  int groups = (6 * device_sm_count() + pl.max_tiles - 1) / pl.max_tiles;
+  if (groups > tiles) groups = tiles;
+  const int per = (tiles + groups - 1) / groups;
+  groups = (tiles + per - 1) / per;
+  const bool wide = is_aligned(y, 32) && ldy % 16 == 0 && is_aligned(base, 32) && ldbase % 16 == 0;
+  return by_rank(p.r, [&](auto rp) {
+    constexpr int RP = decltype(rp)::value;
+    const ExpandTcArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, terms,
+                         static_cast<const __nv_bfloat16*>(w),
+                         static_cast<const __nv_bfloat16*>(base), static_cast<__nv_bfloat16*>(y),
+                         ldbase, ldy, terms_per * RP, static_cast<int>(K), per, wide,
+                         device_error_word()};
+    return go(expand_tc_kernel<RP>, dim3(pl.max_tiles, groups), kThreads,
+              1024 + kExpandV<RP> + 2 * kExpandW<RP>, s, a);
+  });
+}
+
+GradSide grad_side(const LowRank& u, const __nv_bfloat16* terms, const void* x, tbn_dtype dt,
+                   int64_t ldx, int64_t K, float* part, float* out) {
+  return {u, terms, x, part, out, ldx, static_cast<int>(K),
+          rows_aligned(x, ldx, K, dtype_size(dt), 16)};
+}
+
+cudaError_t run_grad(const AdapterProblem& p, const Plan& pl, const Route& route,
+                     const GradSide& side, tbn_dtype dt, cudaStream_t s) {
+  const GradArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, side};
+  const dim3 grid(pl.max_items, static_cast<unsigned>((side.K + kCols - 1) / kCols));
+  return by_rank(p.r, [&](auto rp) {
+    constexpr int RP = decltype(rp)::value;
+    const int terms = dt == TBN_BF16 ? 1 : 3;
+    const size_t smem = 3 * static_cast<size_t>((RP + 63) / 64 * kHalf) + terms * 2 * kHalf;
+    if (dt == TBN_BF16) return go(grad_kernel<__nv_bfloat16, RP>, grid, kThreads, smem, s, a);
+    return go(grad_kernel<float, RP>, grid, kThreads, smem, s, a);
+  });
+}
+
+cudaError_t run_grads_tc(const AdapterProblem& p, const Plan& pl, const Route& route,
+                         const GradSide* sides, int count, cudaStream_t s) {
+  return by_rank(p.r, [&](auto rp) {
+    constexpr int RP = decltype(rp)::value;
+    const auto tiles = [](const GradSide& d) { return (d.K + kGradCols<RP> - 1) / kGradCols<RP>; };
+    const GradTcArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)},
+                       {sides[0], sides[count - 1]}, tiles(sides[0]), device_error_word()};
+    const dim3 grid(pl.max_items, tiles(sides[0]) + (count > 1 ? tiles(sides[1]) : 0));
+    return go(grad_tc_kernel<RP>, grid, kThreads, 1024 + kGradStages * kGradStage<RP>, s, a);
+  });
+}
+
+cudaError_t run_reduce(const AdapterProblem& p, const Route& route, const GradSide& side,
+                       cudaStream_t s) {
+  const int64_t size = p.r * side.K;
   return launch_dependent(grad_reduce_kernel,
                           dim3(static_cast<unsigned>((size + 255) / 256), static_cast<unsigned>(p.n)),
-                          dim3(256), 0, s, route, part, out, size);
+                          dim3(256), 0, s, route, side.part, side.out, size);
+}
+
+// The tensor-core kernels: many tokens, bf16 activations in 16-byte aligned rows.
+bool takes_tc(const AdapterProblem& p, bool backward) {
+  if (p.T < kTcFrom || p.xdt != TBN_BF16 || p.ydt != TBN_BF16) return false;
+  const auto ok = [](const void* q, int64_t ld, int64_t K) {
+    return q == nullptr || rows_aligned(q, ld, K, 2, 16);
+  };
+  if (!ok(p.x, p.ldx, p.K_in) || !ok(p.a, p.K_in, p.K_in) || !ok(p.b, p.K_out, p.K_out)) return false;
+  if (backward)
+    return ok(p.dy, p.lddy, p.K_out) && ok(p.dx, p.lddx, p.K_in) && ok(p.base, p.ldbase, p.K_in);
+  return ok(p.y, p.ldy, p.K_out) && ok(p.base, p.ldbase, p.K_out);
 }
 
 }  // namespace
 
 size_t adapter_workspace_bytes(int64_t T, int64_t K_in, int64_t K_out, int64_t n, int64_t r,
                                bool backward) {
-  return make_plan(T, n, r, K_in, K_out, backward).total;
+  const size_t plain = make_plan(T, n, r, K_in, K_out, backward, false).total;
+  if (T < kTcFrom) return plain;
+  const size_t tc = make_plan(T, n, r, K_in, K_out, backward, true).total;
+  return plain > tc ? plain : tc;
 }
 
 tbn_status launch_adapter_fwd(const AdapterProblem& p, void* ws, cudaStream_t s) {
   if (p.T == 0) return TBN_OK;
-  const Plan pl = make_plan(p.T, p.n, p.r, p.K_in, p.K_out, false);
+  const Plan pl = make_plan(p.T, p.n, p.r, p.K_in, p.K_out, false, takes_tc(p, false));
   const Route route = route_at(pl, ws);
-  float* part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + pl.v);
+  uint8_t* b = static_cast<uint8_t*>(ws);
+  float* part = reinterpret_cast<float*>(b + pl.v);
   cudaError_t e = run_route(p, pl, route, s);
   if (e != cudaSuccess) return cuda_fail(e, "adapter route_kernel");
   e = run_shrink(p, pl, route, p.x, p.xdt, p.ldx, p.a, p.K_in, pl.splits_in, pl.per_in, part, s);
   if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_kernel");
   const LowRank v{part, p.T * p.r, pl.splits_in, 0};
-  e = run_expand(p, pl, route, v, p.b, p.K_out, p.base, p.ldbase, p.y, p.ydt, p.ldy, p.v_out, s);
+  if (pl.tc) {
+    __nv_bfloat16* terms = reinterpret_cast<__nv_bfloat16*>(b + pl.v_terms);
+    e = run_terms<2>(p, pl, route, v, terms, p.v_out, s);
+    if (e != cudaSuccess) return cuda_fail(e, "adapter terms_kernel");
+    e = run_expand_tc(p, pl, route, terms, 2, p.b, p.K_out, p.base, p.ldbase, p.y, p.ldy, s);
+  } else {
+    e = run_expand(p, pl, route, v, p.b, p.K_out, p.base, p.ldbase, p.y, p.ydt, p.ldy, p.v_out, s);
+  }
   return e == cudaSuccess ? TBN_OK : cuda_fail(e, "adapter expand_kernel");
 }
 
 tbn_status launch_adapter_bwd(const AdapterProblem& p, void* ws, cudaStream_t s) {
-  const Plan pl = make_plan(p.T, p.n, p.r, p.K_in, p.K_out, true);
+  const Plan pl = make_plan(p.T, p.n, p.r, p.K_in, p.K_out, true, takes_tc(p, true));
   const Route route = route_at(pl, ws);
   uint8_t* b = static_cast<uint8_t*>(ws);
   float* vpart = reinterpret_cast<float*>(b + pl.v);
-  float* du = reinterpret_cast<float*>(b + pl.du);
-  float* part = reinterpret_cast<float*>(b + pl.part);
+  float* dupart = reinterpret_cast<float*>(b + pl.du);
+  __nv_bfloat16* v_terms = reinterpret_cast<__nv_bfloat16*>(b + pl.v_terms);
+  __nv_bfloat16* du_terms = reinterpret_cast<__nv_bfloat16*>(b + pl.du_terms);
+  const bool need_du = p.dx != nullptr || p.da != nullptr;
   cudaError_t e = run_route(p, pl, route, s);
   if (e != cudaSuccess) return cuda_fail(e, "adapter route_kernel");
   LowRank v{p.v, 0, 1, 1};
+  const LowRank u{dupart, p.T * p.r, pl.splits_out, 0};
   if (p.T > 0) {
-    if (p.dx != nullptr || p.da != nullptr) {
-      e = run_shrink(p, pl, route, p.dy, p.ydt, p.lddy, p.b, p.K_out, pl.splits_out, pl.per_out, du, s);
+    if (need_du) {
+      e = run_shrink(p, pl, route, p.dy, p.ydt, p.lddy, p.b, p.K_out, pl.splits_out, pl.per_out,
+                     dupart, s);
       if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_kernel");
     }
     if (p.db != nullptr && p.v == nullptr) {
@@ -905,19 +1503,38 @@ tbn_status launch_adapter_bwd(const AdapterProblem& p, void* ws, cudaStream_t s)
       if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_kernel");
       v = {vpart, p.T * p.r, pl.splits_in, 0};
     }
+    if (pl.tc) {
+      if (need_du) e = run_terms<3>(p, pl, route, u, du_terms, nullptr, s);
+      if (e == cudaSuccess && p.db != nullptr) e = run_terms<3>(p, pl, route, v, v_terms, nullptr, s);
+      if (e != cudaSuccess) return cuda_fail(e, "adapter terms_kernel");
+    }
   }
-  const LowRank u{du, p.T * p.r, pl.splits_out, 0};
+  GradSide sides[2];
+  tbn_dtype types[2];
+  int count = 0;
   if (p.da != nullptr) {
-    e = run_grad(p, pl, route, u, p.x, p.xdt, p.ldx, p.K_in, part, p.da, s);
-    if (e != cudaSuccess) return cuda_fail(e, "adapter grad_kernel");
+    types[count] = p.xdt;
+    sides[count++] = grad_side(u, du_terms, p.x, p.xdt, p.ldx, p.K_in,
+                               reinterpret_cast<float*>(b + pl.part_a), p.da);
   }
   if (p.db != nullptr) {
-    e = run_grad(p, pl, route, v, p.dy, p.ydt, p.lddy, p.K_out, part, p.db, s);
-    if (e != cudaSuccess) return cuda_fail(e, "adapter grad_kernel");
+    types[count] = p.ydt;
+    sides[count++] = grad_side(v, v_terms, p.dy, p.ydt, p.lddy, p.K_out,
+                               reinterpret_cast<float*>(b + pl.part_b), p.db);
   }
+  if (pl.tc && count > 0) {
+    e = run_grads_tc(p, pl, route, sides, count, s);
+  } else if (p.T > 0) {
+    for (int i = 0; i < count && e == cudaSuccess; ++i) e = run_grad(p, pl, route, sides[i], types[i], s);
+  }
+  for (int i = 0; i < count && e == cudaSuccess; ++i) e = run_reduce(p, route, sides[i], s);
+  if (e != cudaSuccess) return cuda_fail(e, "adapter grad_kernel");
   // last: dx may be written over x or over the base
   if (p.dx != nullptr && p.T > 0) {
-    e = run_expand(p, pl, route, u, p.a, p.K_in, p.base, p.ldbase, p.dx, p.xdt, p.lddx, nullptr, s);
+    if (pl.tc)
+      e = run_expand_tc(p, pl, route, du_terms, 3, p.a, p.K_in, p.base, p.ldbase, p.dx, p.lddx, s);
+    else
+      e = run_expand(p, pl, route, u, p.a, p.K_in, p.base, p.ldbase, p.dx, p.xdt, p.lddx, nullptr, s);
     if (e != cudaSuccess) return cuda_fail(e, "adapter expand_kernel");
   }
   return TBN_OK;
