@@ -169,97 +169,132 @@ struct Route {
 
 // One block.  Warp w owns the w-th of 32 runs of tokens; it counts each
 // adapter's (lanes of equal ids find each other, so that no two add at once),
-// the counts are summed over adapters and warps, and the warp goes through its
+// the counts are summed over warps and adapters, and the warp goes through its
 // run once more to place the tokens: the order within an adapter is kept.
+// Latency is what it costs (everything else waits for it): a run's ids are asked
+// for eight at a time and kept, 8192 tokens in all.
+constexpr int kRouteBatch = 8;
+
 __global__ void __launch_bounds__(1024) route_kernel(const int32_t* ids, int T, int n,
                                                      int tile, int tokens_per_item, Route r) {
-  extern __shared__ int sh[];          // counts [32][n + 1], then starts [n + 2]
-  __shared__ int warp_sum[32][2], total[2];
+  extern __shared__ int sh[];          // counts [n + 1][32], then starts, tiles, items [n + 2] each
+  __shared__ int warp_sum[3][32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int groups = n + 1;            // the last: no adapter
-  int* start = sh + 32 * groups;
+  int *start = sh + 32 * groups, *first_tile = start + groups + 1, *first_item = first_tile + groups + 1;
+  for (int i = tid; i < 32 * groups; i += 1024) sh[i] = 0;
   grid_dependency_wait();
   grid_dependents_launch();
-  for (int i = tid; i < 32 * groups; i += 1024) sh[i] = 0;
-  __syncthreads();
   const int run = (T + 31) / 32;
   const int beg = min(T, warp * run), end = min(T, beg + run);
-  const auto group_of = [&](int t) {
-    const int id = ids != nullptr ? ids[t] : 0;
-    return id >= 0 && id < n ? id : n;
+  int g[kRouteBatch];   // groups of the lane's tokens of a batch, -1: none
+  const auto load = [&](int t0) {
+#pragma unroll
+    for (int i = 0; i < kRouteBatch; ++i) {
+      const int t = t0 + 32 * i + lane;
+      g[i] = t < end ? (ids != nullptr ? __ldg(ids + t) : 0) : -2;
+    }
+#pragma unroll
+    for (int i = 0; i < kRouteBatch; ++i)
+      g[i] = g[i] >= 0 && g[i] < n ? g[i] : t0 + 32 * i + lane < end ? n : -1;
   };
-  for (int t0 = beg; t0 < end; t0 += 32) {
-    const int t = t0 + lane;
-    const int g = t < end ? group_of(t) : -1;
-    const uint32_t same = __match_any_sync(0xffffffffu, g);
-    if (g >= 0 && lane == __ffs(same) - 1) sh[warp * groups + g] += __popc(same);
-    __syncwarp();
-  }
+  load(beg);
   __syncthreads();
-  // thread g: adapter g's tokens, tiles and items; exclusive sums over adapters
-  int tokens = 0;
-  if (tid < groups) {
-    for (int w = 0; w < 32; ++w) {
-      const int c = sh[w * groups + tid];
-      sh[w * groups + tid] = tokens;
-      tokens += c;
+  for (int t0 = beg; t0 < end; t0 += 32 * kRouteBatch) {
+    if (t0 != beg) load(t0);
+#pragma unroll
+    for (int i = 0; i < kRouteBatch; ++i) {
+      if (t0 + 32 * i >= end) break;
+      const uint32_t same = __match_any_sync(0xffffffffu, g[i]);
+      if (g[i] >= 0 && lane == __ffs(same) - 1) sh[g[i] * 32 + warp] += __popc(same);
+      __syncwarp();
     }
   }
-  const int tiles = (tokens + tile - 1) / tile;
-  const int items = tid < n ? (tokens + tokens_per_item - 1) / tokens_per_item : 0;
-  const auto exclusive = [&](int v, int* sum_all) {
-    int s = v;
+  __syncthreads();
+  // a warp per adapter: its runs' counts become their first places
+  for (int q = warp; q < groups; q += 32) {
+    const int c = sh[q * 32 + lane];
+    int s = c;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int u = __shfl_up_sync(0xffffffffu, s, o);
       if (lane >= o) s += u;
     }
-    if (lane == 31) warp_sum[warp][0] = s;
-    __syncthreads();
-    if (warp == 0) {
-      int w = warp_sum[lane][0], x = w;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += u;
-      }
-      warp_sum[lane][1] = x - w;
-      if (lane == 31) *sum_all = x;
-    }
-    __syncthreads();
-    return s - v + warp_sum[warp][1];
-  };
-  __shared__ int unused;
-  const int first = exclusive(tokens, &unused);
-  const int first_tile = exclusive(tiles, &total[0]);
-  const int first_item = exclusive(items, &total[1]);
-  if (tid < groups) {
-    start[tid] = first;
-    const int adapter = tid < n ? tid : -1;
-    for (int i = 0; i < tiles; ++i)
-      r.tiles[first_tile + i] =
-          make_int4(adapter, first + i * tile, min(tile, tokens - i * tile), 0);
-    for (int i = 0; i < items; ++i)
-      r.items[first_item + i] = make_int4(adapter, first + i * tokens_per_item,
-                                          min(tokens_per_item, tokens - i * tokens_per_item), 0);
-    r.item_begin[tid] = first_item;
-  }
-  if (tid == 0) {
-    r.counts[0] = total[0];
-    r.counts[1] = total[1];
+    sh[q * 32 + lane] = s - c;
+    if (lane == 31) start[q] = s;
   }
   __syncthreads();
-  for (int t0 = beg; t0 < end; t0 += 32) {
-    const int t = t0 + lane;
-    const int g = t < end ? group_of(t) : -1;
-    const uint32_t same = __match_any_sync(0xffffffffu, g);
-    if (g >= 0) {
-      const int at = start[g] + sh[warp * groups + g] + __popc(same & ((1u << lane) - 1u));
-      r.perm[at] = t;
+  // exclusive sums over the adapters of tokens, tiles and items
+  int v[3] = {0, 0, 0}, s[3];
+  if (tid < groups) {
+    v[0] = start[tid];
+    v[1] = (v[0] + tile - 1) / tile;
+    v[2] = tid < n ? (v[0] + tokens_per_item - 1) / tokens_per_item : 0;
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    s[k] = v[k];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, s[k], o);
+      if (lane >= o) s[k] += u;
     }
-    __syncwarp();
-    if (g >= 0 && lane == __ffs(same) - 1) sh[warp * groups + g] += __popc(same);
-    __syncwarp();
+    if (lane == 31) warp_sum[k][warp] = s[k];
+  }
+  __syncthreads();
+  if (warp < 3) {
+    const int c = warp_sum[warp][lane];
+    int x = c;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += u;
+    }
+    warp_sum[warp][lane] = x - c;
+  }
+  __syncthreads();
+  if (tid < groups) {
+    start[tid] = s[0] - v[0] + warp_sum[0][warp];
+    first_tile[tid] = s[1] - v[1] + warp_sum[1][warp];
+    first_item[tid] = s[2] - v[2] + warp_sum[2][warp];
+    r.item_begin[tid] = first_item[tid];
+    if (tid == groups - 1) {
+      start[groups] = start[tid] + v[0];
+      first_tile[groups] = first_tile[tid] + v[1];
+      first_item[groups] = first_item[tid] + v[2];
+      r.counts[0] = first_tile[groups];
+      r.counts[1] = first_item[groups];
+    }
+  }
+  __syncthreads();
+  // the lists: entry i belongs to the last adapter that begins at or before it
+  const auto list = [&](const int* begin, int4* out, int per) {
+    for (int i = tid; i < begin[groups]; i += 1024) {
+      int lo = 0, hi = groups;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (begin[mid] <= i) lo = mid;
+        else hi = mid;
+      }
+      const int at = start[lo] + (i - begin[lo]) * per;
+      out[i] = make_int4(lo < n ? lo : -1, at, min(per, start[lo + 1] - at), 0);
+    }
+  };
+  list(first_tile, r.tiles, tile);
+  list(first_item, r.items, tokens_per_item);
+  for (int t0 = beg; t0 < end; t0 += 32 * kRouteBatch) {
+    if (run > 32 * kRouteBatch) load(t0);
+#pragma unroll
+    for (int i = 0; i < kRouteBatch; ++i) {
+      if (t0 + 32 * i >= end) break;
+      const uint32_t same = __match_any_sync(0xffffffffu, g[i]);
+      if (g[i] >= 0)
+        r.perm[start[g[i]] + sh[g[i] * 32 + warp] + __popc(same & ((1u << lane) - 1u))] =
+            t0 + 32 * i + lane;
+      __syncwarp();
+      if (g[i] >= 0 && lane == __ffs(same) - 1) sh[g[i] * 32 + warp] += __popc(same);
+      __syncwarp();
+    }
   }
 }
 
@@ -283,7 +318,7 @@ struct ShrinkArgs {
   const __nv_bfloat16* w;    // [n][r][K]
   float* part;               // [splits][T][r], by sorted position
   int64_t ldx;
-  int T, K, chunks, chunks_per;
+  int T, K, chunks, chunks_per, splits;
   int x_aligned, w_aligned;
 };
 
@@ -691,18 +726,39 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
       }
 }
 
-// Adapters of several items: their sums in order; of none: zeros.
-__global__ void __launch_bounds__(256) grad_reduce_kernel(Route route, const float* part,
-                                                          float* out, int64_t size) {
+// Adapters of several items: their sums in order; of none: zeros.  Four
+// consecutive values a thread where that divides both gradients' rows.
+struct ReduceArgs {
+  Route route;
+  const float* part[2];
+  float* out[2];
+  int64_t size[2];   // r K, of gridDim.z gradients
+};
+
+template <int kWide>
+__global__ void __launch_bounds__(256) grad_reduce_kernel(const __grid_constant__ ReduceArgs a) {
+  using V = typename std::conditional<kWide == 4, float4, float>::type;
   grid_dependency_wait();
   grid_dependents_launch();
-  const int beg = route.item_begin[blockIdx.y], end = route.item_begin[blockIdx.y + 1];
+  const int beg = a.route.item_begin[blockIdx.y], end = a.route.item_begin[blockIdx.y + 1];
   if (end - beg == 1) return;
-  const int64_t i = blockIdx.x * 256ll + threadIdx.x;
+  const int64_t size = a.size[blockIdx.z];
+  const int64_t i = (blockIdx.x * 256ll + threadIdx.x) * kWide;
   if (i >= size) return;
-  float s = 0.0f;
-  for (int k = beg; k < end; ++k) s += part[k * size + i];
-  out[blockIdx.y * size + i] = s;
+  const float* part = a.part[blockIdx.z] + i;
+  float s[kWide] = {};
+#pragma unroll 8
+  for (int k = beg; k < end; ++k) {
+    const V v = *reinterpret_cast<const V*>(part + k * size);
+    const float* f = reinterpret_cast<const float*>(&v);
+#pragma unroll
+    for (int j = 0; j < kWide; ++j) s[j] += f[j];
+  }
+  V v;
+  float* f = reinterpret_cast<float*>(&v);
+#pragma unroll
+  for (int j = 0; j < kWide; ++j) f[j] = s[j];
+  *reinterpret_cast<V*>(a.out[blockIdx.z] + blockIdx.y * size + i) = v;
 }
 
 // ==================================================================== tcgen05
@@ -713,6 +769,8 @@ __global__ void __launch_bounds__(256) grad_reduce_kernel(Route route, const flo
 // bf16 terms (terms_kernel), a row's terms side by side.
 constexpr int kTcTile = 128;
 constexpr int64_t kTcFrom = 128;   // tokens
+constexpr int kExpandCtas = 4;      // of expand, an SM and launch
+constexpr int kGradCtas = 2;        // of grad
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
@@ -770,8 +828,16 @@ __device__ __forceinline__ uint8_t* align_1k(uint8_t* p) {
   return p + ((1024u - (smem_addr(p) & 1023u)) & 1023u);
 }
 
-// ---- shrink: D[128 tokens][RP] over a range of K, both operands K-major
-constexpr int kShrinkStages = 4;
+// 32 bytes to a 32-byte aligned address: a whole sector.
+__device__ __forceinline__ void store_32(void* p, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]),
+               "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+
+// ---- shrink: D[128 tokens][RP] over every splits-th chunk of K, both operands
+// K-major
+constexpr int kShrinkStages = 3;
 template <int RP>
 constexpr int kShrinkStage = kTcTile * 128 + RP * 128;
 
@@ -784,14 +850,15 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const ShrinkArgs a,
   constexpr int kWPieces = (RP * 8 + kThreads - 1) / kThreads;
   grid_dependency_wait();
   grid_dependents_launch();
-  if (static_cast<int>(blockIdx.x) >= a.route.counts[0]) return;
-  const int4 tile = a.route.tiles[blockIdx.x];
+  const int tile_id = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+  if (tile_id >= a.route.counts[0]) return;
+  const int4 tile = a.route.tiles[tile_id];
   if (tile.x < 0) return;
   const uint32_t tmem = tc_begin<kTmem>(&slot, bar, S);
   const uint32_t ring = smem_addr(align_1k(smem_raw));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, ch = tid & 7;
   const int rank = a.ad.rank(tile.x);
-  const int c0 = blockIdx.y * a.chunks_per, n = min(a.chunks, c0 + a.chunks_per) - c0;
+  const int n = (a.chunks - split + a.splits - 1) / a.splits;   // chunks split, split + splits, ...
   const __nv_bfloat16* xr[4];
   uint32_t there = 0;
 #pragma unroll
@@ -805,7 +872,7 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const ShrinkArgs a,
   const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * a.ad.r * a.K;
   const auto issue = [&](int ci) {
     const uint32_t st = ring + (ci % S) * kShrinkStage<RP>;
-    const int e = (c0 + ci) * kChunk + 8 * ch;
+    const int e = (split + ci * a.splits) * kChunk + 8 * ch;
     const bool in = e < a.K;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -858,58 +925,96 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const ShrinkArgs a,
                    kWaitLimitNs) && ok;
   ok = __syncthreads_and(ok);
   tc_fence_after_sync();
-  // warp w: tokens 32 (w % 4) .., every other 16 ranks
-  const int row = 32 * (warp & 3) + lane;
-  float* out = a.part + (static_cast<int64_t>(blockIdx.y) * a.T + tile.y + row) * a.ad.r;
+  // warp w: tokens 32 (w % 4) .., every other 16 ranks.  A thread holds a row:
+  // its stores are as wide as the rows' alignment lets them be (single floats
+  // cost a sector each: 10 us of the kernel's 28 at 8192 tokens, rank 64)
+  const int row = 32 * (warp & 3) + lane, r = a.ad.r;
+  float* out = a.part + (static_cast<int64_t>(split) * a.T + tile.y + row) * r;
 #pragma unroll
   for (int c = 16 * (warp >> 2); c < RP; c += 32) {
     uint32_t v[16];
     tmem_ld_32x32b_x16(tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + c, v);
     tmem_wait_ld();
-    if (ok && row < tile.z) {
+    if (!ok || row >= tile.z) continue;
+    if (r % 16 == 0) {
+      if (c < r) {
+        store_32(out + c, &v[0]);
+        store_32(out + c + 8, &v[8]);
+      }
+    } else {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (c + i < a.ad.r) out[c + i] = __uint_as_float(v[i]);
+        if (c + i < r) out[c + i] = __uint_as_float(v[i]);
     }
   }
   tc_end<kTmem>(tmem);
 }
 
 // ---- the low-rank activations as bf16 terms, by sorted position
-struct TermsArgs {
-  Route route;
-  Adapters ad;
+struct TermsSide {
   LowRank v;
   __nv_bfloat16* terms;   // [T][kTerms RP]
   float* v_out;           // or nullptr: [T][r] by token, unscaled
 };
 
-// A tile per block.  Past the rank the terms are zero, whatever v holds there.
+struct TermsArgs {
+  Route route;
+  Adapters ad;
+  TermsSide side[2];      // gridDim.z of them
+};
+
+// Block (tile, part, side); a thread takes eight ranks of a token.  Past the rank
+// the terms are zero, whatever v holds there.
 template <int RP, int kTerms>
-__global__ void __launch_bounds__(kThreads) terms_kernel(const TermsArgs a) {
+__global__ void __launch_bounds__(kThreads) terms_kernel(const __grid_constant__ TermsArgs a) {
   grid_dependency_wait();
   grid_dependents_launch();
   if (static_cast<int>(blockIdx.x) >= a.route.counts[0]) return;
   const int4 tile = a.route.tiles[blockIdx.x];
+  const TermsSide& sd = a.side[blockIdx.z];
   const int r = a.ad.r, rank = tile.x < 0 ? 0 : a.ad.rank(tile.x);
-  if (tile.x < 0 && a.v_out == nullptr) return;
+  if (tile.x < 0 && sd.v_out == nullptr) return;
   const float factor = tile.x < 0 ? 0.0f : a.ad.factor(tile.x);
-  for (int i = threadIdx.x + blockIdx.y * kThreads; i < tile.z * RP / 2; i += kThreads * gridDim.y) {
-    const int m = i / (RP / 2), col = 2 * (i % (RP / 2));
+  const bool whole = r % 8 == 0;   // eight ranks lie in whole 16-byte words
+  for (int i = threadIdx.x + blockIdx.y * kThreads; i < tile.z * (RP / 8);
+       i += kThreads * gridDim.y) {
+    const int m = i / (RP / 8), col = 8 * (i % (RP / 8));
     const int token = a.route.perm[tile.y + m];
-    const int64_t at = a.v.by_token ? token : tile.y + m;
-    float v[2] = {0.0f, 0.0f};
+    const float* p = sd.v.p + static_cast<int64_t>(sd.v.by_token ? token : tile.y + m) * r + col;
+    float v[8] = {};
+    if (whole && col < rank) {
+#pragma unroll 4
+      for (int q = 0; q < sd.v.splits; ++q) {
+        const float4* f = reinterpret_cast<const float4*>(p + q * sd.v.split_stride);
+        const float4 x = f[0], y = f[1];
+        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+        v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+      }
+    } else if (!whole) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-      if (col + j < rank) v[j] = a.v.get(at, r, col + j);
-    if (a.v_out != nullptr) {
-      float* o = a.v_out + static_cast<int64_t>(token) * r;
-      if (col < r) o[col] = v[0];
-      if (col + 1 < r) o[col + 1] = v[1];
+      for (int j = 0; j < 8; ++j)
+        if (col + j < rank)
+          for (int q = 0; q < sd.v.splits; ++q) v[j] += p[q * sd.v.split_stride + j];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (col + j >= rank) v[j] = 0.0f;
+    if (sd.v_out != nullptr) {
+      float* o = sd.v_out + static_cast<int64_t>(token) * r + col;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (col + j < r) o[j] = v[j];
     }
     if (tile.x < 0) continue;
-    store_pair<kTerms>(reinterpret_cast<uint8_t*>(a.terms + (tile.y + m) * static_cast<int64_t>(kTerms * RP)),
-                       2 * RP, 2 * col, v[0] * factor, v[1] * factor);
+    float t[8][kTerms];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) split(v[j] * factor, t[j]);
+    __nv_bfloat16* out = sd.terms + (tile.y + m) * static_cast<int64_t>(kTerms * RP) + col;
+#pragma unroll
+    for (int k = 0; k < kTerms; ++k)
+      *reinterpret_cast<uint4*>(out + k * RP) =
+          make_uint4(pack_bf16x2(t[0][k], t[1][k]), pack_bf16x2(t[2][k], t[3][k]),
+                     pack_bf16x2(t[4][k], t[5][k]), pack_bf16x2(t[6][k], t[7][k]));
   }
 }
 
@@ -922,188 +1027,219 @@ struct ExpandTcArgs {
   const __nv_bfloat16* base;    // or nullptr
   __nv_bfloat16* y;
   int64_t ldbase, ldy;
-  int row_terms, K, cols_per;
-  int wide;                     // rows of base and y start at multiples of 32 bytes
+  int row_terms, K, groups;     // CTAs of a tile
   uint32_t* err;
 };
-
-// 64 bytes of a row (32 bf16, of which `left` exist) as four 16-byte words.
-__device__ __forceinline__ void load_64(uint4 (&d)[4], const __nv_bfloat16* p, bool wide, int left) {
-  if (wide && left >= 32) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                   : "=r"(d[2 * i].x), "=r"(d[2 * i].y), "=r"(d[2 * i].z), "=r"(d[2 * i].w),
-                     "=r"(d[2 * i + 1].x), "=r"(d[2 * i + 1].y), "=r"(d[2 * i + 1].z),
-                     "=r"(d[2 * i + 1].w)
-                   : "l"(p + 16 * i)
-                   : "memory");
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      d[i] = 8 * i < left ? *reinterpret_cast<const uint4*>(p + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
-  }
-}
-
-__device__ __forceinline__ void store_64(__nv_bfloat16* p, const uint4 (&d)[4], bool wide, int left) {
-  if (wide && left >= 32) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + 16 * i),
-                   "r"(d[2 * i].x), "r"(d[2 * i].y), "r"(d[2 * i].z), "r"(d[2 * i].w),
-                   "r"(d[2 * i + 1].x), "r"(d[2 * i + 1].y), "r"(d[2 * i + 1].z), "r"(d[2 * i + 1].w)
-                   : "memory");
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (8 * i < left) *reinterpret_cast<uint4*>(p + 8 * i) = d[i];
-  }
-}
 
 template <int RP>
 constexpr int kExpandV = (2 * RP + 63) / 64 * kTcTile * 128;
 template <int RP>
-constexpr int kExpandW = 2 * RP * 128;   // of a stage: two blocks of 64 columns
-
-// CTA (tile, column group).  V is the K-major operand, w the other, ranks as
-// steps.  A thread owns a token's row: it reads and writes 64 bytes at a time, so
-// that every 32-byte sector is moved whole without going through shared memory.
+constexpr int kExpandW = 2 * RP * 128;            // of a stage: two blocks of 64 columns
+constexpr int kExpandThreads = 512;
+constexpr int kExpandRows = kExpandThreads / 16;  // rows of y of a pass
+constexpr int kExpandY = kTcTile * kCols * 2;     // the base's rows, then y's
 template <int RP>
-__global__ void __launch_bounds__(kThreads, RP == 128 ? 1 : 3) expand_tc_kernel(const ExpandTcArgs a) {
+constexpr int kExpandYs = RP == 64 ? 1 : 2;       // as many as leave room for the CTAs
+template <int RP>
+constexpr int kExpandSmem =
+    1024 + kExpandV<RP> + 2 * kExpandW<RP> + kExpandYs<RP> * kExpandY;
+
+// CTA (tile, column tiles group, group + groups, ...), two on an SM up to rank
+// 64.  V is the K-major operand, w the other, ranks as steps.  The MMAs of one
+// column tile run while the tile before it is finished: a thread adds its token's
+// sums to the base's row in shared memory (16-byte chunk c of row m at c ^ (m &
+// 7)), and y leaves in rows of 256 bytes, as the base came.  (Rows read and
+// written by their own threads take a tag lookup a sector: 88 us at 8209 x 8192,
+// rank 64.)
+template <int RP>
+__global__ void __launch_bounds__(kExpandThreads, RP <= 64 ? 2 : 1)
+    expand_tc_kernel(const __grid_constant__ ExpandTcArgs a) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bar[1];
+  __shared__ uint64_t bar[2];
   __shared__ uint32_t slot;
+  __shared__ int token[kTcTile];
   grid_dependency_wait();
   grid_dependents_launch();
-  if (static_cast<int>(blockIdx.x) >= a.route.counts[0]) return;
-  const int4 tile = a.route.tiles[blockIdx.x];
+  const int tile_id = blockIdx.x / a.groups, group = blockIdx.x % a.groups;
+  if (tile_id >= a.route.counts[0]) return;
+  const int4 tile = a.route.tiles[tile_id];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int row = 32 * (warp & 3) + lane, half = 64 * (warp >> 2);
-  const bool there = row < tile.z;
-  const int64_t token = there ? a.route.perm[tile.y + row] : 0;
-  const __nv_bfloat16* base = a.base == nullptr ? nullptr : a.base + token * a.ldbase;
-  __nv_bfloat16* y = a.y + token * a.ldy;
-  const int col_beg = blockIdx.y * a.cols_per * kCols;
-  const int col_end = min(a.K, col_beg + a.cols_per * kCols);
+  if (tid < kTcTile) token[tid] = tid < tile.z ? a.route.perm[tile.y + tid] : 0;
+  // this thread's pieces of a tile of y: chunk tid % 16 of rows tid / 16 + 32 i
+  const int pc = tid & 15, prow = tid >> 4;
   if (tile.x < 0) {   // no adapter: the base, or zeros
-    if (!there || base == y) return;
-    for (int c = col_beg + half; c < col_end; c += c % kCols == half + 32 ? kCols - 32 : 32) {
-      uint4 d[4] = {};
-      if (base != nullptr) load_64(d, base + c, a.wide, a.K - c);
-      store_64(y + c, d, a.wide, a.K - c);
-    }
+    if (a.base == a.y && a.ldbase == a.ldy) return;
+    __syncthreads();
+    for (int c = group * kCols + 8 * pc; c < a.K; c += a.groups * kCols)
+      for (int m = prow; m < tile.z; m += kExpandRows) {
+        uint4 d = make_uint4(0u, 0u, 0u, 0u);
+        if (a.base != nullptr) d = *reinterpret_cast<const uint4*>(a.base + token[m] * a.ldbase + c);
+        *reinterpret_cast<uint4*>(a.y + token[m] * a.ldy + c) = d;
+      }
     return;
   }
-  const uint32_t tmem = tc_begin<kCols>(&slot, bar, 1);
-  const uint32_t sv = smem_addr(align_1k(smem_raw)), sw = sv + kExpandV<RP>;
+  const uint32_t tmem = tc_begin<2 * kCols>(&slot, bar, 2);
+  uint8_t* smem = align_1k(smem_raw);
+  uint8_t* ybuf = smem + kExpandV<RP> + 2 * kExpandW<RP>;
+  const uint32_t sv = smem_addr(smem), sw = sv + kExpandV<RP>, sy = smem_addr(ybuf);
   const int rank = a.ad.rank(tile.x);
   const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * a.ad.r * a.K;
+  const int tiles = (a.K + kCols - 1) / kCols, n = (tiles - group + a.groups - 1) / a.groups;
+  const auto column = [&](int t) { return (group + t * a.groups) * kCols; };
+  const auto load_w = [&](int t) {
+    if (t < n) {
+      const int c0 = column(t);
+#pragma unroll
+      for (int i = 0; i < (RP + kExpandRows - 1) / kExpandRows; ++i) {
+        const int wr = prow + kExpandRows * i, e = c0 + 8 * pc;
+        if (RP < kExpandRows && wr >= RP) break;
+        const bool v = wr < rank && e < a.K;
+        cp_async16(sw + (t & 1) * kExpandW<RP> + (pc >> 3) * (RP * 128) + tile_off(wr, pc & 7),
+                   v ? w + static_cast<int64_t>(wr) * a.K + e : w, v);
+      }
+    }
+    cp_async_commit();
+  };
+  constexpr int YB = kExpandYs<RP>;
+  const auto load_base = [&](int t) {
+    if (t < n) {
+      const uint32_t to = sy + (t % YB) * kExpandY;
+      const int e = column(t) + 8 * pc;
+#pragma unroll
+      for (int i = 0; i < kTcTile / kExpandRows; ++i) {
+        const int m = prow + kExpandRows * i;
+        const bool v = a.base != nullptr && m < tile.z && e < a.K;
+        cp_async16(to + m * 256 + ((pc ^ (m & 7)) << 4),
+                   v ? a.base + token[m] * a.ldbase + e : a.w, v);
+      }
+    }
+    cp_async_commit();
+  };
   constexpr int kRow = 2 * RP / 8;   // 16-byte pieces of a row of V
-  for (int p = tid; p < kTcTile * kRow; p += kThreads) {
+  for (int p = tid; p < kTcTile * kRow; p += kExpandThreads) {
     const int m = p / kRow, c = p % kRow;
     const bool v = m < tile.z;
     cp_async16(sv + (c >> 3) * (kTcTile * 128) + tile_off(m, c & 7),
                a.terms + static_cast<int64_t>(tile.y + (v ? m : 0)) * a.row_terms + 8 * c, v);
   }
-  const auto issue = [&](int c0, int st) {
-#pragma unroll
-    for (int i = 0; i < RP * 16 / kThreads; ++i) {
-      const int p = tid + i * kThreads, wr = p >> 4, pc = p & 15, e = c0 + 8 * pc;
-      const bool v = wr < rank && e < a.K;
-      cp_async16(sw + st * kExpandW<RP> + (pc >> 3) * (RP * 128) + tile_off(wr, pc & 7),
-                 v ? w + static_cast<int64_t>(wr) * a.K + e : w, v);
-    }
-    cp_async_commit();
-  };
-  issue(col_beg, 0);
+  load_w(0);      // one group with V's
+  load_w(1);
+  load_base(0);
+  if (YB == 2) load_base(1);
   constexpr uint32_t idesc = idesc_bf16_f32(128, kCols) | (1u << 16);   // w: columns contiguous
-  int turn = 0;
-  for (int c0 = col_beg; c0 < col_end; c0 += kCols, ++turn) {
-    const int st = turn & 1;
-    cp_async_wait<0>();
-    fence_proxy_async_smem();
-    __syncthreads();   // also: every warp has read the last tile's sums
-    if (tid == 0) {
-      tc_fence_after_sync();
+  bool ok = true;
+  for (int t = 0; t <= n; ++t) {
+    if (t < n) {
+      // w of tile t; the groups after it are a base and, at the start, w of tile 1
+      // and all bases that there is room for
+      if (t == 0) cp_async_wait<YB + 1>();
+      else if (t == 1) cp_async_wait<YB>();
+      else cp_async_wait<1>();
+      fence_proxy_async_smem();
+      __syncthreads();
+      if (tid == 0) {
+        tc_fence_after_sync();
+        const uint32_t wt = sw + (t & 1) * kExpandW<RP>;
 #pragma unroll
-      for (int k = 0; k < 2 * RP / 16; ++k)   // the leading terms' ranks, then the second terms'
-        tc_mma_ss(tmem,
-                  smem_desc_sw128_kmajor(sv + (k >> 2) * (kTcTile * 128) + 32 * (k & 3)),
-                  desc_mn(sw + st * kExpandW<RP> + (k % (RP / 16)) * 2048, RP * 128), idesc, k != 0);
-      tc_commit(&bar[0]);
+        for (int k = 0; k < 2 * RP / 16; ++k)   // the leading terms' ranks, then the second terms'
+          tc_mma_ss(tmem + (t & 1) * kCols,
+                    smem_desc_sw128_kmajor(sv + (k >> 2) * (kTcTile * 128) + 32 * (k & 3)),
+                    desc_mn(wt + (k % (RP / 16)) * 2048, RP * 128), idesc, k != 0);
+        tc_commit(&bar[t & 1]);
+      }
     }
-    if (c0 + kCols < col_end) issue(c0 + kCols, st ^ 1);   // last read by the MMAs waited for
-    const int c = c0 + half;
-    uint4 b[2][4] = {};
-    if (base != nullptr && there) {
-      load_64(b[0], base + c, a.wide, a.K - c);
-      load_64(b[1], base + c + 32, a.wide, a.K - c - 32);
-    }
-    const bool ok = mbar_wait(&bar[0], static_cast<uint32_t>(turn) & 1u, nullptr, a.err, kWaitLimitNs);
+    if (t == 0) continue;
+    const int q = t - 1;   // the tile to finish
+    // its base (with two buffers, later on, it came before w of tile t)
+    if (YB == 1 || t == n) cp_async_wait<0>();
+    else if (t == 1) cp_async_wait<1>();
+    ok = mbar_wait(&bar[q & 1], static_cast<uint32_t>(q >> 1) & 1u, nullptr, a.err, kWaitLimitNs);
     if (!__syncthreads_and(ok)) break;
     tc_fence_after_sync();
+    load_w(t + 1);         // over tile q's, which its MMAs have read
+    const int m = 32 * (warp & 3) + lane;
+    uint8_t* ytile = ybuf + (q % YB) * kExpandY;
+    uint8_t* yrow = ytile + m * 256;
+    const int c = 32 * (warp >> 2);   // of the tile's columns
+    uint32_t v[32];
+    tmem_ld_32x32b_x32(tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + (q & 1) * kCols + c, v);
+    tmem_wait_ld();
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      uint32_t v[32];
-      tmem_ld_32x32b_x32(tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + half + 32 * q, v);
-      tmem_wait_ld();
+    for (int i = 0; i < 4; ++i) {
+      uint4* p = reinterpret_cast<uint4*>(yrow + (((c >> 3) + i) ^ (m & 7)) * 16);
+      uint4 b = *p;
+      uint32_t* u = reinterpret_cast<uint32_t*>(&b);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t* u = reinterpret_cast<uint32_t*>(&b[q][i]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          u[j] = pack_bf16x2(__uint_as_float(v[8 * i + 2 * j]) + __uint_as_float(u[j] << 16),
-                             __uint_as_float(v[8 * i + 2 * j + 1]) + __uint_as_float(u[j] & 0xFFFF0000u));
-      }
-      if (there) store_64(y + c + 32 * q, b[q], a.wide, a.K - c - 32 * q);
+      for (int j = 0; j < 4; ++j)
+        u[j] = pack_bf16x2(__uint_as_float(v[8 * i + 2 * j]) + __uint_as_float(u[j] << 16),
+                           __uint_as_float(v[8 * i + 2 * j + 1]) + __uint_as_float(u[j] & 0xFFFF0000u));
+      *p = b;
     }
     tc_fence_before_sync();
+    __syncthreads();
+    const int e = column(q) + 8 * pc;
+    if (e < a.K) {
+#pragma unroll
+      for (int i = 0; i < kTcTile / kExpandRows; ++i) {
+        const int row = prow + kExpandRows * i;
+        if (row < tile.z)
+          *reinterpret_cast<uint4*>(a.y + token[row] * a.ldy + e) = *reinterpret_cast<const uint4*>(
+              ytile + row * 256 + ((pc ^ (row & 7)) << 4));
+      }
+    }
+    // the pieces that this thread copied out are those that it copies in
+    load_base(q + YB);
   }
   cp_async_wait<0>();
-  tc_end<kCols>(tmem);
+  tc_end<2 * kCols>(tmem);
 }
 
 // ---- grad: D[columns of x][3 RP] over an item's tokens, both operands token by
 // token.  The three terms are columns of one MMA and are added at the end, the
 // smaller ones first: each term's sum loses nothing to the leading one's size.
+constexpr int kGradTokens = 32;                  // of a stage
+constexpr int kGradBlock = kGradTokens * 128;    // bytes of 64 columns of it
 template <int RP>
 constexpr int kGradCols = RP == 128 ? 128 : 256;
 template <int RP>
-constexpr int kGradU = (3 * RP + 63) / 64 * kHalf;
+constexpr int kGradU = (3 * RP + 63) / 64 * kGradBlock;
 template <int RP>
-constexpr int kGradStage = kGradCols<RP> / 64 * kHalf + kGradU<RP>;
-constexpr int kGradStages = 3;
+constexpr int kGradStage = kGradCols<RP> / 64 * kGradBlock + kGradU<RP>;
+// 96 to 192 KB of an SM's shared memory, two CTAs up to rank 32
+template <int RP>
+constexpr int kGradStages = RP <= 32 ? 4 : 6;
 
 struct GradTcArgs {
   Route route;
   Adapters ad;
   GradSide side[2];
-  int tiles0;       // column tiles of side 0; the launch's others are side 1's
+  int tiles0, tiles;   // column tiles of side 0, and of both
   uint32_t* err;
 };
 
 template <int RP>
-__global__ void __launch_bounds__(kThreads, 1) grad_tc_kernel(const GradTcArgs a) {
+__global__ void __launch_bounds__(kThreads) grad_tc_kernel(const __grid_constant__ GradTcArgs a) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bar[kGradStages];
+  __shared__ uint64_t bar[kGradStages<RP>];
   __shared__ uint32_t slot;
-  constexpr int S = kGradStages, kCt = kGradCols<RP>, N = 3 * RP;
+  constexpr int S = kGradStages<RP>, kCt = kGradCols<RP>, N = 3 * RP;
   constexpr int kAcc = kCt / 128 * N;
   constexpr int kTmem = kAcc <= 128 ? 128 : kAcc <= 256 ? 256 : 512;
-  constexpr int kXRows = kThreads / (kCt / 8), kXPasses = 64 / kXRows;   // rows of a pass
+  constexpr int kXRows = kThreads / (kCt / 8), kXPasses = kGradTokens / kXRows;   // rows of a pass
   constexpr int kURow = N / 8;                                           // pieces of a row of u
-  constexpr int kUPasses = (64 * kURow + kThreads - 1) / kThreads;
+  constexpr int kUPasses = (kGradTokens * kURow + kThreads - 1) / kThreads;
   grid_dependency_wait();
   grid_dependents_launch();
-  if (static_cast<int>(blockIdx.x) >= a.route.counts[1]) return;
-  const int4 item = a.route.items[blockIdx.x];
-  const bool first = static_cast<int>(blockIdx.y) < a.tiles0;
+  const int item_id = blockIdx.x / a.tiles, column = blockIdx.x % a.tiles;
+  if (item_id >= a.route.counts[1]) return;
+  const int4 item = a.route.items[item_id];
+  const bool first = column < a.tiles0;
   const GradSide& sd = a.side[first ? 0 : 1];
-  const int c0 = (first ? blockIdx.y : blockIdx.y - a.tiles0) * kCt;
+  const int c0 = (first ? column : column - a.tiles0) * kCt;
   const uint32_t tmem = tc_begin<kTmem>(&slot, bar, S);
   const uint32_t ring = smem_addr(align_1k(smem_raw));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int n = (item.z + 63) / 64;
+  const int n = (item.z + kGradTokens - 1) / kGradTokens;
   const int xc = tid % (kCt / 8), xrow = tid / (kCt / 8);
   const bool col_in = c0 + 8 * xc < sd.K;
   const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(sd.x) + (col_in ? c0 + 8 * xc : 0);
@@ -1112,7 +1248,7 @@ __global__ void __launch_bounds__(kThreads, 1) grad_tc_kernel(const GradTcArgs a
   const auto find = [&](int ci) {
 #pragma unroll
     for (int i = 0; i < kXPasses; ++i) {
-      const int t = 64 * ci + xrow + kXRows * i;
+      const int t = kGradTokens * ci + xrow + kXRows * i;
       token[i] = t < item.z ? a.route.perm[item.y + t] : -1;
     }
   };
@@ -1121,16 +1257,16 @@ __global__ void __launch_bounds__(kThreads, 1) grad_tc_kernel(const GradTcArgs a
 #pragma unroll
     for (int i = 0; i < kXPasses; ++i) {
       const bool v = col_in && token[i] >= 0;
-      cp_async16(st + (xc >> 3) * kHalf + tile_off(xrow + kXRows * i, xc & 7),
+      cp_async16(st + (xc >> 3) * kGradBlock + tile_off(xrow + kXRows * i, xc & 7),
                  v ? x + token[i] * sd.ldx : x, v);
     }
 #pragma unroll
     for (int i = 0; i < kUPasses; ++i) {
       const int p = tid + i * kThreads, m = p / kURow, c = p % kURow;
-      if (64 * kURow % kThreads == 0 || m < 64) {
-        const int t = 64 * ci + m;
+      if (kGradTokens * kURow % kThreads == 0 || m < kGradTokens) {
+        const int t = kGradTokens * ci + m;
         const bool v = t < item.z;
-        cp_async16(st + kCt / 64 * kHalf + (c >> 3) * kHalf + tile_off(m, c & 7),
+        cp_async16(st + kCt / 64 * kGradBlock + (c >> 3) * kGradBlock + tile_off(m, c & 7),
                    terms + static_cast<int64_t>(v ? t : 0) * N + 8 * c, v);
       }
     }
@@ -1151,15 +1287,15 @@ __global__ void __launch_bounds__(kThreads, 1) grad_tc_kernel(const GradTcArgs a
     __syncthreads();
     if (tid == 0) {
       tc_fence_after_sync();
-      const uint32_t st = ring + (ci % S) * kGradStage<RP>, su = st + kCt / 64 * kHalf;
+      const uint32_t st = ring + (ci % S) * kGradStage<RP>, su = st + kCt / 64 * kGradBlock;
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
+      for (int ks = 0; ks < kGradTokens / 16; ++ks)
 #pragma unroll
         for (int m = 0; m < kCt / 128; ++m)
 #pragma unroll
           for (int q = 0; q < kMmas; ++q)
-            tc_mma_ss(tmem + m * N + q * kN, desc_mn(st + 2 * m * kHalf + ks * 2048, kHalf),
-                      desc_mn(su + q * (kN / 64) * kHalf + ks * 2048, kHalf), idesc, (ci | ks) != 0);
+            tc_mma_ss(tmem + m * N + q * kN, desc_mn(st + 2 * m * kGradBlock + ks * 2048, kGradBlock),
+                      desc_mn(su + q * (kN / 64) * kGradBlock + ks * 2048, kGradBlock), idesc, (ci | ks) != 0);
       tc_commit(&bar[ci % S]);
     }
     if (ci + S - 1 < n) {
@@ -1180,7 +1316,7 @@ __global__ void __launch_bounds__(kThreads, 1) grad_tc_kernel(const GradTcArgs a
   const int r = a.ad.r, rank = a.ad.rank(item.x);
   const bool alone = a.route.item_begin[item.x + 1] - a.route.item_begin[item.x] == 1;
   float* out = alone ? sd.out + static_cast<int64_t>(item.x) * r * sd.K
-                     : sd.part + static_cast<int64_t>(blockIdx.x) * r * sd.K;
+                     : sd.part + static_cast<int64_t>(item_id) * r * sd.K;
   // a warp's lanes are 32 columns of x; with 256 of them warps 4 .. 7 take the
   // upper 128, else every other 16 ranks
   const int m = kCt == 256 ? warp >> 2 : 0;
@@ -1216,9 +1352,9 @@ struct Plan {
   size_t counts, perm, tiles, items, begin, v, du, v_terms, du_terms, part_a, part_b, total;
 };
 
-void cut(int64_t K, int tiles, int most, int* splits, int* per) {
+void cut(int64_t K, int tiles, int ctas, int most, int* splits, int* per) {
   const int chunks = static_cast<int>((K + kChunk - 1) / kChunk);
-  int want = (2 * device_sm_count() + tiles - 1) / tiles;
+  int want = ctas * device_sm_count() / tiles;   // not one more: they would be a second wave
   if (want > most) want = most;
   if (want > chunks) want = chunks;
   if (want < 1) want = 1;
@@ -1235,12 +1371,14 @@ Plan make_plan(int64_t T, int64_t n, int64_t r, int64_t K_in, int64_t K_out, boo
   const int64_t used = n < T ? n : T;
   p.max_tiles = static_cast<int>((T + p.tile - 1) / p.tile + used + 1);
   const int most = T <= 64 ? 32 : 8;
-  cut(K_in, p.max_tiles, most, &p.splits_in, &p.per_in);
-  cut(K_out, p.max_tiles, most, &p.splits_out, &p.per_out);
+  const int ctas = tc && r > 64 ? 1 : 3;   // of shrink, resident on an SM
+  cut(K_in, p.max_tiles, ctas, most, &p.splits_in, &p.per_in);
+  cut(K_out, p.max_tiles, ctas, most, &p.splits_out, &p.per_out);
   // grad: about two CTAs an SM over the columns of both gradients
   const int64_t ct = tc && r <= 64 ? 256 : kCols;
   const int64_t column_tiles = (K_in + ct - 1) / ct + (K_out + ct - 1) / ct;
-  const int64_t want = (2 * device_sm_count() + column_tiles - 1) / column_tiles;
+  // (items of an adapter end unevenly: a little below two a slot is quickest)
+  const int64_t want = (kGradCtas * device_sm_count() * 4 / 5 + column_tiles - 1) / column_tiles;
   int64_t per = (T + want - 1) / want;
   per = (per + kTile - 1) / kTile * kTile;
   if (per < kTile) per = kTile;
@@ -1279,18 +1417,13 @@ Route route_at(const Plan& p, void* ws) {
           reinterpret_cast<int*>(b + p.begin)};
 }
 
-cudaError_t allow(const void* kernel, size_t smem) {
-  if (smem <= 48 * 1024) return cudaSuccess;
-  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              static_cast<int>(smem));
-}
-
-template <typename... P, typename... A>
-cudaError_t go(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s,
-               const A&... args) {
-  const cudaError_t e = allow(reinterpret_cast<const void*>(kernel), smem);
-  if (e != cudaSuccess) return e;
-  return launch_dependent(kernel, grid, dim3(threads), smem, s, args...);
+// Launches kKernel; the shared memory that it may ask for is set once.
+template <auto kKernel, typename... A>
+cudaError_t go(dim3 grid, int threads, size_t smem, cudaStream_t s, const A&... args) {
+  static const cudaError_t allowed = cudaFuncSetAttribute(
+      reinterpret_cast<const void*>(kKernel), cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024);
+  if (allowed != cudaSuccess) return allowed;
+  return launch_dependent(kKernel, grid, dim3(threads), smem, s, args...);
 }
 
 // f(std::integral_constant<int, RP>) for the padded rank of r.
@@ -1307,8 +1440,8 @@ bool rows_aligned(const void* p, int64_t ld, int64_t K, size_t elem, size_t byte
 }
 
 cudaError_t run_route(const AdapterProblem& p, const Plan& pl, const Route& r, cudaStream_t s) {
-  const size_t smem = sizeof(int) * (33 * static_cast<size_t>(p.n + 1) + 1);
-  return go(route_kernel, dim3(1), 1024, smem, s, p.ids, static_cast<int>(p.T),
+  const size_t smem = sizeof(int) * (32 * static_cast<size_t>(p.n + 1) + 3 * static_cast<size_t>(p.n + 2));
+  return go<route_kernel>(dim3(1), 1024, smem, s, p.ids, static_cast<int>(p.T),
             static_cast<int>(p.n), pl.tile, pl.tokens_per_item, r);
 }
 
@@ -1318,13 +1451,13 @@ cudaError_t run_shrink(const AdapterProblem& p, const Plan& pl, const Route& rou
   const int chunks = static_cast<int>((K + kChunk - 1) / kChunk);
   ShrinkArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, x,
                static_cast<const __nv_bfloat16*>(w), part, ldx, static_cast<int>(p.T),
-               static_cast<int>(K), chunks, per, rows_aligned(x, ldx, K, dtype_size(dt), 16),
+               static_cast<int>(K), chunks, per, splits, rows_aligned(x, ldx, K, dtype_size(dt), 16),
                rows_aligned(w, K, K, 2, 16)};
   const dim3 grid(pl.max_tiles, splits);
   if (pl.tc)
     return by_rank(p.r, [&](auto rp) {
       constexpr int RP = decltype(rp)::value;
-      return go(shrink_tc_kernel<RP>, grid, kThreads, 1024 + kShrinkStages * kShrinkStage<RP>, s, a,
+      return go<shrink_tc_kernel<RP>>(dim3(pl.max_tiles * splits), kThreads, 1024 + kShrinkStages * kShrinkStage<RP>, s, a,
                 device_error_word());
     });
   return by_rank(p.r, [&](auto rp) {
@@ -1332,8 +1465,8 @@ cudaError_t run_shrink(const AdapterProblem& p, const Plan& pl, const Route& rou
     const int terms = dt == TBN_BF16 ? 1 : 3;
     size_t smem = 2 * (terms * static_cast<size_t>(kHalf) + RP * 128);
     if (smem < sizeof(float) * kTile * RP) smem = sizeof(float) * kTile * RP;
-    if (dt == TBN_BF16) return go(shrink_kernel<__nv_bfloat16, RP>, grid, kThreads, smem, s, a);
-    return go(shrink_kernel<float, RP>, grid, kThreads, smem, s, a);
+    if (dt == TBN_BF16) return go<shrink_kernel<__nv_bfloat16, RP>>(grid, kThreads, smem, s, a);
+    return go<shrink_kernel<float, RP>>(grid, kThreads, smem, s, a);
   });
 }
 
@@ -1358,20 +1491,21 @@ cudaError_t run_expand(const AdapterProblem& p, const Plan& pl, const Route& rou
     const int terms = dt == TBN_BF16 ? 2 : 3;
     const size_t smem = static_cast<size_t>(terms) * ((RP + 63) / 64 * kHalf) + 2 * RP * 128 +
                         sizeof(float) * kTile * (kCols + 4);
-    if (dt == TBN_BF16) return go(expand_kernel<RP, 2>, grid, kThreads, smem, s, a);
-    return go(expand_kernel<RP, 3>, grid, kThreads, smem, s, a);
+    if (dt == TBN_BF16) return go<expand_kernel<RP, 2>>(grid, kThreads, smem, s, a);
+    return go<expand_kernel<RP, 3>>(grid, kThreads, smem, s, a);
   });
 }
 
 // Low-rank activations as bf16 terms, of `kTerms` a value.
 template <int kTerms>
-cudaError_t run_terms(const AdapterProblem& p, const Plan& pl, const Route& route, const LowRank& v,
-                      __nv_bfloat16* terms, float* v_out, cudaStream_t s) {
-  const TermsArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, v, terms, v_out};
+cudaError_t run_terms(const AdapterProblem& p, const Plan& pl, const Route& route,
+                      const TermsSide* sides, int count, cudaStream_t s) {
+  const TermsArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, {sides[0], sides[count - 1]}};
   int parts = (2 * device_sm_count() + pl.max_tiles - 1) / pl.max_tiles;   // blocks of a tile
   if (parts > 8) parts = 8;
   return by_rank(p.r, [&](auto rp) {
-    return go(terms_kernel<decltype(rp)::value, kTerms>, dim3(pl.max_tiles, parts), kThreads, 0, s, a);
+    return go<terms_kernel<decltype(rp)::value, kTerms>>(dim3(pl.max_tiles, parts, count), kThreads, 0,
+                                                         s, a);
   });
 }
 
@@ -1379,20 +1513,16 @@ cudaError_t run_expand_tc(const AdapterProblem& p, const Plan& pl, const Route& 
                           const __nv_bfloat16* terms, int terms_per, const void* w, int64_t K,
                           const void* base, int64_t ldbase, void* y, int64_t ldy, cudaStream_t s) {
   const int tiles = static_cast<int>((K + kCols - 1) / kCols);
-  int groups = (6 * device_sm_count() + pl.max_tiles - 1) / pl.max_tiles;
+  int groups = (kExpandCtas * device_sm_count() + pl.max_tiles - 1) / pl.max_tiles;
   if (groups > tiles) groups = tiles;
-  const int per = (tiles + groups - 1) / groups;
-  groups = (tiles + per - 1) / per;
-  const bool wide = is_aligned(y, 32) && ldy % 16 == 0 && is_aligned(base, 32) && ldbase % 16 == 0;
   return by_rank(p.r, [&](auto rp) {
     constexpr int RP = decltype(rp)::value;
     const ExpandTcArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, terms,
                          static_cast<const __nv_bfloat16*>(w),
                          static_cast<const __nv_bfloat16*>(base), static_cast<__nv_bfloat16*>(y),
-                         ldbase, ldy, terms_per * RP, static_cast<int>(K), per, wide,
+                         ldbase, ldy, terms_per * RP, static_cast<int>(K), groups,
                          device_error_word()};
-    return go(expand_tc_kernel<RP>, dim3(pl.max_tiles, groups), kThreads,
-              1024 + kExpandV<RP> + 2 * kExpandW<RP>, s, a);
+    return go<expand_tc_kernel<RP>>(dim3(pl.max_tiles * groups), kExpandThreads, kExpandSmem<RP>, s, a);
   });
 }
 
@@ -1410,8 +1540,8 @@ cudaError_t run_grad(const AdapterProblem& p, const Plan& pl, const Route& route
     constexpr int RP = decltype(rp)::value;
     const int terms = dt == TBN_BF16 ? 1 : 3;
     const size_t smem = 3 * static_cast<size_t>((RP + 63) / 64 * kHalf) + terms * 2 * kHalf;
-    if (dt == TBN_BF16) return go(grad_kernel<__nv_bfloat16, RP>, grid, kThreads, smem, s, a);
-    return go(grad_kernel<float, RP>, grid, kThreads, smem, s, a);
+    if (dt == TBN_BF16) return go<grad_kernel<__nv_bfloat16, RP>>(grid, kThreads, smem, s, a);
+    return go<grad_kernel<float, RP>>(grid, kThreads, smem, s, a);
   });
 }
 
@@ -1421,18 +1551,27 @@ cudaError_t run_grads_tc(const AdapterProblem& p, const Plan& pl, const Route& r
     constexpr int RP = decltype(rp)::value;
     const auto tiles = [](const GradSide& d) { return (d.K + kGradCols<RP> - 1) / kGradCols<RP>; };
     const GradTcArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)},
-                       {sides[0], sides[count - 1]}, tiles(sides[0]), device_error_word()};
-    const dim3 grid(pl.max_items, tiles(sides[0]) + (count > 1 ? tiles(sides[1]) : 0));
-    return go(grad_tc_kernel<RP>, grid, kThreads, 1024 + kGradStages * kGradStage<RP>, s, a);
+                       {sides[0], sides[count - 1]}, tiles(sides[0]),
+                       tiles(sides[0]) + (count > 1 ? tiles(sides[1]) : 0), device_error_word()};
+    return go<grad_tc_kernel<RP>>(dim3(pl.max_items * a.tiles), kThreads, 1024 + kGradStages<RP> * kGradStage<RP>, s, a);
   });
 }
 
-cudaError_t run_reduce(const AdapterProblem& p, const Route& route, const GradSide& side,
+cudaError_t run_reduce(const AdapterProblem& p, const Route& route, const GradSide* sides, int count,
                        cudaStream_t s) {
-  const int64_t size = p.r * side.K;
-  return launch_dependent(grad_reduce_kernel,
-                          dim3(static_cast<unsigned>((size + 255) / 256), static_cast<unsigned>(p.n)),
-                          dim3(256), 0, s, route, side.part, side.out, size);
+  ReduceArgs a{route, {}, {}, {}};
+  int64_t most = 0;
+  bool wide = true;
+  for (int i = 0; i < count; ++i) {
+    a.part[i] = sides[i].part;
+    a.out[i] = sides[i].out;
+    a.size[i] = p.r * sides[i].K;
+    most = a.size[i] > most ? a.size[i] : most;
+    wide = wide && a.size[i] % 4 == 0 && is_aligned(a.out[i], 16);
+  }
+  const int64_t per = wide ? 1024 : 256;
+  const dim3 grid(static_cast<unsigned>((most + per - 1) / per), static_cast<unsigned>(p.n), count);
+  return launch_dependent(wide ? grad_reduce_kernel<4> : grad_reduce_kernel<1>, grid, dim3(256), 0, s, a);
 }
 
 // The tensor-core kernels: many tokens, bf16 activations in 16-byte aligned rows.
@@ -1470,7 +1609,8 @@ tbn_status launch_adapter_fwd(const AdapterProblem& p, void* ws, cudaStream_t s)
   const LowRank v{part, p.T * p.r, pl.splits_in, 0};
   if (pl.tc) {
     __nv_bfloat16* terms = reinterpret_cast<__nv_bfloat16*>(b + pl.v_terms);
-    e = run_terms<2>(p, pl, route, v, terms, p.v_out, s);
+    const TermsSide side{v, terms, p.v_out};
+    e = run_terms<2>(p, pl, route, &side, 1, s);
     if (e != cudaSuccess) return cuda_fail(e, "adapter terms_kernel");
     e = run_expand_tc(p, pl, route, terms, 2, p.b, p.K_out, p.base, p.ldbase, p.y, p.ldy, s);
   } else {
@@ -1503,9 +1643,12 @@ tbn_status launch_adapter_bwd(const AdapterProblem& p, void* ws, cudaStream_t s)
       if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_kernel");
       v = {vpart, p.T * p.r, pl.splits_in, 0};
     }
-    if (pl.tc) {
-      if (need_du) e = run_terms<3>(p, pl, route, u, du_terms, nullptr, s);
-      if (e == cudaSuccess && p.db != nullptr) e = run_terms<3>(p, pl, route, v, v_terms, nullptr, s);
+    if (pl.tc && (need_du || p.db != nullptr)) {
+      TermsSide both[2];
+      int many = 0;
+      if (need_du) both[many++] = {u, du_terms, nullptr};
+      if (p.db != nullptr) both[many++] = {v, v_terms, nullptr};
+      e = run_terms<3>(p, pl, route, both, many, s);
       if (e != cudaSuccess) return cuda_fail(e, "adapter terms_kernel");
     }
   }
@@ -1527,7 +1670,7 @@ tbn_status launch_adapter_bwd(const AdapterProblem& p, void* ws, cudaStream_t s)
   } else if (p.T > 0) {
     for (int i = 0; i < count && e == cudaSuccess; ++i) e = run_grad(p, pl, route, sides[i], types[i], s);
   }
-  for (int i = 0; i < count && e == cudaSuccess; ++i) e = run_reduce(p, route, sides[i], s);
+  if (count > 0 && e == cudaSuccess) e = run_reduce(p, route, sides, count, s);
   if (e != cudaSuccess) return cuda_fail(e, "adapter grad_kernel");
   // last: dx may be written over x or over the base
   if (p.dx != nullptr && p.T > 0) {

@@ -99,6 +99,18 @@ SHAPES = [(1, 64, 64, 1, 8), (1, 4096, 4096, 3, 16), (2, 7, 5, 2, 1), (5, 1001, 
           (1500, 640, 704, 9, 32), (300, 1, 1, 2, 3), (257, 4100, 1028, 1, 16)]
 
 
+# many bf16 tokens in aligned rows: ranks of each padded size, one adapter and
+# many, widths that end inside a tile, tokens that end inside one
+MANY = [(513, 4096, 328, 3, 12), (129, 64, 8, 1, 16), (2050, 1032, 2000, 2, 17), (1300, 512, 136, 40, 48),
+        (700, 264, 520, 5, 65), (5000, 1024, 768, 3, 32), (9001, 256, 384, 2, 16), (400, 8, 4096, 2, 128)]
+
+
+@pytest.mark.parametrize("T,K_in,K_out,n,r", MANY)
+def test_many_tokens(T, K_in, K_out, n, r):
+    test_forward(T, K_in, K_out, n, r, BF16, BF16)
+    test_backward(T, K_in, K_out, n, r, BF16, BF16)
+
+
 @pytest.mark.parametrize("T,K_in,K_out,n,r", SHAPES)
 @pytest.mark.parametrize("xdt,ydt", [(BF16, BF16), (F32, F32), (BF16, F32), (F32, BF16)])
 def test_forward(T, K_in, K_out, n, r, xdt, ydt):
