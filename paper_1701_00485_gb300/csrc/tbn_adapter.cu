@@ -1598,6 +1598,7 @@ size_t adapter_workspace_bytes(int64_t T, int64_t K_in, int64_t K_out, int64_t n
 
 tbn_status launch_adapter_fwd(const AdapterProblem& p, void* ws, cudaStream_t s) {
   if (p.T == 0) return TBN_OK;
+  if (adapter_small_takes(p)) return launch_adapter_small(p, s);
   const Plan pl = make_plan(p.T, p.n, p.r, p.K_in, p.K_out, false, takes_tc(p, false));
   const Route route = route_at(pl, ws);
   uint8_t* b = static_cast<uint8_t*>(ws);

@@ -1,0 +1,330 @@
+// tbn_adapter_small.cu -- low-rank adapters for few tokens (a serving step) in
+// one launch:  y_t = base_t + scale_i (a_i x_t) b_i,  i = ids[t].
+//
+// What such a call has to read is each adapter in use, once: 2 r (K_in + K_out)
+// bytes, some 17 MB for 64 requests of rank 16 at 4096 -> 4096, 2.5 us of HBM
+// time, so that launches and waits are what counts.  A cluster of eight CTAs
+// takes up to four tokens of one adapter (each of them finds in ids whether it
+// has any): CTA c computes a_i x over an eighth of K_in, the eight parts are
+// exchanged through distributed shared memory, and each CTA computes its share
+// of the columns.  The loads of b_i are under way before that exchange.  With
+// few tokens several clusters share a token's columns, each with a whole v of
+// its own: reading a_i again from L2 is quicker than a second launch.  All in
+// 32 bits on the CUDA cores (products of bf16 values are exact).
+#include <cuda_bf16.h>
+
+#include "tbn_device.cuh"
+#include "tbn_internal.h"
+
+namespace tbn {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kCluster = 8;
+constexpr int kTokens = 4;           // of a cluster
+constexpr int kMaxTokens = 256;      // of a call: a thread looks at one id
+constexpr int kMaxRank = 128;
+constexpr int kAhead = 4;            // rank rows of b that a thread asks for early
+
+struct SmallArgs {
+  const void *x, *base;
+  void* y;
+  const __nv_bfloat16 *a, *b;
+  const int32_t *ids, *ranks;
+  const float* scale;
+  float* v_out;
+  int64_t ldx, ldbase, ldy;
+  int T, n, r, K_in, K_out;
+  int k_per, cols_per, vectors;      // of a CTA: elements of K_in, columns; vectors of a pass
+  int y_bf16;
+};
+
+// Eight consecutive elements from e on, of which those before `end` exist.
+template <bool kAligned>
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, int e, int end, float (&v)[8]) {
+  if constexpr (kAligned) {
+    uint4 r = make_uint4(0u, 0u, 0u, 0u);
+    if (e < end) r = __ldg(reinterpret_cast<const uint4*>(p + e));
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = e + i < end ? __bfloat162float(p[e + i]) : 0.0f;
+  }
+}
+
+template <bool kAligned>
+__device__ __forceinline__ void load8(const float* p, int e, int end, float (&v)[8]) {
+  if constexpr (kAligned) {
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+    if (e < end) {
+      a = __ldg(reinterpret_cast<const float4*>(p + e));
+      b = __ldg(reinterpret_cast<const float4*>(p + e) + 1);
+    }
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = e + i < end ? p[e + i] : 0.0f;
+  }
+}
+
+__device__ __forceinline__ float get(const void* p, bool bf16, int64_t i) {
+  return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i])
+              : static_cast<const float*>(p)[i];
+}
+__device__ __forceinline__ void put(void* p, bool bf16, int64_t i, float v) {
+  if (bf16)
+    static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+  else
+    static_cast<float*>(p)[i] = v;
+}
+
+// The address of a shared variable of this CTA in CTA `rank` of the cluster, and
+// a store to it.
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, int rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void store_cluster(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+
+// kAligned: x, a and b in rows of whole 16-byte words.
+template <typename T, bool kAligned>
+__global__ void __launch_bounds__(kThreads) adapter_small_kernel(const SmallArgs a) {
+  // the eight parts of v, then the columns' sums over the ranks' threads
+  __shared__ __align__(16) float red[kThreads * kTokens * 8];
+  float (*vpart)[kTokens][kMaxRank] = reinterpret_cast<float (*)[kTokens][kMaxRank]>(red);
+  static_assert(kCluster * kTokens * kMaxRank <= kThreads * kTokens * 8, "parts of v");
+  __shared__ float vsum[kTokens][kMaxRank];
+  __shared__ uint32_t same[kThreads / 32];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int c = blockIdx.x, token = blockIdx.z;
+  grid_dependency_wait();
+  grid_dependents_launch();
+  const int id = a.ids != nullptr ? __ldg(a.ids + token) : 0;
+  const int mine = tid >= a.T ? -1 : a.ids != nullptr ? __ldg(a.ids + tid) : 0;
+  const int col0 = (blockIdx.y * kCluster + c) * a.cols_per;
+  const int cols = min(a.K_out - col0, a.cols_per);   // may be below 1
+  if (id < 0 || id >= a.n) {   // no adapter: the base, or zeros
+    const int64_t from = token * a.ldbase + col0, to = token * a.ldy + col0;
+    if (a.base != a.y || from != to)
+      for (int i = tid; i < cols; i += kThreads)
+        put(a.y, a.y_bf16, to + i, a.base != nullptr ? get(a.base, a.y_bf16, from + i) : 0.0f);
+    if (a.v_out != nullptr && c == 0 && blockIdx.y == 0)
+      for (int i = tid; i < a.r; i += kThreads) a.v_out[static_cast<int64_t>(token) * a.r + i] = 0.0f;
+    return;
+  }
+  // the tokens of this adapter in order: this cluster begins at every kTokens-th
+  const uint32_t vote = __ballot_sync(0xffffffffu, tid < a.T && mine == id);
+  if (lane == 0) same[warp] = vote;
+  __syncthreads();
+  int before = 0;
+  for (int w = 0; w < (token >> 5); ++w) before += __popc(same[w]);
+  before += __popc(same[token >> 5] & ((1u << (token & 31)) - 1u));
+  if (before % kTokens != 0) return;   // all CTAs of the cluster alike
+  // the cluster's CTAs must run before their shared memory is written to
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  int tokens[kTokens], count = 0;
+#pragma unroll
+  for (int i = 0; i < kTokens; ++i) tokens[i] = token;
+  for (int w = token >> 5; w < kThreads / 32 && count < kTokens; ++w) {
+    uint32_t m = same[w];
+    if (w == (token >> 5)) m &= ~((1u << (token & 31)) - 1u);
+    while (m != 0u && count < kTokens) {
+      const int t = 32 * w + __ffs(m) - 1;
+      m &= m - 1u;
+#pragma unroll
+      for (int i = 0; i < kTokens; ++i)
+        if (i == count) tokens[i] = t;
+      ++count;
+    }
+  }
+  const int rank = a.ranks != nullptr ? max(0, min(__ldg(a.ranks + id), a.r)) : a.r;
+  const float factor = a.scale != nullptr ? __ldg(a.scale + id) : 1.0f;
+
+  // the first rows of b that this thread will need
+  const int vec = tid & (a.vectors - 1), rs = tid / a.vectors, splits = kThreads / a.vectors;
+  const __nv_bfloat16* b = a.b + static_cast<int64_t>(id) * a.r * a.K_out + col0;
+  float ahead[kAhead][8];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) {
+    const int q = rs + i * splits;
+    load8<kAligned>(b + static_cast<int64_t>(q < rank ? q : 0) * a.K_out, 8 * vec, q < rank ? cols : 0,
+                    ahead[i]);
+  }
+
+  // v over this CTA's part of K_in: a warp takes two ranks at a time
+  const int k0 = c * a.k_per, k1 = min(a.K_in, k0 + a.k_per);
+  const __nv_bfloat16* wa = a.a + static_cast<int64_t>(id) * a.r * a.K_in;
+  bool waited = false;
+  for (int q0 = 2 * warp; q0 < rank; q0 += 2 * (kThreads / 32)) {
+    const bool two = q0 + 1 < rank;
+    float acc[2][kTokens] = {};
+#pragma unroll 2
+    for (int e = k0 + 8 * lane; e < k1; e += 256) {
+      float w0[8], w1[8];
+      load8<kAligned>(wa + static_cast<int64_t>(q0) * a.K_in, e, k1, w0);
+      load8<kAligned>(wa + static_cast<int64_t>(two ? q0 + 1 : q0) * a.K_in, e, k1, w1);
+#pragma unroll
+      for (int t = 0; t < kTokens; ++t) {
+        if (t >= count) break;
+        float x[8];
+        load8<kAligned>(static_cast<const T*>(a.x) + tokens[t] * a.ldx, e, k1, x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          acc[0][t] = fmaf(w0[j], x[j], acc[0][t]);
+          acc[1][t] = fmaf(w1[j], x[j], acc[1][t]);
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < kTokens; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) acc[i][t] += __shfl_xor_sync(0xffffffffu, acc[i][t], o);
+    if (!waited) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    waited = true;
+    // lane 8 i + j, i < 2: rank q0 + i into CTA j
+    const int i = lane >> 3;
+    if (i < (two ? 2 : 1)) {
+#pragma unroll
+      for (int t = 0; t < kTokens; ++t)
+        if (t < count)
+          store_cluster(in_cta(smem_addr(&vpart[c][t][q0 + i]), lane & 7), i == 0 ? acc[0][t] : acc[1][t]);
+    }
+  }
+  if (!waited) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  cluster_sync();
+
+  // the eight parts, in order
+  for (int i = tid; i < kTokens * a.r; i += kThreads) {
+    const int t = i / a.r, q = i - t * a.r;
+    float v = 0.0f;
+    if (t < count && q < rank) {
+#pragma unroll
+      for (int j = 0; j < kCluster; ++j) v += vpart[j][t][q];
+      vsum[t][q] = v;
+    }
+    if (t < count && a.v_out != nullptr && c == 0 && blockIdx.y == 0) {
+      int to = token;
+#pragma unroll
+      for (int k = 1; k < kTokens; ++k)
+        if (k == t) to = tokens[k];
+      a.v_out[static_cast<int64_t>(to) * a.r + q] = v;
+    }
+  }
+  __syncthreads();
+
+  // the columns, `vectors` of eight a pass, their ranks over `splits` threads
+  for (int first = 0; first < cols; first += 8 * a.vectors) {
+    float acc[kTokens][8] = {};
+    const auto add = [&](int q, const float (&w)[8]) {
+#pragma unroll
+      for (int t = 0; t < kTokens; ++t) {
+        if (t >= count) break;
+        const float v = vsum[t][q];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[t][j] = fmaf(v, w[j], acc[t][j]);
+      }
+    };
+    int q = rs;
+    if (first == 0) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i, q += splits)
+        if (q < rank) add(q, ahead[i]);
+    }
+#pragma unroll 4
+    for (; q < rank; q += splits) {
+      float w[8];
+      load8<kAligned>(b + static_cast<int64_t>(q) * a.K_out, first + 8 * vec, cols, w);
+      add(q, w);
+    }
+    // red[token][rs][column]
+    const int width = 8 * a.vectors;
+#pragma unroll
+    for (int t = 0; t < kTokens; ++t) {
+      if (t >= count) break;
+      float4* p = reinterpret_cast<float4*>(red + (t * splits + rs) * width + 8 * vec);
+      p[0] = make_float4(acc[t][0], acc[t][1], acc[t][2], acc[t][3]);
+      p[1] = make_float4(acc[t][4], acc[t][5], acc[t][6], acc[t][7]);
+    }
+    __syncthreads();
+    const int used = min(splits, rank);
+    for (int o = tid; o < count * width; o += kThreads) {
+      const int t = o / width, col = first + o - t * width;
+      if (col >= cols) continue;
+      float s = 0.0f;
+      for (int k = 0; k < used; ++k) s += red[(t * splits + k) * width + o - t * width];
+      int to = token;
+#pragma unroll
+      for (int k = 1; k < kTokens; ++k)
+        if (k == t) to = tokens[k];
+      s *= factor;
+      if (a.base != nullptr) s += get(a.base, a.y_bf16, to * a.ldbase + col0 + col);
+      put(a.y, a.y_bf16, to * a.ldy + col0 + col, s);
+    }
+    __syncthreads();
+  }
+}
+
+template <typename T>
+cudaError_t launch(const SmallArgs& a, bool aligned, int groups, cudaStream_t s) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(kCluster, groups, a.T);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = kCluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, aligned ? adapter_small_kernel<T, true> : adapter_small_kernel<T, false>, a);
+}
+
+}  // namespace
+
+// Every cluster reads its adapter from L2, so tokens that share one cost what
+// others do; past this much the tiled kernels are quicker.
+bool adapter_small_takes(const AdapterProblem& p) {
+  return p.T <= kMaxTokens && p.T * p.r * (p.K_in + p.K_out) <= (int64_t(1) << 28);
+}
+
+tbn_status launch_adapter_small(const AdapterProblem& p, cudaStream_t s) {
+  const auto rows = [](const void* q, int64_t ld, size_t elem) {
+    return is_aligned(q, 16) && (ld * elem) % 16 == 0;
+  };
+  const bool aligned = rows(p.x, p.ldx, dtype_size(p.xdt)) && p.K_in % 8 == 0 && p.K_out % 8 == 0 &&
+                       is_aligned(p.a, 16) && is_aligned(p.b, 16);
+  // two CTAs an SM, and at least 64 columns each
+  int64_t groups = (2 * device_sm_count() + kCluster * p.T - 1) / (kCluster * p.T);
+  const int64_t most = (p.K_out + 64 * kCluster - 1) / (64 * kCluster);
+  if (groups > most) groups = most;
+  const auto share = [](int64_t K, int64_t parts) {   // in whole vectors of eight
+    return ((K + 7) / 8 + parts - 1) / parts * 8;
+  };
+  SmallArgs a{p.x, p.base, p.y, static_cast<const __nv_bfloat16*>(p.a),
+              static_cast<const __nv_bfloat16*>(p.b), p.ids, p.ranks, p.scale, p.v_out,
+              p.ldx, p.ldbase, p.ldy,
+              static_cast<int>(p.T), static_cast<int>(p.n), static_cast<int>(p.r),
+              static_cast<int>(p.K_in), static_cast<int>(p.K_out),
+              static_cast<int>(share(p.K_in, kCluster)),
+              static_cast<int>(share(p.K_out, kCluster * groups)), 1, p.ydt == TBN_BF16};
+  while (a.vectors < 64 && 8 * a.vectors < a.cols_per) a.vectors *= 2;
+  const cudaError_t e = p.xdt == TBN_BF16 ? launch<__nv_bfloat16>(a, aligned, static_cast<int>(groups), s)
+                                          : launch<float>(a, aligned, static_cast<int>(groups), s);
+  return e == cudaSuccess ? TBN_OK : cuda_fail(e, "adapter_small_kernel");
+}
+
+}  // namespace tbn

@@ -252,6 +252,9 @@ struct AdapterProblem {
 size_t adapter_workspace_bytes(int64_t T, int64_t K_in, int64_t K_out, int64_t n, int64_t r,
                                bool backward);
 tbn_status launch_adapter_fwd(const AdapterProblem& p, void* workspace, cudaStream_t s);
+// Its form for few tokens (tbn_adapter_small.cu).
+bool adapter_small_takes(const AdapterProblem& p);
+tbn_status launch_adapter_small(const AdapterProblem& p, cudaStream_t s);
 tbn_status launch_adapter_bwd(const AdapterProblem& p, void* workspace, cudaStream_t s);
 
 // AdamW over validated tensors (tbn_adamw.cu).
