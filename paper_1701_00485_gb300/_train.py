@@ -7,7 +7,9 @@ import struct
 
 import torch
 
-from . import TBN_F32, _check, _dt, _raw_stream, lib
+import paper_1701_00485_gb300 as _pkg
+
+from . import TBN_BF16, TBN_F32, _check, lib
 
 _OP_NORM_FWD, _OP_NORM_BWD, _OP_ADAPTER_FWD, _OP_ADAPTER_BWD = range(5, 9)
 _pack_norm_fwd = struct.Struct("=8qd6q").pack
@@ -39,59 +41,83 @@ class Adapters(ctypes.Structure):
                 ("ids", ctypes.c_void_p), ("ranks", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
 
 
-def _rows(t, name, shape=None):
-    """The row stride of a CUDA tensor [rows, D] whose rows are contiguous."""
-    if not t.is_cuda:
-        raise ValueError("%s must be a CUDA tensor" % name)
-    if t.dim() != 2 or (shape is not None and t.shape != shape):
-        raise ValueError("%s must be a 2-D tensor%s" % (
-            name, "" if shape is None else " of shape %s" % (tuple(shape),)))
-    ld, unit = t.stride()
-    if unit != 1 and t.shape[1] > 1:
-        raise ValueError("%s must have contiguous rows" % name)
-    # rows of one element, and single rows, may carry any stride
-    return ld if t.shape[0] > 1 else t.shape[1]
+# A decoding step's call takes a few microseconds on the GPU, so what its checks
+# cost counts: one look at each property of a tensor (40 to 100 ns each), and the
+# reason for a refusal only once there is one.
+_DTYPES = {torch.float32: TBN_F32, torch.bfloat16: TBN_BF16}
 
 
-def _flat(t, name, n, dtypes):
-    """The pointer of a contiguous CUDA tensor of n elements, 0 for None."""
+def _rows(t, name, shape):
+    """The row stride of a CUDA tensor of this 2-D shape whose rows are contiguous."""
+    ld, unit = t.stride() if t.dim() == 2 else (0, 0)
+    if t.shape != shape or not t.is_cuda or (unit != 1 and shape[1] > 1):
+        raise ValueError("%s must be a CUDA tensor of shape %s with contiguous rows" % (
+            name, tuple(shape)))
+    # single rows may carry any stride
+    return ld if shape[0] > 1 else shape[1]
+
+
+def _matrix(t, name):
+    """Shape, row stride and dtype code of a 2-D CUDA tensor with contiguous rows."""
+    if t.dim() != 2:
+        raise ValueError("%s must be a 2-D tensor" % name)
+    shape = t.shape
+    return shape, _rows(t, name, shape), _code(t, name)
+
+
+def _code(t, name):
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+    return dt
+
+
+def _flat(t, name, n, dtype):
+    """The pointer of a contiguous CUDA tensor of n elements of dtype, 0 for None."""
     if t is None:
         return 0
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous CUDA tensor" % name)
-    if t.numel() != n or t.dtype not in dtypes:
-        raise ValueError("%s must have %d elements of %s" % (
-            name, n, " or ".join(str(d) for d in dtypes)))
-    return t.data_ptr()
+    if t.dtype is dtype and t.numel() == n and t.is_contiguous() and t.is_cuda:
+        return t.data_ptr()
+    raise ValueError("%s must be a contiguous CUDA tensor of %d elements of %s" % (name, n, dtype))
 
 
-_F32 = (torch.float32,)
-_FLOATS = (torch.float32, torch.bfloat16)
-_BF16 = (torch.bfloat16,)
-_I32 = (torch.int32,)
+_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
 
 
 def _weights(gamma, beta, D):
-    if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
-        raise ValueError("gamma and beta must have the same dtype")
-    w = gamma if gamma is not None else beta
-    return (_flat(gamma, "gamma", D, _FLOATS), _flat(beta, "beta", D, _FLOATS),
-            TBN_F32 if w is None else _dt(w))
+    """Pointers of gamma and beta (either type, both the same) and its code."""
+    w = beta if gamma is None else gamma
+    if w is None:
+        return 0, 0, TBN_F32
+    dt = w.dtype if w.dtype is _BF16 else _F32
+    return _flat(gamma, "gamma", D, dt), _flat(beta, "beta", D, dt), _DTYPES[dt]
+
+
+def _stream_of(t, stream):
+    """The cudaStream_t of `stream`, or of the current stream of t's device."""
+    if stream is not None:
+        return stream.cuda_stream
+    raw = _pkg._current_raw_stream
+    return raw(t.get_device()) if raw is not None else torch.cuda.current_stream(t.device).cuda_stream
 
 
 def _bytes(t, name):
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous CUDA tensor" % name)
-    return t.numel() * t.element_size()
+    if t.is_cuda and t.is_contiguous():
+        return t.nbytes
+    raise ValueError("%s must be a contiguous CUDA tensor" % name)
+
+
+def _empty(shape, dtype, device, stream):
+    """A tensor for a call on `stream`, from that stream's memory: what the current
+    stream's allocator hands out may still be in use by work queued there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _scratch(nbytes, device, stream):
-    """A workspace for one call; on another stream than the current one its
-    memory is not handed out again before that stream's work is done."""
-    t = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-    if stream is not None:
-        t.record_stream(stream)
-    return t
+    return _empty(max(nbytes, 256), torch.uint8, device, stream)
 
 
 def tbn_layernorm_fwd(x, gamma=None, beta=None, eps: float = 1e-5, out_dtype=None, out=None,
@@ -101,19 +127,19 @@ def tbn_layernorm_fwd(x, gamma=None, beta=None, eps: float = 1e-5, out_dtype=Non
 
     Returns (y, mean, rstd); y has x's dtype or, with out_dtype or out, bf16;
     mean and rstd [rows] fp32 are what tbn_layernorm_bwd needs."""
-    ldx = _rows(x, "x")
-    rows, D = x.shape
+    shape, ldx, xdt = _matrix(x, "x")
+    rows, D = shape
     g, b, wdt = _weights(gamma, beta, D)
     if out is None:
-        out = torch.empty((rows, D), dtype=out_dtype or x.dtype, device=x.device)
+        out = _empty((rows, D), out_dtype or x.dtype, x.device, stream)
     if mean is None:
-        mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+        mean = _empty(rows, _F32, x.device, stream)
     if rstd is None:
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    ldy = _rows(out, "out", x.shape)
+        rstd = _empty(rows, _F32, x.device, stream)
     _call_packed(_OP_NORM_FWD, "tbn_layernorm_fwd", _pack_norm_fwd(
-        x.data_ptr(), _dt(x), rows, D, ldx, g, b, wdt, eps, out.data_ptr(), _dt(out), ldy,
-        _flat(mean, "mean", rows, _F32), _flat(rstd, "rstd", rows, _F32), _raw_stream(stream)))
+        x.data_ptr(), xdt, rows, D, ldx, g, b, wdt, eps, out.data_ptr(), _code(out, "out"),
+        _rows(out, "out", shape), _flat(mean, "mean", rows, _F32), _flat(rstd, "rstd", rows, _F32),
+        _stream_of(x, stream)))
     return out, mean, rstd
 
 
@@ -128,31 +154,32 @@ def tbn_layernorm_bwd(dy, x, mean, rstd, gamma=None, dres=None, dx=None, dgamma=
     dx has x's dtype and is added to dres, the gradient of a residual branch
     around the norm, where one is given.  Returns (dx, dgamma, dbeta), the last
     two fp32 [D], or None without weight_grads."""
-    ldx, lddy = _rows(x, "x"), _rows(dy, "dy", x.shape)
-    rows, D = x.shape
+    shape, ldx, xdt = _matrix(x, "x")
+    lddy = _rows(dy, "dy", shape)
+    rows, D = shape
     g, _, wdt = _weights(gamma, None, D)
     if dx is None:
-        dx = torch.empty((rows, D), dtype=x.dtype, device=x.device)
+        dx = _empty((rows, D), x.dtype, x.device, stream)
     if weight_grads:
         if dgamma is None:
-            dgamma = torch.empty(D, dtype=torch.float32, device=x.device)
+            dgamma = _empty(D, _F32, x.device, stream)
         if dbeta is None:
-            dbeta = torch.empty(D, dtype=torch.float32, device=x.device)
+            dbeta = _empty(D, _F32, x.device, stream)
         if workspace is None:
             workspace = _scratch(tbn_layernorm_bwd_workspace_bytes(rows, D), x.device, stream)
         nws = _bytes(workspace, "workspace")
     else:
         dgamma = dbeta = workspace = None
         nws = 0
-    if dx.dtype != x.dtype or (dres is not None and dres.dtype != x.dtype):
+    if dx.dtype is not x.dtype or (dres is not None and dres.dtype is not x.dtype):
         raise ValueError("dx and dres must have x's dtype")
-    lddres = 0 if dres is None else _rows(dres, "dres", x.shape)
+    lddres = 0 if dres is None else _rows(dres, "dres", shape)
     _call_packed(_OP_NORM_BWD, "tbn_layernorm_bwd", _pack_norm_bwd(
-        dy.data_ptr(), _dt(dy), lddy, x.data_ptr(), _dt(x), rows, D, ldx,
+        dy.data_ptr(), _code(dy, "dy"), lddy, x.data_ptr(), xdt, rows, D, ldx,
         _flat(mean, "mean", rows, _F32), _flat(rstd, "rstd", rows, _F32), g, wdt,
-        0 if dres is None else dres.data_ptr(), lddres, dx.data_ptr(), _rows(dx, "dx", x.shape),
+        0 if dres is None else dres.data_ptr(), lddres, dx.data_ptr(), _rows(dx, "dx", shape),
         _flat(dgamma, "dgamma", D, _F32), _flat(dbeta, "dbeta", D, _F32),
-        0 if workspace is None else workspace.data_ptr(), nws, _raw_stream(stream)))
+        0 if workspace is None else workspace.data_ptr(), nws, _stream_of(x, stream)))
     return dx, dgamma, dbeta
 
 
@@ -185,16 +212,16 @@ class AdamWPlan:
             p, size = params[i], params[i].numel()
             eight = m[i].dtype == torch.float8_e4m3fn
             blocks = -(-size // _ADAMW_BLOCK)
-            t.param = _flat(p, "params[%d]" % i, size, _FLOATS)
-            t.m = _flat(m[i], "m[%d]" % i, size, (torch.float8_e4m3fn,) if eight else _F32)
-            t.v = _flat(v[i], "v[%d]" % i, size, (torch.float8_e5m2,) if eight else _F32)
+            t.param_dtype = _code(p, "params[%d]" % i)
+            t.param = _flat(p, "params[%d]" % i, size, p.dtype)
+            t.m = _flat(m[i], "m[%d]" % i, size, torch.float8_e4m3fn if eight else _F32)
+            t.v = _flat(v[i], "v[%d]" % i, size, torch.float8_e5m2 if eight else _F32)
             if eight and (m_scale[i] is None or v_scale[i] is None):
                 raise ValueError("8-bit moments need m_scale and v_scale")
             t.m_scale = _flat(m_scale[i], "m_scale[%d]" % i, blocks, _F32) if eight else 0
             t.v_scale = _flat(v_scale[i], "v_scale[%d]" % i, blocks, _F32) if eight else 0
-            t.copy = _flat(copies[i], "copies[%d]" % i, size, (torch.bfloat16,))
+            t.copy = _flat(copies[i], "copies[%d]" % i, size, _BF16)
             t.n, t.weight_decay, t.lr_scale = size, decay[i], lrs[i]
-            t.param_dtype = _dt(p)
             t.state = _STATE_8BIT if eight else _STATE_32BIT
         self._hyper = AdamWHyper()
         self.set_grads(grads)
@@ -212,7 +239,8 @@ class AdamWPlan:
         if len(grads) != self.count:
             raise ValueError("lists of %d tensors are needed" % self.count)
         for i, (t, g) in enumerate(zip(self._array, grads)):
-            t.grad, t.grad_dtype = _flat(g, "grads[%d]" % i, t.n, _FLOATS), _dt(g)
+            t.grad_dtype = _code(g, "grads[%d]" % i)
+            t.grad = _flat(g, "grads[%d]" % i, t.n, g.dtype)
         self.grads = list(grads)
 
 
@@ -227,8 +255,9 @@ def tbn_adamw_step(plan: AdamWPlan, step: int, lr: float, betas=(0.9, 0.999), ep
     h.lr, (h.beta1, h.beta2), h.eps, h.step = lr, betas, eps, step
     h.grad_scale = _flat(grad_scale, "grad_scale", 1, _F32)
     h.seed = seed & 0xFFFFFFFF
-    _check(lib().tbn_adamw_step(plan._array, plan.count, ctypes.byref(h), _raw_stream(stream)),
-           "tbn_adamw_step")
+    like = plan.tensors[0][0] if plan.count else None
+    s = 0 if like is None else _stream_of(like, stream)
+    _check(lib().tbn_adamw_step(plan._array, plan.count, ctypes.byref(h), s), "tbn_adamw_step")
 
 
 def tbn_adapter_workspace_bytes(T: int, K_in: int, K_out: int, n: int, r: int,
@@ -239,20 +268,22 @@ def tbn_adapter_workspace_bytes(T: int, K_in: int, K_out: int, n: int, r: int,
 
 def _adapters(a, b, T, ids, scale, ranks):
     """The first nine arguments of a packed adapter call."""
-    if a.dim() != 3 or b.dim() != 3 or a.shape[:2] != b.shape[:2]:
+    sa, sb = a.shape, b.shape
+    if len(sa) != 3 or len(sb) != 3 or sa[:2] != sb[:2]:
         raise ValueError("a must be [n, r, K_in] and b [n, r, K_out]")
-    n, r, K_in = a.shape
-    return (_flat(a, "a", n * r * K_in, _BF16), _flat(b, "b", b.numel(), _BF16), n, r, K_in,
-            b.shape[2], _flat(ids, "ids", T, _I32), _flat(ranks, "ranks", n, _I32),
-            _flat(scale, "scale", n, _F32))
+    n, r, K_in = sa
+    K_out = sb[2]
+    return (_flat(a, "a", n * r * K_in, _BF16), _flat(b, "b", n * r * K_out, _BF16), n, r, K_in, K_out,
+            _flat(ids, "ids", T, _I32), _flat(ranks, "ranks", n, _I32), _flat(scale, "scale", n, _F32))
 
 
-def _base(base, like, name):
+def _base(base, like, shape, name):
+    """Pointer and row stride of the tensor added to `like`, of its dtype and shape."""
     if base is None:
         return 0, 0
-    if base.dtype != like.dtype:
+    if base.dtype is not like.dtype:
         raise ValueError("base must have %s's dtype" % name)
-    return base.data_ptr(), _rows(base, "base", like.shape)
+    return base.data_ptr(), _rows(base, "base", shape)
 
 
 def tbn_adapter_fwd(x, a, b, ids=None, scale=None, ranks=None, base=None, out_dtype=None,
@@ -267,22 +298,22 @@ def tbn_adapter_fwd(x, a, b, ids=None, scale=None, ranks=None, base=None, out_dt
     them is not read); base [T, K_out] of y's dtype, the shared projection's
     output, which `out` may be.  v: None, or fp32 [T, r] that receives a_i x_t
     for tbn_adapter_bwd.  y has base's, out's, out_dtype's or x's dtype."""
-    ldx = _rows(x, "x")
-    T = x.shape[0]
+    shape, ldx, xdt = _matrix(x, "x")
+    T = shape[0]
     ad = _adapters(a, b, T, ids, scale, ranks)
-    if x.shape[1] != ad[4]:
-        raise ValueError("x has %d columns, a expects %d" % (x.shape[1], ad[4]))
+    if shape[1] != ad[4]:
+        raise ValueError("x has %d columns, a expects %d" % (shape[1], ad[4]))
     if out is None:
         dt = out_dtype or (x if base is None else base).dtype
-        out = torch.empty((T, ad[5]), dtype=dt, device=x.device)
+        out = _empty((T, ad[5]), dt, x.device, stream)
     if workspace is None:
         workspace = _scratch(tbn_adapter_workspace_bytes(T, ad[4], ad[5], ad[2], ad[3]), x.device,
                              stream)
-    ldy = _rows(out, "out", (T, ad[5]))
+    shape = (T, ad[5])
     _call_packed(_OP_ADAPTER_FWD, "tbn_adapter_fwd", _pack_adapter_fwd(
-        *ad, x.data_ptr(), _dt(x), T, ldx, *_base(base, out, "y"), out.data_ptr(), _dt(out), ldy,
-        _flat(v, "v", T * ad[3], _F32), workspace.data_ptr(), _bytes(workspace, "workspace"),
-        _raw_stream(stream)))
+        *ad, x.data_ptr(), xdt, T, ldx, *_base(base, out, shape, "y"), out.data_ptr(),
+        _code(out, "out"), _rows(out, "out", shape), _flat(v, "v", T * ad[3], _F32),
+        workspace.data_ptr(), _bytes(workspace, "workspace"), _stream_of(x, stream)))
     return out
 
 
@@ -295,38 +326,39 @@ def tbn_adapter_bwd(dy, x, a, b, ids=None, scale=None, ranks=None, v=None, base=
     b's shape, zero past an adapter's rank and for adapters without tokens.  v:
     what tbn_adapter_fwd wrote, or None to compute it again.  need: which of the
     three are wanted; the others come back as None."""
-    ldx, lddy = _rows(x, "x"), _rows(dy, "dy")
-    T = x.shape[0]
+    shape, ldx, xdt = _matrix(x, "x")
+    T = shape[0]
     ad = _adapters(a, b, T, ids, scale, ranks)
-    if x.shape[1] != ad[4] or tuple(dy.shape) != (T, ad[5]):
-        raise ValueError("x must be [T, K_in] and dy [T, K_out] of a and b")
+    if shape[1] != ad[4]:
+        raise ValueError("x has %d columns, a expects %d" % (shape[1], ad[4]))
+    lddy = _rows(dy, "dy", (T, ad[5]))
     if not need[0]:
         dx = None
     elif dx is None:
-        dx = torch.empty((T, ad[4]), dtype=x.dtype, device=x.device)
-    elif dx.dtype != x.dtype:
+        dx = _empty((T, ad[4]), x.dtype, x.device, stream)
+    elif dx.dtype is not x.dtype:
         raise ValueError("dx must have x's dtype")
     if not need[1]:
         da = None
     elif da is None:
-        da = torch.empty(a.shape, dtype=torch.float32, device=x.device)
+        da = _empty(a.shape, _F32, x.device, stream)
     if not need[2]:
         db = None
     elif db is None:
-        db = torch.empty(b.shape, dtype=torch.float32, device=x.device)
+        db = _empty(b.shape, _F32, x.device, stream)
     if workspace is None:
         workspace = _scratch(tbn_adapter_workspace_bytes(T, ad[4], ad[5], ad[2], ad[3], True),
                              x.device, stream)
     _call_packed(_OP_ADAPTER_BWD, "tbn_adapter_bwd", _pack_adapter_bwd(
-        *ad, dy.data_ptr(), _dt(dy), lddy, x.data_ptr(), _dt(x), T, ldx,
-        _flat(v, "v", T * ad[3], _F32), *(_base(base, x, "x") if dx is not None else (0, 0)),
-        0 if dx is None else dx.data_ptr(), 0 if dx is None else _rows(dx, "dx", x.shape),
+        *ad, dy.data_ptr(), _code(dy, "dy"), lddy, x.data_ptr(), xdt, T, ldx,
+        _flat(v, "v", T * ad[3], _F32), *(_base(base, x, shape, "x") if dx is not None else (0, 0)),
+        0 if dx is None else dx.data_ptr(), 0 if dx is None else _rows(dx, "dx", shape),
         _flat(da, "da", a.numel(), _F32), _flat(db, "db", b.numel(), _F32), workspace.data_ptr(),
-        _bytes(workspace, "workspace"), _raw_stream(stream)))
+        _bytes(workspace, "workspace"), _stream_of(x, stream)))
     return dx, da, db
 
 
 def _call_packed(op, where, block):
-    status = lib().tbn_packed_call(op, block)
+    status = (_pkg._lib or lib()).tbn_packed_call(op, block)
     if status != 0:
         _check(status, where)
