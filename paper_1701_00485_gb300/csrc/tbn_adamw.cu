@@ -55,6 +55,7 @@ struct Tensor {
 
 struct Hyper {
   float beta1, one_beta1, beta2, one_beta2, root_fix2, eps;
+  float one;               // 1, which the compiler does not know
   const float* grad_scale;
   uint32_t salt;
   int count;
@@ -75,45 +76,53 @@ __device__ __forceinline__ uint32_t random_bits(uint32_t salt, uint32_t i) {
   return h ^ (h >> 16);
 }
 
+// Eight consecutive values as four pairs.
+using Eight = uint64_t[kLane / 2];
+
+__device__ __forceinline__ float get(const Eight& v, int i) {
+  return __uint_as_float(static_cast<uint32_t>(v[i / 2] >> (32 * (i % 2))));
+}
+__device__ __forceinline__ uint64_t both(float f) { return f32x2(__float_as_uint(f), __float_as_uint(f)); }
+
 __device__ __forceinline__ void load8(const void* base, bool bf16, bool aligned, int64_t at,
-                                      int there, float (&v)[kLane]) {
+                                      int there, Eight& v) {
   if (aligned && there == kLane) {
     if (bf16) {
       const uint4 r = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) + at);
       const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-      }
-    } else {
-      const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
-      const float4 a = f[0], b = f[1];
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+      for (int i = 0; i < 4; ++i) v[i] = f32x2(w[i] << 16, w[i] & 0xFFFF0000u);
+    } else {   // a sector
+      asm volatile("ld.global.v4.b64 {%0, %1, %2, %3}, [%4];"
+                   : "=l"(v[0]), "=l"(v[1]), "=l"(v[2]), "=l"(v[3])
+                   : "l"(static_cast<const float*>(base) + at)
+                   : "memory");
     }
     return;
   }
 #pragma unroll
-  for (int i = 0; i < kLane; ++i) {
-    v[i] = 0.0f;
-    if (i < there)
-      v[i] = bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(base)[at + i])
-                  : static_cast<const float*>(base)[at + i];
+  for (int i = 0; i < kLane; i += 2) {
+    float f[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (i + j < there)
+        f[j] = bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(base)[at + i + j])
+                    : static_cast<const float*>(base)[at + i + j];
+    v[i / 2] = f32x2(__float_as_uint(f[0]), __float_as_uint(f[1]));
   }
 }
 
 __device__ __forceinline__ void store8(void* base, bool bf16, bool aligned, int64_t at, int there,
-                                       const float (&v)[kLane]) {
+                                       const Eight& v) {
   if (aligned && there == kLane) {
     if (bf16) {
       *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(base) + at) =
-          make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                     pack_bf16x2(v[6], v[7]));
+          make_uint4(pack_bf16x2(get(v, 0), get(v, 1)), pack_bf16x2(get(v, 2), get(v, 3)),
+                     pack_bf16x2(get(v, 4), get(v, 5)), pack_bf16x2(get(v, 6), get(v, 7)));
     } else {
-      float4* f = reinterpret_cast<float4*>(static_cast<float*>(base) + at);
-      f[0] = make_float4(v[0], v[1], v[2], v[3]);
-      f[1] = make_float4(v[4], v[5], v[6], v[7]);
+      asm volatile("st.global.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(static_cast<float*>(base) + at),
+                   "l"(v[0]), "l"(v[1]), "l"(v[2]), "l"(v[3])
+                   : "memory");
     }
     return;
   }
@@ -121,9 +130,9 @@ __device__ __forceinline__ void store8(void* base, bool bf16, bool aligned, int6
   for (int i = 0; i < kLane; ++i)
     if (i < there) {
       if (bf16)
-        static_cast<__nv_bfloat16*>(base)[at + i] = __float2bfloat16_rn(v[i]);
+        static_cast<__nv_bfloat16*>(base)[at + i] = __float2bfloat16_rn(get(v, i));
       else
-        static_cast<float*>(base)[at + i] = v[i];
+        static_cast<float*>(base)[at + i] = get(v, i);
     }
 }
 
@@ -151,15 +160,15 @@ __device__ __forceinline__ void store_codes(void* base, bool aligned, int64_t at
 
 // Eight codes of a block to values: code * scale.
 template <__nv_fp8_interpretation_t kFormat>
-__device__ __forceinline__ void decode(uint2 codes, float scale, float (&v)[kLane]) {
+__device__ __forceinline__ void decode(uint2 codes, float scale, Eight& v) {
   const uint32_t w[2] = {codes.x, codes.y};
+  const uint64_t by = both(scale);
 #pragma unroll
   for (int i = 0; i < kLane / 2; ++i) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(
         static_cast<__nv_fp8x2_storage_t>(w[i / 2] >> (16 * (i % 2))), kFormat);
     const float2 f = __half22float2(__half2(h));
-    v[2 * i] = f.x * scale;
-    v[2 * i + 1] = f.y * scale;
+    v[i] = mul_f32x2(f32x2(__float_as_uint(f.x), __float_as_uint(f.y)), by);
   }
 }
 
@@ -176,14 +185,52 @@ __device__ __forceinline__ uint32_t finite_bits(float v) {
   return b < 0x7F800000u ? b : 0u;
 }
 
-// |v| / scale in a format of exponent bias kBias and 23 - kDrop mantissa bits,
-// rounded at random: the multiplication by 2^(kBias - 127) brings the format's
-// exponent field, subnormal numbers included, to that of the 32-bit number,
-// whose kDrop low bits and as many random ones then carry or do not.
-template <int kBias, int kDrop>
-__device__ __forceinline__ uint32_t encode(float v, float inv_scale, uint32_t random16) {
-  const float u = fabsf(v) * inv_scale * __uint_as_float(static_cast<uint32_t>(kBias) << 23);
-  return (__float_as_uint(u) + (random16 << (kDrop - 16))) >> kDrop;
+// Eight |v| / scale in a format of exponent bias kBias and 23 - kDrop mantissa
+// bits, rounded at random: the multiplication by 2^(kBias - 127) brings the
+// format's exponent field, subnormal numbers included, to that of the 32-bit
+// number, whose kDrop low bits and as many random ones then carry or do not.
+// kRare: what is not finite, and scales so large that the two powers of two are
+// not one (where they are, the product is the same).
+template <int kBias, int kDrop, bool kRare>
+__device__ __forceinline__ uint32_t encode(float v, int field, uint32_t random) {
+  float u;
+  if constexpr (kRare)
+    u = fabsf(v) * __uint_as_float(static_cast<uint32_t>(254 - field) << 23) *
+        __uint_as_float(static_cast<uint32_t>(kBias) << 23);
+  else
+    u = fabsf(v) * __uint_as_float(static_cast<uint32_t>(127 + kBias - field) << 23);
+  return (__float_as_uint(u) + random) >> kDrop;
+}
+
+template <bool kRare>
+__device__ __forceinline__ void encode8(const Eight& m, const Eight& v, int mf, int vf, uint32_t salt,
+                                        uint32_t first, uint32_t (&mw)[2], uint32_t (&vw)[2]) {
+#pragma unroll
+  for (int i = 0; i < kLane; ++i) {
+    const uint32_t r = random_bits(salt, first + i);
+    const float mi = get(m, i), vi = get(v, i);
+    uint32_t mc = encode<7, 20, kRare>(mi, mf, (r >> 12) & 0xFFFF0u);
+    uint32_t vc = encode<15, 21, kRare>(vi, vf, (r << 5) & 0x1FFFE0u);
+    vc = max(vc, min(__float_as_uint(vi), 1u));   // v >= 0: only 0 is stored as 0
+    if constexpr (kRare) {
+      if (!(fabsf(mi) < INFINITY)) mc = 0x7Fu;
+      if (!(vi < INFINITY)) vc = vi > 0.0f ? 0x7Cu : 0x7Fu;   // infinity, NaN
+    }
+    mc |= (__float_as_uint(mi) >> 24) & 0x80u;
+    mw[i / 4] |= mc << (8 * (i % 4));
+    vw[i / 4] |= vc << (8 * (i % 4));
+  }
+}
+
+__device__ __forceinline__ float sqrt_approx(float v) {   // 2 units of the last place
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float rcp_approx(float v) {    // 1 unit
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
 }
 
 template <int N>
@@ -205,25 +252,36 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
   const bool al = t.flags & kAligned;
   grid_dependency_wait();
   grid_dependents_launch();
-  float p[kLane], g[kLane], m[kLane], v[kLane];
+  Eight p, g, m, v;
   load8(t.g, g16, al, at, there, g);
   load8(t.p, p16, al, at, there, p);
   if (s8) {
-    decode<__NV_E4M3>(load_codes(t.m, al, at, there), t.m_scale[block], m);
-    decode<__NV_E5M2>(load_codes(t.v, al, at, there), t.v_scale[block], v);
+    const uint2 mc = load_codes(t.m, al, at, there), vc = load_codes(t.v, al, at, there);
+    const float ms = t.m_scale[block], vs = t.v_scale[block];
+    decode<__NV_E4M3>(mc, ms, m);
+    decode<__NV_E5M2>(vc, vs, v);
   } else {
     load8(t.m, false, al, at, there, m);
     load8(t.v, false, al, at, there, v);
   }
-  const float gs = b.h.grad_scale != nullptr ? *b.h.grad_scale : 1.0f;
+  const uint64_t gs = both(b.h.grad_scale != nullptr ? *b.h.grad_scale : 1.0f);
 #pragma unroll
-  for (int i = 0; i < kLane; ++i) {
-    // each operation rounded by itself, as the definition has them
-    const float gi = __fmul_rn(g[i], gs);
-    m[i] = __fadd_rn(__fmul_rn(b.h.beta1, m[i]), __fmul_rn(b.h.one_beta1, gi));
-    v[i] = __fadd_rn(__fmul_rn(b.h.beta2, v[i]), __fmul_rn(__fmul_rn(b.h.one_beta2, gi), gi));
-    const float den = sqrtf(v[i]) * b.h.root_fix2 + b.h.eps;
-    p[i] = p[i] * t.decay - t.lr * (m[i] / den);
+  for (int i = 0; i < kLane / 2; ++i) {
+    // the moments' operations each rounded by itself, as the definition has them;
+    // a + b is written a * one + b, since a pair's product and addition are fused
+    // by the assembler although both ask for their own rounding
+    const uint64_t gi = mul_f32x2(g[i], gs);
+    m[i] = fma_f32x2(mul_f32x2(both(b.h.beta1), m[i]), both(b.h.one),
+                     mul_f32x2(both(b.h.one_beta1), gi));
+    v[i] = fma_f32x2(mul_f32x2(both(b.h.beta2), v[i]), both(b.h.one),
+                     mul_f32x2(mul_f32x2(both(b.h.one_beta2), gi), gi));
+    // the step's own roundings (2^-22 of it at most) do not reach p's last place
+    float step[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      step[j] = -t.lr * (get(m, 2 * i + j) *
+                         rcp_approx(fmaf(sqrt_approx(get(v, 2 * i + j)), b.h.root_fix2, b.h.eps)));
+    p[i] = fma_f32x2(p[i], both(t.decay), f32x2(__float_as_uint(step[0]), __float_as_uint(step[1])));
   }
   store8(t.p, p16, al, at, there, p);
   if (t.copy != nullptr) store8(t.copy, true, al, at, there, p);
@@ -232,30 +290,30 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     store8(t.v, false, al, at, there, v);
     return;
   }
+  // elements past the tensor's end are zeros: they ask for no scale
   uint32_t m_most = 0u, v_most = 0u;
 #pragma unroll
-  for (int i = 0; i < kLane; ++i)
-    if (i < there) {
-      m_most = max(m_most, finite_bits(m[i]));
-      v_most = max(v_most, finite_bits(v[i]));
-    }
+  for (int i = 0; i < kLane; ++i) {
+    m_most = max(m_most, __float_as_uint(get(m, i)) & 0x7FFFFFFFu);
+    v_most = max(v_most, __float_as_uint(get(v, i)) & 0x7FFFFFFFu);
+  }
   m_most = __reduce_max_sync(0xffffffffu, m_most);
   v_most = __reduce_max_sync(0xffffffffu, v_most);
-  const int mf = scale_field<8>(m_most), vf = scale_field<15>(v_most);
-  const float m_inv = __uint_as_float(static_cast<uint32_t>(254 - mf) << 23);
-  const float v_inv = __uint_as_float(static_cast<uint32_t>(254 - vf) << 23);
+  int mf = scale_field<8>(m_most), vf = scale_field<15>(v_most);
+  const uint32_t first = t.first_random + static_cast<uint32_t>(at);
   uint32_t mw[2] = {0u, 0u}, vw[2] = {0u, 0u};
+  if (max(m_most, v_most) < 0x7F800000u && mf < 127 + 7 && vf < 127 + 15) {
+    encode8<false>(m, v, mf, vf, b.h.salt, first, mw, vw);
+  } else {
+    m_most = v_most = 0u;   // of the finite ones
 #pragma unroll
-  for (int i = 0; i < kLane; ++i) {
-    const uint32_t r = random_bits(b.h.salt, t.first_random + static_cast<uint32_t>(at) + i);
-    uint32_t mc = encode<7, 20>(m[i], m_inv, r >> 16);
-    uint32_t vc = encode<15, 21>(v[i], v_inv, r & 0xFFFFu);
-    if (vc == 0u && v[i] > 0.0f) vc = 1u;
-    if (!(fabsf(m[i]) < INFINITY)) mc = 0x7Fu;
-    if (!(v[i] < INFINITY)) vc = v[i] > 0.0f ? 0x7Cu : 0x7Fu;   // infinity, NaN
-    mc |= (__float_as_uint(m[i]) >> 24) & 0x80u;
-    mw[i / 4] |= mc << (8 * (i % 4));
-    vw[i / 4] |= vc << (8 * (i % 4));
+    for (int i = 0; i < kLane; ++i) {
+      m_most = max(m_most, finite_bits(get(m, i)));
+      v_most = max(v_most, finite_bits(get(v, i)));
+    }
+    mf = scale_field<8>(__reduce_max_sync(0xffffffffu, m_most));
+    vf = scale_field<15>(__reduce_max_sync(0xffffffffu, v_most));
+    encode8<true>(m, v, mf, vf, b.h.salt, first, mw, vw);
   }
   store_codes(t.m, al, at, there, mw);
   store_codes(t.v, al, at, there, vw);
@@ -301,6 +359,7 @@ tbn_status launch_adamw(const tbn_adamw_tensor* tensors, int count, const tbn_ad
   b.h.one_beta2 = static_cast<float>(1.0 - h.beta2);
   b.h.root_fix2 = static_cast<float>(1.0 / std::sqrt(fix2));
   b.h.eps = static_cast<float>(h.eps);
+  b.h.one = 1.0f;
   b.h.grad_scale = h.grad_scale;
   b.h.salt = h.seed * 0x9E3779B9u;
   b.h.count = 0;
@@ -320,8 +379,9 @@ tbn_status launch_adamw(const tbn_adamw_tensor* tensors, int count, const tbn_ad
     }
     chunks += mine;
     const bool state8 = t.state == TBN_ADAMW_STATE_8BIT;
-    const size_t state_align = state8 ? 8 : 16;
-    const bool al = is_aligned(t.param, 16) && is_aligned(t.grad, 16) &&
+    const size_t state_align = state8 ? 8 : 32;
+    const bool al = is_aligned(t.param, t.param_dtype == TBN_BF16 ? 16 : 32) &&
+                    is_aligned(t.grad, t.grad_dtype == TBN_BF16 ? 16 : 32) &&
                     is_aligned(t.m, state_align) && is_aligned(t.v, state_align) &&
                     is_aligned(t.copy, 16);
     Tensor& d = b.t[b.h.count];
