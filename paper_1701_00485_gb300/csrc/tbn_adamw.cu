@@ -185,51 +185,73 @@ __device__ __forceinline__ uint32_t finite_bits(float v) {
   return b < 0x7F800000u ? b : 0u;
 }
 
-// Eight |v| / scale in a format of exponent bias kBias and 23 - kDrop mantissa
-// bits, rounded at random: the multiplication by 2^(kBias - 127) brings the
-// format's exponent field, subnormal numbers included, to that of the 32-bit
-// number, whose kDrop low bits and as many random ones then carry or do not.
-// kRare: what is not finite, and scales so large that the two powers of two are
-// not one (where they are, the product is the same).
+// |v| / scale in a format of exponent bias kBias and 23 - kDrop mantissa bits,
+// rounded at random: the multiplication by 2^(kBias - 127) brings the format's
+// exponent field, subnormal numbers included, to that of the 32-bit number, whose
+// kDrop low bits and 16 random ones above bit kDrop - 16 then carry or do not.
+// kRare: what is not finite, and scales
+// so large that the two powers of two are not one (where they are, the product is
+// the same).
 template <int kBias, int kDrop, bool kRare>
-__device__ __forceinline__ uint32_t encode(float v, int field, uint32_t random) {
+__device__ __forceinline__ uint32_t encode(float v, int field, uint32_t random16) {
   float u;
   if constexpr (kRare)
     u = fabsf(v) * __uint_as_float(static_cast<uint32_t>(254 - field) << 23) *
         __uint_as_float(static_cast<uint32_t>(kBias) << 23);
   else
     u = fabsf(v) * __uint_as_float(static_cast<uint32_t>(127 + kBias - field) << 23);
-  return (__float_as_uint(u) + random) >> kDrop;
+  return (__float_as_uint(u) + (random16 << (kDrop - 16))) >> kDrop;
+}
+
+// The lowest bytes of four words, and the highest.
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
 
 template <bool kRare>
 __device__ __forceinline__ void encode8(const Eight& m, const Eight& v, int mf, int vf, uint32_t salt,
                                         uint32_t first, uint32_t (&mw)[2], uint32_t (&vw)[2]) {
+  uint32_t mc[kLane], vc[kLane];
 #pragma unroll
   for (int i = 0; i < kLane; ++i) {
     const uint32_t r = random_bits(salt, first + i);
     const float mi = get(m, i), vi = get(v, i);
-    uint32_t mc = encode<7, 20, kRare>(mi, mf, (r >> 12) & 0xFFFF0u);
-    uint32_t vc = encode<15, 21, kRare>(vi, vf, (r << 5) & 0x1FFFE0u);
-    vc = max(vc, min(__float_as_uint(vi), 1u));   // v >= 0: only 0 is stored as 0
+    mc[i] = encode<7, 20, kRare>(mi, mf, r >> 16);
+    vc[i] = encode<15, 21, kRare>(vi, vf, r & 0xFFFFu);
     if constexpr (kRare) {
-      if (!(fabsf(mi) < INFINITY)) mc = 0x7Fu;
-      if (!(vi < INFINITY)) vc = vi > 0.0f ? 0x7Cu : 0x7Fu;   // infinity, NaN
+      if (vi > 0.0f) vc[i] = max(vc[i], 1u);   // only 0 is stored as 0
+      if (!(fabsf(mi) < INFINITY)) mc[i] = 0x7Fu;
+      if (!(vi < INFINITY)) vc[i] = vi > 0.0f ? 0x7Cu : 0x7Fu;   // infinity, NaN
     }
-    mc |= (__float_as_uint(mi) >> 24) & 0x80u;
-    mw[i / 4] |= mc << (8 * (i % 4));
-    vw[i / 4] |= vc << (8 * (i % 4));
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const auto bits = [&](int i) { return __float_as_uint(get(m, 4 * h + i)); };
+    mw[h] = low_bytes(mc[4 * h], mc[4 * h + 1], mc[4 * h + 2], mc[4 * h + 3]) |
+            (top_bytes(bits(0), bits(1), bits(2), bits(3)) & 0x80808080u);
+    vw[h] = low_bytes(vc[4 * h], vc[4 * h + 1], vc[4 * h + 2], vc[4 * h + 3]);
   }
 }
 
-__device__ __forceinline__ float sqrt_approx(float v) {   // 2 units of the last place
+// The root and the reciprocal of the step, within two units of the last place;
+// subnormal arguments count as zero, which the caller excludes.
+__device__ __forceinline__ float sqrt_approx(float v) {
   float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
-__device__ __forceinline__ float rcp_approx(float v) {    // 1 unit
+__device__ __forceinline__ float rcp_approx(float v) {
   float r;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+// The larger one; NaN where either is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
 
@@ -275,13 +297,15 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
                      mul_f32x2(both(b.h.one_beta1), gi));
     v[i] = fma_f32x2(mul_f32x2(both(b.h.beta2), v[i]), both(b.h.one),
                      mul_f32x2(mul_f32x2(both(b.h.one_beta2), gi), gi));
-    // the step's own roundings (2^-22 of it at most) do not reach p's last place
-    float step[2];
+    // the step's own roundings (2^-22 of it at most) do not reach p's last place;
+    // v below 2^-126 counts as that
+    uint32_t step[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-      step[j] = -t.lr * (get(m, 2 * i + j) *
-                         rcp_approx(fmaf(sqrt_approx(get(v, 2 * i + j)), b.h.root_fix2, b.h.eps)));
-    p[i] = fma_f32x2(p[i], both(t.decay), f32x2(__float_as_uint(step[0]), __float_as_uint(step[1])));
+    for (int j = 0; j < 2; ++j) {
+      const float root = sqrt_approx(max_nan(get(v, 2 * i + j), 1.17549435e-38f));
+      step[j] = __float_as_uint(get(m, 2 * i + j) * rcp_approx(fmaf(root, b.h.root_fix2, b.h.eps)));
+    }
+    p[i] = fma_f32x2(f32x2(step[0], step[1]), both(-t.lr), mul_f32x2(p[i], both(t.decay)));
   }
   store8(t.p, p16, al, at, there, p);
   if (t.copy != nullptr) store8(t.copy, true, al, at, there, p);
@@ -291,28 +315,32 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     return;
   }
   // elements past the tensor's end are zeros: they ask for no scale
-  uint32_t m_most = 0u, v_most = 0u;
+  float m_top = 0.0f, v_top = 0.0f, v_low = INFINITY;
 #pragma unroll
   for (int i = 0; i < kLane; ++i) {
-    m_most = max(m_most, __float_as_uint(get(m, i)) & 0x7FFFFFFFu);
-    v_most = max(v_most, __float_as_uint(get(v, i)) & 0x7FFFFFFFu);
+    m_top = max_nan(m_top, fabsf(get(m, i)));
+    v_top = max_nan(v_top, get(v, i));
+    v_low = fminf(v_low, get(v, i));
   }
-  m_most = __reduce_max_sync(0xffffffffu, m_most);
-  v_most = __reduce_max_sync(0xffffffffu, v_most);
+  const uint32_t m_most = __reduce_max_sync(0xffffffffu, __float_as_uint(m_top) & 0x7FFFFFFFu);
+  const uint32_t v_most = __reduce_max_sync(0xffffffffu, __float_as_uint(v_top) & 0x7FFFFFFFu);
   int mf = scale_field<8>(m_most), vf = scale_field<15>(v_most);
   const uint32_t first = t.first_random + static_cast<uint32_t>(at);
-  uint32_t mw[2] = {0u, 0u}, vw[2] = {0u, 0u};
-  if (max(m_most, v_most) < 0x7F800000u && mf < 127 + 7 && vf < 127 + 15) {
+  uint32_t mw[2], vw[2];
+  // rare: not finite, scales beyond one power of two, v below the format's least
+  const bool common = max(m_most, v_most) < 0x7F800000u && mf < 127 + 7 && vf < 127 + 15 &&
+                      v_low >= __uint_as_float(static_cast<uint32_t>(vf) << 23) * 0x1p-16f;
+  if (__all_sync(0xffffffffu, common)) {
     encode8<false>(m, v, mf, vf, b.h.salt, first, mw, vw);
   } else {
-    m_most = v_most = 0u;   // of the finite ones
+    uint32_t m_fin = 0u, v_fin = 0u;   // of the finite ones
 #pragma unroll
     for (int i = 0; i < kLane; ++i) {
-      m_most = max(m_most, finite_bits(get(m, i)));
-      v_most = max(v_most, finite_bits(get(v, i)));
+      m_fin = max(m_fin, finite_bits(get(m, i)));
+      v_fin = max(v_fin, finite_bits(get(v, i)));
     }
-    mf = scale_field<8>(__reduce_max_sync(0xffffffffu, m_most));
-    vf = scale_field<15>(__reduce_max_sync(0xffffffffu, v_most));
+    mf = scale_field<8>(__reduce_max_sync(0xffffffffu, m_fin));
+    vf = scale_field<15>(__reduce_max_sync(0xffffffffu, v_fin));
     encode8<true>(m, v, mf, vf, b.h.salt, first, mw, vw);
   }
   store_codes(t.m, al, at, there, mw);
