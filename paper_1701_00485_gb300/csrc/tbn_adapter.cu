@@ -367,11 +367,16 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const ShrinkArgs a) {
       }
     }
   };
-  float acc[RP / 8][4];
+  // with several terms the leading one's sum is apart from the others': the tensor
+  // cores cut an addition's low bits off, each time it is added to
+  constexpr int kSums = kTerms > 1 ? 2 : 1;
+  float acc[kSums][RP / 8][4];
 #pragma unroll
-  for (int i = 0; i < RP / 8; ++i)
+  for (int q = 0; q < kSums; ++q)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = 0.0f;
+    for (int i = 0; i < RP / 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[q][i][j] = 0.0f;
   const int tg = 16 * (warp & 3), kh = warp >> 2, mi = lane >> 3, lr = lane & 7;
   load(c0);
   for (int c = c0; c < c1; ++c) {
@@ -399,11 +404,17 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const ShrinkArgs a) {
         ldsm4(af, sx + t * kHalf + tile_off(tg + 8 * (mi & 1) + lr, 2 * ks + (mi >> 1)));
 #pragma unroll
         for (int nt = 0; nt < RP / 16; ++nt) {
-          mma(acc[2 * nt], af, bf[nt][0], bf[nt][1]);
-          mma(acc[2 * nt + 1], af, bf[nt][2], bf[nt][3]);
+          mma(acc[t > 0 ? kSums - 1 : 0][2 * nt], af, bf[nt][0], bf[nt][1]);
+          mma(acc[t > 0 ? kSums - 1 : 0][2 * nt + 1], af, bf[nt][2], bf[nt][3]);
         }
       }
     }
+  }
+  if constexpr (kSums == 2) {
+#pragma unroll
+    for (int i = 0; i < RP / 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[0][i][j] += acc[1][i][j];
   }
   __syncthreads();
   float* sum = reinterpret_cast<float*>(smem);   // [64][RP]
@@ -413,7 +424,7 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const ShrinkArgs a) {
     for (int nt = 0; nt < RP / 8; ++nt)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        sum[(tg + g + 8 * (i >> 1)) * RP + 8 * nt + t2 + (i & 1)] = acc[nt][i];
+        sum[(tg + g + 8 * (i >> 1)) * RP + 8 * nt + t2 + (i & 1)] = acc[0][nt][i];
   }
   __syncthreads();
   if (kh == 0) {
@@ -424,7 +435,7 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const ShrinkArgs a) {
       for (int i = 0; i < 4; ++i) {
         const int m = tg + g + 8 * (i >> 1), col = 8 * nt + t2 + (i & 1);
         if (m < tile.z && col < a.ad.r)
-          part[static_cast<int64_t>(m) * a.ad.r + col] = acc[nt][i] + sum[m * RP + col];
+          part[static_cast<int64_t>(m) * a.ad.r + col] = acc[0][nt][i] + sum[m * RP + col];
       }
   }
 }
@@ -660,13 +671,14 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) load_piece(px[h], p, c0 + 64 * h + 16 * q, a.side.K, a.side.x_aligned);
   };
-  float acc[RP / 16][2][4];
+  // the leading terms' sum, and the others'
+  float acc[RP / 16][2][4], low[RP / 16][2][4];
 #pragma unroll
   for (int i = 0; i < RP / 16; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.0f;
+      for (int k = 0; k < 4; ++k) acc[i][j][k] = low[i][j][k] = 0.0f;
   const uint32_t su_s = smem_addr(su), sx_s = smem_addr(sx);
   load(0);
   for (int t0 = 0; t0 < item.z; t0 += kTile) {
@@ -704,8 +716,8 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
 #pragma unroll
           for (int t = 0; t < kTerms; ++t)
             if (tu + t <= 2) {   // what is left out is below 2^-24 of the product
-              mma(acc[mt][0], af, bf[t][0], bf[t][1]);
-              mma(acc[mt][1], af, bf[t][2], bf[t][3]);
+              mma(tu + t == 0 ? acc[mt][0] : low[mt][0], af, bf[t][0], bf[t][1]);
+              mma(tu + t == 0 ? acc[mt][1] : low[mt][1], af, bf[t][2], bf[t][3]);
             }
         }
     }
@@ -722,7 +734,8 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
       for (int i = 0; i < 4; ++i) {
         const int m = 16 * mt + g + 8 * (i >> 1), e = c0 + 16 * warp + 8 * nt + t2 + (i & 1);
         // rows past the adapter's rank are zero whatever x holds
-        if (m < r && e < a.side.K) out[static_cast<int64_t>(m) * a.side.K + e] = m < rank ? acc[mt][nt][i] : 0.0f;
+        if (m < r && e < a.side.K) out[static_cast<int64_t>(m) * a.side.K + e] =
+              m < rank ? acc[mt][nt][i] + low[mt][nt][i] : 0.0f;
       }
 }
 
@@ -836,7 +849,8 @@ __device__ __forceinline__ void store_32(void* p, const uint32_t* v) {
 }
 
 // ---- shrink: D[128 tokens][RP] over every splits-th chunk of K, both operands
-// K-major
+// K-major.  Two sums take the chunks in turn: the tensor cores cut an addition's
+// low bits off, so that a sum's error grows with the number of additions to it.
 constexpr int kShrinkStages = 3;
 template <int RP>
 constexpr int kShrinkStage = kTcTile * 128 + RP * 128;
@@ -846,7 +860,7 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const ShrinkArgs a,
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bar[kShrinkStages];
   __shared__ uint32_t slot;
-  constexpr int kTmem = RP < 32 ? 32 : RP, S = kShrinkStages;
+  constexpr int kTmem = 2 * RP, S = kShrinkStages;
   constexpr int kWPieces = (RP * 8 + kThreads - 1) / kThreads;
   grid_dependency_wait();
   grid_dependents_launch();
@@ -905,8 +919,8 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const ShrinkArgs a,
       const uint32_t st = ring + (ci % S) * kShrinkStage<RP>;
 #pragma unroll
       for (int ks = 0; ks < kChunk / 16; ++ks)
-        tc_mma_ss(tmem, smem_desc_sw128_kmajor(st + 32 * ks),
-                  smem_desc_sw128_kmajor(st + kTcTile * 128 + 32 * ks), idesc, (ci | ks) != 0);
+        tc_mma_ss(tmem + (ci & 1) * RP, smem_desc_sw128_kmajor(st + 32 * ks),
+                  smem_desc_sw128_kmajor(st + kTcTile * 128 + 32 * ks), idesc, ci > 1 || ks != 0);
       tc_commit(&bar[ci % S]);
     }
     if (ci + S - 1 < n) {
@@ -932,10 +946,16 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const ShrinkArgs a,
   float* out = a.part + (static_cast<int64_t>(split) * a.T + tile.y + row) * r;
 #pragma unroll
   for (int c = 16 * (warp >> 2); c < RP; c += 32) {
-    uint32_t v[16];
-    tmem_ld_32x32b_x16(tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + c, v);
+    uint32_t v[16], u[16];
+    const uint32_t at = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + c;
+    tmem_ld_32x32b_x16(at, v);
+    tmem_ld_32x32b_x16(at + RP, u);
     tmem_wait_ld();
     if (!ok || row >= tile.z) continue;
+    if (n > 1) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(u[i]));
+    }
     if (r % 16 == 0) {
       if (c < r) {
         store_32(out + c, &v[0]);

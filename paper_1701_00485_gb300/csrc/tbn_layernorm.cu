@@ -599,9 +599,18 @@ __global__ void __launch_bounds__(G != 0 ? 256 : 512) layernorm_bwd_kernel(const
       }
     }
   } else {
-    // the groups of the block one after another
-    for (int g = 0; g < kGroups; ++g) {
-      if (group == g) {
+    // a warp's groups by shuffles, then the block's warps one after another
+#pragma unroll
+    for (int o = G; o < 32; o <<= 1)
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+          dg[j][i] = add_f32x2(dg[j][i], __shfl_xor_sync(0xffffffffu, dg[j][i], o));
+          db[j][i] = add_f32x2(db[j][i], __shfl_xor_sync(0xffffffffu, db[j][i], o));
+        }
+    for (int g = 0; g < 8; ++g) {
+      if (threadIdx.x >> 5 == g && (threadIdx.x & 31) < G) {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -875,10 +884,15 @@ Teams make_teams(int64_t D, int max_nv, int resident, int bytes, int budget) {
   return t;
 }
 
-// The blocks of a launch that stay and take `rows` in turn, at least four each.
+// The blocks of a launch that stay and take `rows` in turn: as many as fit, at
+// least four rows for each of their teams, but no fewer than there are SMs while
+// every team has a row.
 int staying_blocks(int64_t rows, int64_t teams, int per_sm) {
-  int64_t n = static_cast<int64_t>(device_sm_count()) * per_sm;
-  const int64_t most = (rows + 4 * teams - 1) / (4 * teams);
+  const int64_t sms = device_sm_count();
+  int64_t n = sms * per_sm;
+  int64_t most = (rows + 4 * teams - 1) / (4 * teams);
+  const int64_t each = (rows + teams - 1) / teams;
+  if (most < sms) most = each < sms ? each : sms;
   if (n > most) n = most;
   return static_cast<int>(n < 1 ? 1 : n);
 }
