@@ -1217,6 +1217,9 @@ __global__ void __launch_bounds__(kExpandThreads, RP <= 64 ? 2 : 1)
 // ---- grad: D[columns of x][3 RP] over an item's tokens, both operands token by
 // token.  The three terms are columns of one MMA and are added at the end, the
 // smaller ones first: each term's sum loses nothing to the leading one's size.
+// The leading term has two sums that take the stages in turn (an addition cuts low
+// bits off, see shrink): in odd stages the terms stand as second, third, first and
+// D begins RP columns further on, [first, even | second | third | first, odd].
 constexpr int kGradTokens = 32;                  // of a stage
 constexpr int kGradBlock = kGradTokens * 128;    // bytes of 64 columns of it
 template <int RP>
@@ -1243,8 +1246,7 @@ __global__ void __launch_bounds__(kThreads) grad_tc_kernel(const __grid_constant
   __shared__ uint64_t bar[kGradStages<RP>];
   __shared__ uint32_t slot;
   constexpr int S = kGradStages<RP>, kCt = kGradCols<RP>, N = 3 * RP;
-  constexpr int kAcc = kCt / 128 * N;
-  constexpr int kTmem = kAcc <= 128 ? 128 : kAcc <= 256 ? 256 : 512;
+  constexpr int kD = 4 * RP, kTmem = kCt / 128 * kD;   // columns of D, and of all
   constexpr int kXRows = kThreads / (kCt / 8), kXPasses = kGradTokens / kXRows;   // rows of a pass
   constexpr int kURow = N / 8;                                           // pieces of a row of u
   constexpr int kUPasses = (kGradTokens * kURow + kThreads - 1) / kThreads;
@@ -1259,6 +1261,17 @@ __global__ void __launch_bounds__(kThreads) grad_tc_kernel(const __grid_constant
   const uint32_t tmem = tc_begin<kTmem>(&slot, bar, S);
   const uint32_t ring = smem_addr(align_1k(smem_raw));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // the odd stages' leading sums begin in the middle of an MMA's columns: zeros
+  {
+    const uint32_t zero[16] = {};
+    const uint32_t at = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + 3 * RP;
+    for (int c = 16 * (warp >> 2); c < kCt / 128 * RP; c += 32)
+      tmem_st_32x32b_x16(at + c / RP * kD + c % RP, zero);
+    tmem_wait_st();
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+  }
   const int n = (item.z + kGradTokens - 1) / kGradTokens;
   const int xc = tid % (kCt / 8), xrow = tid / (kCt / 8);
   const bool col_in = c0 + 8 * xc < sd.K;
@@ -1286,7 +1299,8 @@ __global__ void __launch_bounds__(kThreads) grad_tc_kernel(const __grid_constant
       if (kGradTokens * kURow % kThreads == 0 || m < kGradTokens) {
         const int t = kGradTokens * ci + m;
         const bool v = t < item.z;
-        cp_async16(st + kCt / 64 * kGradBlock + (c >> 3) * kGradBlock + tile_off(m, c & 7),
+        const int to = ci % 2 == 0 ? c : c >= RP / 8 ? c - RP / 8 : c + RP / 4;
+        cp_async16(st + kCt / 64 * kGradBlock + (to >> 3) * kGradBlock + tile_off(m, to & 7),
                    terms + static_cast<int64_t>(v ? t : 0) * N + 8 * c, v);
       }
     }
@@ -1314,7 +1328,7 @@ __global__ void __launch_bounds__(kThreads) grad_tc_kernel(const __grid_constant
         for (int m = 0; m < kCt / 128; ++m)
 #pragma unroll
           for (int q = 0; q < kMmas; ++q)
-            tc_mma_ss(tmem + m * N + q * kN, desc_mn(st + 2 * m * kGradBlock + ks * 2048, kGradBlock),
+            tc_mma_ss(tmem + m * kD + (ci & 1) * RP + q * kN, desc_mn(st + 2 * m * kGradBlock + ks * 2048, kGradBlock),
                       desc_mn(su + q * (kN / 64) * kGradBlock + ks * 2048, kGradBlock), idesc, (ci | ks) != 0);
       tc_commit(&bar[ci % S]);
     }
@@ -1341,19 +1355,20 @@ __global__ void __launch_bounds__(kThreads) grad_tc_kernel(const __grid_constant
   // upper 128, else every other 16 ranks
   const int m = kCt == 256 ? warp >> 2 : 0;
   const int e = c0 + 128 * m + 32 * (warp & 3) + lane;
-  const uint32_t acc = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + m * N;
+  const uint32_t acc = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + m * kD;
 #pragma unroll 1
   for (int k = kCt == 256 ? 0 : 16 * (warp >> 2); k < RP; k += kCt == 256 ? 16 : 32) {
-    uint32_t v[3][16];
+    uint32_t v[4][16];
 #pragma unroll
-    for (int t = 0; t < 3; ++t) tmem_ld_32x32b_x16(acc + t * RP + k, v[t]);
+    for (int t = 0; t < 4; ++t) tmem_ld_32x32b_x16(acc + t * RP + k, v[t]);
     tmem_wait_ld();
     if (ok && e < sd.K) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (k + i < r)   // past the adapter's rank zeros, whatever x holds
           out[static_cast<int64_t>(k + i) * sd.K + e] =
-              k + i < rank ? __uint_as_float(v[0][i]) + (__uint_as_float(v[1][i]) + __uint_as_float(v[2][i]))
+              k + i < rank ? (__uint_as_float(v[0][i]) + __uint_as_float(v[3][i])) +
+                                 (__uint_as_float(v[1][i]) + __uint_as_float(v[2][i]))
                            : 0.0f;
     }
   }
