@@ -171,130 +171,115 @@ struct Route {
 // adapter's (lanes of equal ids find each other, so that no two add at once),
 // the counts are summed over warps and adapters, and the warp goes through its
 // run once more to place the tokens: the order within an adapter is kept.
-// Latency is what it costs (everything else waits for it): a run's ids are asked
-// for eight at a time and kept, 8192 tokens in all.
-constexpr int kRouteBatch = 8;
+// Everything else waits for this kernel and each of its instructions runs once or
+// a few times, so its loops stay rolled (fetching unrolled code took longer than
+// it saved) and up to 8192 ids are kept in shared memory.
+constexpr int kRouteKept = 256;   // ids of a run
 
 __global__ void __launch_bounds__(1024) route_kernel(const int32_t* ids, int T, int n,
                                                      int tile, int tokens_per_item, Route r) {
-  extern __shared__ int sh[];          // counts [n + 1][32], then starts, tiles, items [n + 2] each
-  __shared__ int warp_sum[3][32];
+  extern __shared__ int sh[];   // counts [n + 1][32]; starts, tiles, items [n + 2] each; ids kept
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int groups = n + 1;            // the last: no adapter
+  const int groups = n + 1;     // the last: no adapter
   int *start = sh + 32 * groups, *first_tile = start + groups + 1, *first_item = first_tile + groups + 1;
+  int* kept = first_item + groups + 1 + warp * kRouteKept;
+#pragma unroll 1
   for (int i = tid; i < 32 * groups; i += 1024) sh[i] = 0;
   grid_dependency_wait();
   grid_dependents_launch();
   const int run = (T + 31) / 32;
   const int beg = min(T, warp * run), end = min(T, beg + run);
-  int g[kRouteBatch];   // groups of the lane's tokens of a batch, -1: none
-  const auto load = [&](int t0) {
-#pragma unroll
-    for (int i = 0; i < kRouteBatch; ++i) {
-      const int t = t0 + 32 * i + lane;
-      g[i] = t < end ? (ids != nullptr ? __ldg(ids + t) : 0) : -2;
-    }
-#pragma unroll
-    for (int i = 0; i < kRouteBatch; ++i)
-      g[i] = g[i] >= 0 && g[i] < n ? g[i] : t0 + 32 * i + lane < end ? n : -1;
+  const auto read = [&](int t) {
+    const int id = ids != nullptr ? __ldg(ids + t) : 0;
+    return id >= 0 && id < n ? id : n;
   };
-  load(beg);
+#pragma unroll 4
+  for (int i = lane; i < min(end - beg, kRouteKept); i += 32) kept[i] = read(beg + i);
   __syncthreads();
-  for (int t0 = beg; t0 < end; t0 += 32 * kRouteBatch) {
-    if (t0 != beg) load(t0);
-#pragma unroll
-    for (int i = 0; i < kRouteBatch; ++i) {
-      if (t0 + 32 * i >= end) break;
-      const uint32_t same = __match_any_sync(0xffffffffu, g[i]);
-      if (g[i] >= 0 && lane == __ffs(same) - 1) sh[g[i] * 32 + warp] += __popc(same);
-      __syncwarp();
-    }
+  // the lane's token's group (-1: no token) and the lanes of the same one.  A
+  // request's tokens stand together: mostly all agree, which is cheaper to find
+  // out than to match them.
+  const auto look = [&](int t0, uint32_t* same) {
+    const int i = t0 - beg + lane;
+    const int g = t0 + lane >= end ? -1 : i < kRouteKept ? kept[i] : read(t0 + lane);
+    *same = __all_sync(0xffffffffu, g == __shfl_sync(0xffffffffu, g, 0))
+                ? 0xffffffffu
+                : __match_any_sync(0xffffffffu, g);
+    return g;
+  };
+#pragma unroll 1
+  for (int t0 = beg; t0 < end; t0 += 32) {
+    uint32_t same;
+    const int g = look(t0, &same);
+    if (g >= 0 && lane == __ffs(same) - 1) sh[g * 32 + warp] += __popc(same);
+    __syncwarp();
   }
   __syncthreads();
-  // a warp per adapter: its runs' counts become their first places
-  for (int q = warp; q < groups; q += 32) {
-    const int c = sh[q * 32 + lane];
-    int s = c;
-#pragma unroll
+  const auto scan = [&](int v) {   // inclusive, over the warp
+#pragma unroll 1
     for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, s, o);
-      if (lane >= o) s += u;
+      const int u = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += u;
     }
+    return v;
+  };
+  // a warp per adapter: its runs' counts become their first places
+#pragma unroll 1
+  for (int q = warp; q < groups; q += 32) {
+    const int c = sh[q * 32 + lane], s = scan(c);
     sh[q * 32 + lane] = s - c;
     if (lane == 31) start[q] = s;
   }
   __syncthreads();
-  // exclusive sums over the adapters of tokens, tiles and items
-  int v[3] = {0, 0, 0}, s[3];
-  if (tid < groups) {
-    v[0] = start[tid];
-    v[1] = (v[0] + tile - 1) / tile;
-    v[2] = tid < n ? (v[0] + tokens_per_item - 1) / tokens_per_item : 0;
-  }
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    s[k] = v[k];
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, s[k], o);
-      if (lane >= o) s[k] += u;
+  // exclusive sums over the adapters: warp 0 tiles, warp 1 items, then tokens,
+  // which the other two are made from
+  const auto sums = [&](int per, int most, int* out) {
+    int carry = 0;
+#pragma unroll 1
+    for (int q0 = 0; q0 < groups; q0 += 32) {
+      const int q = q0 + lane;
+      const int v = q < most ? (start[q] + per - 1) / per : 0, s = scan(v);
+      if (q < groups) out[q] = carry + s - v;
+      carry += __shfl_sync(0xffffffffu, s, 31);
     }
-    if (lane == 31) warp_sum[k][warp] = s[k];
-  }
-  __syncthreads();
-  if (warp < 3) {
-    const int c = warp_sum[warp][lane];
-    int x = c;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += u;
-    }
-    warp_sum[warp][lane] = x - c;
-  }
-  __syncthreads();
-  if (tid < groups) {
-    start[tid] = s[0] - v[0] + warp_sum[0][warp];
-    first_tile[tid] = s[1] - v[1] + warp_sum[1][warp];
-    first_item[tid] = s[2] - v[2] + warp_sum[2][warp];
-    r.item_begin[tid] = first_item[tid];
-    if (tid == groups - 1) {
-      start[groups] = start[tid] + v[0];
-      first_tile[groups] = first_tile[tid] + v[1];
-      first_item[groups] = first_item[tid] + v[2];
-      r.counts[0] = first_tile[groups];
-      r.counts[1] = first_item[groups];
-    }
-  }
-  __syncthreads();
-  // the lists: entry i belongs to the last adapter that begins at or before it
-  const auto list = [&](const int* begin, int4* out, int per) {
-    for (int i = tid; i < begin[groups]; i += 1024) {
-      int lo = 0, hi = groups;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (begin[mid] <= i) lo = mid;
-        else hi = mid;
-      }
-      const int at = start[lo] + (i - begin[lo]) * per;
-      out[i] = make_int4(lo < n ? lo : -1, at, min(per, start[lo + 1] - at), 0);
-    }
+    if (lane == 0) out[groups] = carry;
   };
-  list(first_tile, r.tiles, tile);
-  list(first_item, r.items, tokens_per_item);
-  for (int t0 = beg; t0 < end; t0 += 32 * kRouteBatch) {
-    if (run > 32 * kRouteBatch) load(t0);
-#pragma unroll
-    for (int i = 0; i < kRouteBatch; ++i) {
-      if (t0 + 32 * i >= end) break;
-      const uint32_t same = __match_any_sync(0xffffffffu, g[i]);
-      if (g[i] >= 0)
-        r.perm[start[g[i]] + sh[g[i] * 32 + warp] + __popc(same & ((1u << lane) - 1u))] =
-            t0 + 32 * i + lane;
-      __syncwarp();
-      if (g[i] >= 0 && lane == __ffs(same) - 1) sh[g[i] * 32 + warp] += __popc(same);
-      __syncwarp();
+  if (warp < 2) sums(warp == 0 ? tile : tokens_per_item, warp == 0 ? groups : n,
+                     warp == 0 ? first_tile : first_item);
+  __syncthreads();
+  if (warp == 0) sums(1, groups, start);   // each count is read before its sum is written
+  __syncthreads();
+#pragma unroll 1
+  for (int q = tid; q < groups; q += 1024) r.item_begin[q] = first_item[q];
+  if (tid == 0) {
+    r.counts[0] = first_tile[groups];
+    r.counts[1] = first_item[groups];
+  }
+  // the lists: entry i belongs to the last adapter that begins at or before it
+  const int tiles = first_tile[groups], entries = tiles + first_item[groups];
+#pragma unroll 1
+  for (int j = tid; j < entries; j += 1024) {
+    const bool is_tile = j < tiles;
+    const int* begin = is_tile ? first_tile : first_item;
+    const int i = is_tile ? j : j - tiles, per = is_tile ? tile : tokens_per_item;
+    int lo = 0, hi = groups;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (begin[mid] <= i) lo = mid;
+      else hi = mid;
     }
+    const int at = start[lo] + (i - begin[lo]) * per;
+    (is_tile ? r.tiles : r.items)[i] = make_int4(lo < n ? lo : -1, at, min(per, start[lo + 1] - at), 0);
+  }
+#pragma unroll 1
+  for (int t0 = beg; t0 < end; t0 += 32) {
+    uint32_t same;
+    const int g = look(t0, &same);
+    if (g >= 0)
+      r.perm[start[g] + sh[g * 32 + warp] + __popc(same & ((1u << lane) - 1u))] = t0 + lane;
+    __syncwarp();
+    if (g >= 0 && lane == __ffs(same) - 1) sh[g * 32 + warp] += __popc(same);
+    __syncwarp();
   }
 }
 
@@ -318,7 +303,7 @@ struct ShrinkArgs {
   const __nv_bfloat16* w;    // [n][r][K]
   float* part;               // [splits][T][r], by sorted position
   int64_t ldx;
-  int T, K, chunks, chunks_per, splits;
+  int T, K, chunks, chunks_per;
   int x_aligned, w_aligned;
 };
 
@@ -778,10 +763,11 @@ __global__ void __launch_bounds__(256) grad_reduce_kernel(const __grid_constant_
 // The same three products for bf16 activations in aligned rows, on tiles of 128
 // tokens: operands come by cp.async into a ring (zero-filled where there is no
 // token, no rank or no column), one thread issues the MMAs, sums stay in tensor
-// memory.  The low-rank activations between two products are written once as
-// bf16 terms (terms_kernel), a row's terms side by side.
+// memory.  The low-rank activations between two products are kept as
+// bf16 terms.
 constexpr int kTcTile = 128;
 constexpr int64_t kTcFrom = 128;   // tokens
+constexpr int64_t kPrefetchBytes = int64_t(80) << 20;   // of the 129 MB of L2
 constexpr int kExpandCtas = 4;      // of expand, an SM and launch
 constexpr int kGradCtas = 2;        // of grad
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
@@ -841,37 +827,110 @@ __device__ __forceinline__ uint8_t* align_1k(uint8_t* p) {
   return p + ((1024u - (smem_addr(p) & 1023u)) & 1023u);
 }
 
-// 32 bytes to a 32-byte aligned address: a whole sector.
-__device__ __forceinline__ void store_32(void* p, const uint32_t* v) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]),
-               "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-               : "memory");
-}
-
-// ---- shrink: D[128 tokens][RP] over every splits-th chunk of K, both operands
-// K-major.  Two sums take the chunks in turn: the tensor cores cut an addition's
-// low bits off, so that a sum's error grows with the number of additions to it.
+// ---- shrink: D[128 tokens][RP], both operands K-major, by a cluster of CTAs
+// that take every splits-th chunk of K each (neighbouring CTAs read neighbouring
+// parts of the rows).  Two sums take a CTA's chunks in turn: the tensor cores cut
+// an addition's low bits off, so that a sum's error grows with the number of
+// additions to it.  The CTAs' sums meet in distributed shared memory: each CTA
+// adds some tokens' over the cluster, in order, and writes them as bf16 terms, a
+// token's terms side by side (and once as they are, for the backward pass).
 constexpr int kShrinkStages = 3;
 template <int RP>
 constexpr int kShrinkStage = kTcTile * 128 + RP * 128;
-
 template <int RP>
-__global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const ShrinkArgs a, uint32_t* err) {
+constexpr int kSumRow = RP + 4;   // floats: rows of neighbouring lanes in other banks
+template <int RP>
+constexpr int kShrinkSmem = 1024 + kShrinkStages * kShrinkStage<RP>;
+
+struct ShrinkTcArgs {
+  Route route;
+  Adapters ad;
+  const __nv_bfloat16* x;
+  const __nv_bfloat16* w;   // [n][r][K]
+  __nv_bfloat16* terms;     // [T][kTerms RP], by sorted position
+  float* v_out;             // or nullptr: [T][r] by token, unscaled
+  int64_t ldx;
+  int K, chunks, splits, max_tiles, prefetch_rows;
+  // a second job, of the launch's clusters from max_tiles on (which may be 0: the
+  // only job): these low-rank activations [T][r], by token, as terms
+  const float* v_in;
+  __nv_bfloat16* v_terms;
+  uint32_t* err;
+};
+
+__device__ __forceinline__ float4 load_cluster(uint32_t addr, int rank) {
+  float4 v;
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(at)
+               : "memory");
+  return v;
+}
+
+// Eight ranks from `col` on of the token at sorted position `at`, as terms.  Past
+// the rank they are zero, whatever v holds there.
+template <int RP, int kTerms>
+__device__ __forceinline__ void write_terms(const float (&v)[8], float factor, int col, int rank,
+                                            int64_t at, __nv_bfloat16* terms) {
+  float t[8][kTerms];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) split(col + j < rank ? v[j] * factor : 0.0f, t[j]);
+  __nv_bfloat16* out = terms + at * (kTerms * RP) + col;
+#pragma unroll
+  for (int k = 0; k < kTerms; ++k)
+    *reinterpret_cast<uint4*>(out + k * RP) =
+        make_uint4(pack_bf16x2(t[0][k], t[1][k]), pack_bf16x2(t[2][k], t[3][k]),
+                   pack_bf16x2(t[4][k], t[5][k]), pack_bf16x2(t[6][k], t[7][k]));
+}
+
+template <int RP, int kTerms>
+__global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const __grid_constant__ ShrinkTcArgs a) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bar[kShrinkStages];
   __shared__ uint32_t slot;
   constexpr int kTmem = 2 * RP, S = kShrinkStages;
   constexpr int kWPieces = (RP * 8 + kThreads - 1) / kThreads;
+  static_assert(kTcTile * kSumRow<RP> * 4 <= kShrinkStages * kShrinkStage<RP>, "sums in the ring");
+  // while the tokens are being sorted: x is asked for in L2 (a hint that reads
+  // nothing, so that it may stand before the wait)
+  for (int i = blockIdx.x + gridDim.x * threadIdx.x; i < a.prefetch_rows; i += gridDim.x * kThreads)
+    bulk_prefetch(a.x + i * a.ldx, a.K * 2);
   grid_dependency_wait();
   grid_dependents_launch();
-  const int tile_id = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
-  if (tile_id >= a.route.counts[0]) return;
-  const int4 tile = a.route.tiles[tile_id];
-  if (tile.x < 0) return;
-  const uint32_t tmem = tc_begin<kTmem>(&slot, bar, S);
-  const uint32_t ring = smem_addr(align_1k(smem_raw));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, ch = tid & 7;
+  const int split = blockIdx.x % a.splits, rows = kTcTile / a.splits;   // rows that a CTA finishes
+  int tile_id = blockIdx.x / a.splits;
+  const bool second = tile_id >= a.max_tiles;
+  if (second) tile_id -= a.max_tiles;
+  if (tile_id >= a.route.counts[0]) return;   // all CTAs of the cluster alike
+  const int4 tile = a.route.tiles[tile_id];
+  const int r = a.ad.r;
+  if (tile.x < 0) {
+    if (a.v_out != nullptr && !second)
+      for (int i = split * kThreads + tid; i < tile.z * r; i += a.splits * kThreads)
+        a.v_out[static_cast<int64_t>(a.route.perm[tile.y + i / r]) * r + i % r] = 0.0f;
+    return;
+  }
   const int rank = a.ad.rank(tile.x);
+  const float factor = a.ad.factor(tile.x);
+  if (second) {
+    for (int i = tid; i < rows * (RP / 8); i += kThreads) {
+      const int m = split * rows + i / (RP / 8), col = 8 * (i % (RP / 8));
+      if (m >= tile.z) continue;
+      const float* p = a.v_in + static_cast<int64_t>(a.route.perm[tile.y + m]) * r + col;
+      float v[8] = {};
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (col + j < rank) v[j] = p[j];
+      write_terms<RP, kTerms>(v, factor, col, rank, tile.y + m, a.v_terms);
+    }
+    return;
+  }
+  const uint32_t tmem = tc_begin<kTmem>(&slot, bar, S);
+  uint8_t* smem = align_1k(smem_raw);
+  const uint32_t ring = smem_addr(smem);
   const int n = (a.chunks - split + a.splits - 1) / a.splits;   // chunks split, split + splits, ...
   const __nv_bfloat16* xr[4];
   uint32_t there = 0;
@@ -879,11 +938,10 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const ShrinkArgs a,
   for (int i = 0; i < 4; ++i) {
     const int row = (tid >> 3) + 32 * i;
     const bool v = row < tile.z;
-    xr[i] = static_cast<const __nv_bfloat16*>(a.x) +
-            (v ? a.route.perm[tile.y + row] * a.ldx : 0);
+    xr[i] = a.x + (v ? a.route.perm[tile.y + row] * a.ldx : 0);
     there |= static_cast<uint32_t>(v) << i;
   }
-  const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * a.ad.r * a.K;
+  const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * r * a.K;
   const auto issue = [&](int ci) {
     const uint32_t st = ring + (ci % S) * kShrinkStage<RP>;
     const int e = (split + ci * a.splits) * kChunk + 8 * ch;
@@ -916,17 +974,17 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const ShrinkArgs a,
     __syncthreads();
     if (tid == 0) {
       tc_fence_after_sync();
-      const uint32_t st = ring + (ci % S) * kShrinkStage<RP>;
+      const uint64_t x0 = smem_desc_sw128_kmajor(ring + (ci % S) * kShrinkStage<RP>);
 #pragma unroll
       for (int ks = 0; ks < kChunk / 16; ++ks)
-        tc_mma_ss(tmem + (ci & 1) * RP, smem_desc_sw128_kmajor(st + 32 * ks),
-                  smem_desc_sw128_kmajor(st + kTcTile * 128 + 32 * ks), idesc, ci > 1 || ks != 0);
+        tc_mma_ss(tmem + (ci & 1) * RP, x0 + 2 * ks, x0 + (kTcTile * 128 / 16 + 2 * ks), idesc,
+                  ci > 1 || ks != 0);
       tc_commit(&bar[ci % S]);
     }
     if (ci + S - 1 < n) {
       // the stage refilled held chunk ci - 1: its MMAs must have read it
       if (ci >= 1 && tid == 0)
-        ok = mbar_wait(&bar[(ci - 1) % S], static_cast<uint32_t>((ci - 1) / S) & 1u, nullptr, err,
+        ok = mbar_wait(&bar[(ci - 1) % S], static_cast<uint32_t>((ci - 1) / S) & 1u, nullptr, a.err,
                        kWaitLimitNs);
       if (!__syncthreads_and(ok)) break;
       issue(ci + S - 1);
@@ -935,15 +993,11 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const ShrinkArgs a,
   }
   cp_async_wait<0>();
   if (tid == 0)
-    ok = mbar_wait(&bar[(n - 1) % S], static_cast<uint32_t>((n - 1) / S) & 1u, nullptr, err,
-                   kWaitLimitNs) && ok;
-  ok = __syncthreads_and(ok);
+    mbar_wait(&bar[(n - 1) % S], static_cast<uint32_t>((n - 1) / S) & 1u, nullptr, a.err, kWaitLimitNs);
+  __syncthreads();
   tc_fence_after_sync();
-  // warp w: tokens 32 (w % 4) .., every other 16 ranks.  A thread holds a row:
-  // its stores are as wide as the rows' alignment lets them be (single floats
-  // cost a sector each: 10 us of the kernel's 28 at 8192 tokens, rank 64)
-  const int row = 32 * (warp & 3) + lane, r = a.ad.r;
-  float* out = a.part + (static_cast<int64_t>(split) * a.T + tile.y + row) * r;
+  // warp w: tokens 32 (w % 4) .., every other 16 ranks, a thread a token
+  float* sums = reinterpret_cast<float*>(smem);   // [128][kSumRow]
 #pragma unroll
   for (int c = 16 * (warp >> 2); c < RP; c += 32) {
     uint32_t v[16], u[16];
@@ -951,91 +1005,38 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const ShrinkArgs a,
     tmem_ld_32x32b_x16(at, v);
     tmem_ld_32x32b_x16(at + RP, u);
     tmem_wait_ld();
-    if (!ok || row >= tile.z) continue;
-    if (n > 1) {
+    float4* row = reinterpret_cast<float4*>(sums + (32 * (warp & 3) + lane) * kSumRow<RP> + c);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(u[i]));
-    }
-    if (r % 16 == 0) {
-      if (c < r) {
-        store_32(out + c, &v[0]);
-        store_32(out + c + 8, &v[8]);
-      }
-    } else {
+    for (int i = 0; i < 16; i += 4) {
+      float f[4];
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (c + i < r) out[c + i] = __uint_as_float(v[i]);
+      for (int k = 0; k < 4; ++k)   // the second sum of a single chunk holds nothing
+        f[k] = n > 1 ? __uint_as_float(v[i + k]) + __uint_as_float(u[i + k]) : __uint_as_float(v[i + k]);
+      row[i / 4] = make_float4(f[0], f[1], f[2], f[3]);
     }
   }
-  tc_end<kTmem>(tmem);
-}
-
-// ---- the low-rank activations as bf16 terms, by sorted position
-struct TermsSide {
-  LowRank v;
-  __nv_bfloat16* terms;   // [T][kTerms RP]
-  float* v_out;           // or nullptr: [T][r] by token, unscaled
-};
-
-struct TermsArgs {
-  Route route;
-  Adapters ad;
-  TermsSide side[2];      // gridDim.z of them
-};
-
-// Block (tile, part, side); a thread takes eight ranks of a token.  Past the rank
-// the terms are zero, whatever v holds there.
-template <int RP, int kTerms>
-__global__ void __launch_bounds__(kThreads) terms_kernel(const __grid_constant__ TermsArgs a) {
-  grid_dependency_wait();
-  grid_dependents_launch();
-  if (static_cast<int>(blockIdx.x) >= a.route.counts[0]) return;
-  const int4 tile = a.route.tiles[blockIdx.x];
-  const TermsSide& sd = a.side[blockIdx.z];
-  const int r = a.ad.r, rank = tile.x < 0 ? 0 : a.ad.rank(tile.x);
-  if (tile.x < 0 && sd.v_out == nullptr) return;
-  const float factor = tile.x < 0 ? 0.0f : a.ad.factor(tile.x);
-  const bool whole = r % 8 == 0;   // eight ranks lie in whole 16-byte words
-  for (int i = threadIdx.x + blockIdx.y * kThreads; i < tile.z * (RP / 8);
-       i += kThreads * gridDim.y) {
-    const int m = i / (RP / 8), col = 8 * (i % (RP / 8));
-    const int token = a.route.perm[tile.y + m];
-    const float* p = sd.v.p + static_cast<int64_t>(sd.v.by_token ? token : tile.y + m) * r + col;
+  cluster_sync();
+  const uint32_t sums_s = smem_addr(sums);
+  for (int i = tid; i < rows * (RP / 8); i += kThreads) {
+    const int m = split * rows + i / (RP / 8), col = 8 * (i % (RP / 8));
+    if (m >= tile.z) continue;
     float v[8] = {};
-    if (whole && col < rank) {
-#pragma unroll 4
-      for (int q = 0; q < sd.v.splits; ++q) {
-        const float4* f = reinterpret_cast<const float4*>(p + q * sd.v.split_stride);
-        const float4 x = f[0], y = f[1];
-        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-        v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
-      }
-    } else if (!whole) {
+    for (int q = 0; q < a.splits; ++q) {
+      const uint32_t at = sums_s + (m * kSumRow<RP> + col) * 4;
+      const float4 x = load_cluster(at, q), y = load_cluster(at + 16, q);
+      v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+      v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+    }
+    if (a.v_out != nullptr) {
+      float* o = a.v_out + static_cast<int64_t>(a.route.perm[tile.y + m]) * r + col;
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (col + j < rank)
-          for (int q = 0; q < sd.v.splits; ++q) v[j] += p[q * sd.v.split_stride + j];
+        if (col + j < r) o[j] = col + j < rank ? v[j] : 0.0f;
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (col + j >= rank) v[j] = 0.0f;
-    if (sd.v_out != nullptr) {
-      float* o = sd.v_out + static_cast<int64_t>(token) * r + col;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (col + j < r) o[j] = v[j];
-    }
-    if (tile.x < 0) continue;
-    float t[8][kTerms];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) split(v[j] * factor, t[j]);
-    __nv_bfloat16* out = sd.terms + (tile.y + m) * static_cast<int64_t>(kTerms * RP) + col;
-#pragma unroll
-    for (int k = 0; k < kTerms; ++k)
-      *reinterpret_cast<uint4*>(out + k * RP) =
-          make_uint4(pack_bf16x2(t[0][k], t[1][k]), pack_bf16x2(t[2][k], t[3][k]),
-                     pack_bf16x2(t[4][k], t[5][k]), pack_bf16x2(t[6][k], t[7][k]));
+    if (a.terms != nullptr) write_terms<RP, kTerms>(v, factor, col, rank, tile.y + m, a.terms);
   }
+  cluster_sync();   // no CTA leaves while another reads its sums
+  tc_end<kTmem>(tmem);
 }
 
 // ---- expand: D[128 tokens][128 columns] over two terms of RP ranks
@@ -1055,162 +1056,221 @@ template <int RP>
 constexpr int kExpandV = (2 * RP + 63) / 64 * kTcTile * 128;
 template <int RP>
 constexpr int kExpandW = 2 * RP * 128;            // of a stage: two blocks of 64 columns
-constexpr int kExpandThreads = 512;
-constexpr int kExpandRows = kExpandThreads / 16;  // rows of y of a pass
 constexpr int kExpandY = kTcTile * kCols * 2;     // the base's rows, then y's
 template <int RP>
-constexpr int kExpandYs = RP == 64 ? 1 : 2;       // as many as leave room for the CTAs
+constexpr int kExpandWs = RP == 64 ? 1 : 2;       // stages of w: as many as leave room for two CTAs
 template <int RP>
-constexpr int kExpandSmem =
-    1024 + kExpandV<RP> + 2 * kExpandW<RP> + kExpandYs<RP> * kExpandY;
+constexpr int kExpandSmem = kExpandV<RP> + kExpandWs<RP> * kExpandW<RP> + 2 * kExpandY + 1024;
+constexpr int kFinishers = 8;                     // warps
+constexpr int kLoaders = 4;                       // warps
+constexpr int kExpandThreads = 32 * (kFinishers + 1 + kLoaders);
 
 // CTA (tile, column tiles group, group + groups, ...), two on an SM up to rank
-// 64.  V is the K-major operand, w the other, ranks as steps.  The MMAs of one
-// column tile run while the tile before it is finished: a thread adds its token's
-// sums to the base's row in shared memory (16-byte chunk c of row m at c ^ (m &
-// 7)), and y leaves in rows of 256 bytes, as the base came.  (Rows read and
-// written by their own threads take a tag lookup a sector: 88 us at 8209 x 8192,
-// rank 64.)
+// 64.  V is the K-major operand, w the other, ranks as steps.  Its warps wait for
+// one another only through barriers in shared memory: four load V and w, one
+// issues the MMAs into two sums in turn, and eight finish 32 tokens x 64 columns
+// each, by themselves: their part of the base comes by cp.async, a thread adds its
+// token's sums to it (16-byte chunk c of row m at c ^ (m & 7)), and the warp writes
+// it out in rows of 128 bytes.  (With block-wide barriers between these steps 60 us
+// at 8209 x 8192, rank 64, a third of it the steps' latencies; with rows read and
+// written by their own threads, a tag lookup a sector, 88.)
+struct ExpandControl {
+  uint64_t w_full[2], w_free[2], sum_full[2], sum_free[2];
+  uint32_t slot;
+  int abort;
+  int token[kTcTile];
+};
+static_assert(sizeof(ExpandControl) <= 1024, "control");
+
 template <int RP>
 __global__ void __launch_bounds__(kExpandThreads, RP <= 64 ? 2 : 1)
     expand_tc_kernel(const __grid_constant__ ExpandTcArgs a) {
-  extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bar[2];
-  __shared__ uint32_t slot;
-  __shared__ int token[kTcTile];
+  extern __shared__ __align__(1024) uint8_t smem[];
+  // without static variables the dynamic ones begin at a multiple of 1024 bytes;
+  // the kilobyte behind the tiles holds the rest
+  ExpandControl& ctl = *reinterpret_cast<ExpandControl*>(smem + kExpandSmem<RP> - 1024);
+  constexpr int YB = 2, WB = kExpandWs<RP>;
+  if ((smem_addr(smem) & 1023u) != 0u) {
+    if (threadIdx.x == 0) raise_device_error(a.err, TBN_DEVERR_BAD_LAUNCH);
+    return;
+  }
   grid_dependency_wait();
   grid_dependents_launch();
-  const int tile_id = blockIdx.x / a.groups, group = blockIdx.x % a.groups;
-  if (tile_id >= a.route.counts[0]) return;
+  // the tiles without adapter are the list's last and are copied here first, beside
+  // the others' work
+  const int tile_id = a.route.counts[0] - 1 - static_cast<int>(blockIdx.x / a.groups);
+  const int group = blockIdx.x % a.groups;
+  if (tile_id < 0) return;
   const int4 tile = a.route.tiles[tile_id];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  int* token = ctl.token;
   if (tid < kTcTile) token[tid] = tid < tile.z ? a.route.perm[tile.y + tid] : 0;
-  // this thread's pieces of a tile of y: chunk tid % 16 of rows tid / 16 + 32 i
-  const int pc = tid & 15, prow = tid >> 4;
   if (tile.x < 0) {   // no adapter: the base, or zeros
     if (a.base == a.y && a.ldbase == a.ldy) return;
     __syncthreads();
-    for (int c = group * kCols + 8 * pc; c < a.K; c += a.groups * kCols)
-      for (int m = prow; m < tile.z; m += kExpandRows) {
-        uint4 d = make_uint4(0u, 0u, 0u, 0u);
-        if (a.base != nullptr) d = *reinterpret_cast<const uint4*>(a.base + token[m] * a.ldbase + c);
-        *reinterpret_cast<uint4*>(a.y + token[m] * a.ldy + c) = d;
+    constexpr int kRows = kExpandThreads / 16, kOnce = 5;   // rows of a pass; passes at once
+    for (int c = group * kCols + 8 * (tid & 15); c < a.K; c += a.groups * kCols)
+      for (int m0 = tid >> 4; m0 < tile.z; m0 += kOnce * kRows) {
+        uint4 d[kOnce];
+#pragma unroll
+        for (int i = 0; i < kOnce; ++i) {
+          const int m = m0 + i * kRows;
+          d[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (a.base != nullptr && m < tile.z)
+            d[i] = *reinterpret_cast<const uint4*>(a.base + token[m] * a.ldbase + c);
+        }
+#pragma unroll
+        for (int i = 0; i < kOnce; ++i) {
+          const int m = m0 + i * kRows;
+          if (m < tile.z) *reinterpret_cast<uint4*>(a.y + token[m] * a.ldy + c) = d[i];
+        }
       }
     return;
   }
-  const uint32_t tmem = tc_begin<2 * kCols>(&slot, bar, 2);
-  uint8_t* smem = align_1k(smem_raw);
-  uint8_t* ybuf = smem + kExpandV<RP> + 2 * kExpandW<RP>;
-  const uint32_t sv = smem_addr(smem), sw = sv + kExpandV<RP>, sy = smem_addr(ybuf);
-  const int rank = a.ad.rank(tile.x);
-  const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * a.ad.r * a.K;
+  if (tid == 0) {
+    ctl.abort = 0;
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&ctl.w_full[i], 32 * kLoaders);
+      mbar_init(&ctl.w_free[i], 1);
+      mbar_init(&ctl.sum_full[i], 1);
+      mbar_init(&ctl.sum_free[i], kFinishers);
+    }
+  }
+  const uint32_t tmem = tc_begin<2 * kCols>(&ctl.slot, nullptr, 0);
+  uint8_t* ybuf = smem + kExpandV<RP> + WB * kExpandW<RP>;
+  const uint32_t sv = smem_addr(smem), sw = sv + kExpandV<RP>;
   const int tiles = (a.K + kCols - 1) / kCols, n = (tiles - group + a.groups - 1) / a.groups;
   const auto column = [&](int t) { return (group + t * a.groups) * kCols; };
-  const auto load_w = [&](int t) {
-    if (t < n) {
-      const int c0 = column(t);
+  // tile t is the (t / 2)-th use of its sums and the (t / WB)-th of its stage of w:
+  // the barriers' phases
+  const auto phase = [](int t) { return static_cast<uint32_t>(t >> 1) & 1u; };
+  const auto w_phase = [](int t) { return static_cast<uint32_t>(t / WB) & 1u; };
+  if (warp < kFinishers) {
+    // ---------------- finish: tokens 32 (warp % 4) .., columns 64 (warp / 4) ..
+    const int r0 = 32 * (warp & 3), c0 = 64 * (warp >> 2);
+    uint8_t* mine = ybuf + warp * 4096;                 // of each buffer: 32 rows of 128 bytes
+    const int pc = lane & 7, pr = lane >> 3;            // pieces: chunk pc of rows pr + 4 i
+    const uint32_t acc = tmem + (static_cast<uint32_t>(r0) << 16) + c0;
+    const auto load_base = [&](int t) {
+      if (t < n) {
+        const int e = column(t) + c0 + 8 * pc;
+        const uint32_t to = smem_addr(mine) + (t % YB) * kExpandY;
 #pragma unroll
-      for (int i = 0; i < (RP + kExpandRows - 1) / kExpandRows; ++i) {
-        const int wr = prow + kExpandRows * i, e = c0 + 8 * pc;
-        if (RP < kExpandRows && wr >= RP) break;
-        const bool v = wr < rank && e < a.K;
-        cp_async16(sw + (t & 1) * kExpandW<RP> + (pc >> 3) * (RP * 128) + tile_off(wr, pc & 7),
-                   v ? w + static_cast<int64_t>(wr) * a.K + e : w, v);
+        for (int i = 0; i < 8; ++i) {
+          const int m = pr + 4 * i;
+          const bool v = a.base != nullptr && r0 + m < tile.z && e < a.K;
+          cp_async16(to + tile_off(m, pc), v ? a.base + token[r0 + m] * a.ldbase + e : a.w, v);
+        }
+      }
+      cp_async_commit();
+    };
+    for (int t = 0; t < YB; ++t) load_base(t);
+    for (int t = 0; t < n; ++t) {
+      cp_async_wait<YB - 1>();
+      __syncwarp();
+      mbar_wait(&ctl.sum_full[t & 1], phase(t), &ctl.abort, a.err, kWaitLimitNs);
+      tc_fence_after_sync();
+      uint8_t* rows = mine + (t % YB) * kExpandY;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t v[32];
+        tmem_ld_32x32b_x32(acc + (t & 1) * kCols + 32 * h, v);
+        tmem_wait_ld();
+        if (h == 1) {
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ctl.sum_free[t & 1]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint4* p = reinterpret_cast<uint4*>(rows + tile_off(lane, 4 * h + i));
+          uint4 b = *p;
+          uint32_t* u = reinterpret_cast<uint32_t*>(&b);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint64_t f = add_f32x2(f32x2(v[8 * i + 2 * j], v[8 * i + 2 * j + 1]),
+                                         f32x2(u[j] << 16, u[j] & 0xFFFF0000u));
+            u[j] = pack_bf16x2(__uint_as_float(static_cast<uint32_t>(f)),
+                               __uint_as_float(static_cast<uint32_t>(f >> 32)));
+          }
+          *p = b;
+        }
+      }
+      __syncwarp();
+      const int e = column(t) + c0 + 8 * pc;
+      if (e < a.K) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int m = pr + 4 * i;
+          if (r0 + m < tile.z)
+            *reinterpret_cast<uint4*>(a.y + token[r0 + m] * a.ldy + e) =
+                *reinterpret_cast<const uint4*>(rows + tile_off(m, pc));
+        }
+      }
+      // the pieces that this lane copied out are those that it copies in
+      load_base(t + YB);
+    }
+    cp_async_wait<0>();
+  } else if (warp == kFinishers) {
+    // ---------------- MMA issue: the leading terms' ranks, then the second terms'
+    constexpr uint32_t idesc = idesc_bf16_f32(128, kCols) | (1u << 16);   // w: columns contiguous
+    const uint64_t v0 = smem_desc_sw128_kmajor(sv), w0 = desc_mn(sw, RP * 128);
+    for (int t = 0; t < n; ++t) {
+      bool ok = mbar_wait_warp(&ctl.w_full[t % WB], w_phase(t), &ctl.abort, a.err, kWaitLimitNs);
+      ok = mbar_wait_warp(&ctl.sum_free[t & 1], phase(t) ^ 1u, &ctl.abort, a.err, kWaitLimitNs) && ok;
+      if (!ok) break;
+      tc_fence_after_sync();
+      if (elect_one()) {
+        const uint64_t wt = w0 + (t % WB) * (kExpandW<RP> / 16);
+#pragma unroll
+        for (int k = 0; k < 2 * RP / 16; ++k)
+          tc_mma_ss(tmem + (t & 1) * kCols, v0 + ((k >> 2) * (kTcTile * 128 / 16) + 2 * (k & 3)),
+                    wt + (k % (RP / 16)) * 128, idesc, k != 0);
+        tc_commit(&ctl.w_free[t % WB]);
+        tc_commit(&ctl.sum_full[t & 1]);
+      }
+      __syncwarp();
+    }
+  } else {
+    // ---------------- V, and w ahead of the MMAs
+    const int lt = tid - 32 * (kFinishers + 1);
+    constexpr int kLt = 32 * kLoaders, kRow = 2 * RP / 8;   // threads; 16-byte pieces of a row of V
+    const int rank = a.ad.rank(tile.x);
+    const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * a.ad.r * a.K;
+    for (int p = lt; p < kTcTile * kRow; p += kLt) {
+      const int m = p / kRow, c = p % kRow;
+      const bool v = m < tile.z;
+      cp_async16(sv + (c >> 3) * (kTcTile * 128) + tile_off(m, c & 7),
+                 a.terms + static_cast<int64_t>(tile.y + (v ? m : 0)) * a.row_terms + 8 * c, v);
+    }
+    const int pc = lt & 15, pr = lt >> 4;
+    // (with one stage each tile's copies are waited for at once, else a tile later)
+    for (int t = 0; t < n + WB - 1; ++t) {
+      if (t < n) {
+        // the stage's tile before, if any, has been multiplied
+        mbar_wait(&ctl.w_free[t % WB], w_phase(t) ^ 1u, &ctl.abort, a.err, kWaitLimitNs);
+        const int e = column(t) + 8 * pc;
+#pragma unroll
+        for (int i = 0; i < RP * 16 / kLt; ++i) {
+          const int wr = pr + kLt / 16 * i;
+          const bool v = wr < rank && e < a.K;
+          cp_async16(sw + (t % WB) * kExpandW<RP> + (pc >> 3) * (RP * 128) + tile_off(wr, pc & 7),
+                     v ? w + static_cast<int64_t>(wr) * a.K + e : w, v);
+        }
+      }
+      cp_async_commit();
+      const int come = t - (WB - 1);   // this tile (and V) has come
+      if (come >= 0) {
+        cp_async_wait<WB - 1>();
+        fence_proxy_async_smem();
+        mbar_arrive(&ctl.w_full[come % WB]);
       }
     }
-    cp_async_commit();
-  };
-  constexpr int YB = kExpandYs<RP>;
-  const auto load_base = [&](int t) {
-    if (t < n) {
-      const uint32_t to = sy + (t % YB) * kExpandY;
-      const int e = column(t) + 8 * pc;
-#pragma unroll
-      for (int i = 0; i < kTcTile / kExpandRows; ++i) {
-        const int m = prow + kExpandRows * i;
-        const bool v = a.base != nullptr && m < tile.z && e < a.K;
-        cp_async16(to + m * 256 + ((pc ^ (m & 7)) << 4),
-                   v ? a.base + token[m] * a.ldbase + e : a.w, v);
-      }
-    }
-    cp_async_commit();
-  };
-  constexpr int kRow = 2 * RP / 8;   // 16-byte pieces of a row of V
-  for (int p = tid; p < kTcTile * kRow; p += kExpandThreads) {
-    const int m = p / kRow, c = p % kRow;
-    const bool v = m < tile.z;
-    cp_async16(sv + (c >> 3) * (kTcTile * 128) + tile_off(m, c & 7),
-               a.terms + static_cast<int64_t>(tile.y + (v ? m : 0)) * a.row_terms + 8 * c, v);
+    cp_async_wait<0>();
   }
-  load_w(0);      // one group with V's
-  load_w(1);
-  load_base(0);
-  if (YB == 2) load_base(1);
-  constexpr uint32_t idesc = idesc_bf16_f32(128, kCols) | (1u << 16);   // w: columns contiguous
-  bool ok = true;
-  for (int t = 0; t <= n; ++t) {
-    if (t < n) {
-      // w of tile t; the groups after it are a base and, at the start, w of tile 1
-      // and all bases that there is room for
-      if (t == 0) cp_async_wait<YB + 1>();
-      else if (t == 1) cp_async_wait<YB>();
-      else cp_async_wait<1>();
-      fence_proxy_async_smem();
-      __syncthreads();
-      if (tid == 0) {
-        tc_fence_after_sync();
-        const uint32_t wt = sw + (t & 1) * kExpandW<RP>;
-#pragma unroll
-        for (int k = 0; k < 2 * RP / 16; ++k)   // the leading terms' ranks, then the second terms'
-          tc_mma_ss(tmem + (t & 1) * kCols,
-                    smem_desc_sw128_kmajor(sv + (k >> 2) * (kTcTile * 128) + 32 * (k & 3)),
-                    desc_mn(wt + (k % (RP / 16)) * 2048, RP * 128), idesc, k != 0);
-        tc_commit(&bar[t & 1]);
-      }
-    }
-    if (t == 0) continue;
-    const int q = t - 1;   // the tile to finish
-    // its base (with two buffers, later on, it came before w of tile t)
-    if (YB == 1 || t == n) cp_async_wait<0>();
-    else if (t == 1) cp_async_wait<1>();
-    ok = mbar_wait(&bar[q & 1], static_cast<uint32_t>(q >> 1) & 1u, nullptr, a.err, kWaitLimitNs);
-    if (!__syncthreads_and(ok)) break;
-    tc_fence_after_sync();
-    load_w(t + 1);         // over tile q's, which its MMAs have read
-    const int m = 32 * (warp & 3) + lane;
-    uint8_t* ytile = ybuf + (q % YB) * kExpandY;
-    uint8_t* yrow = ytile + m * 256;
-    const int c = 32 * (warp >> 2);   // of the tile's columns
-    uint32_t v[32];
-    tmem_ld_32x32b_x32(tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + (q & 1) * kCols + c, v);
-    tmem_wait_ld();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint4* p = reinterpret_cast<uint4*>(yrow + (((c >> 3) + i) ^ (m & 7)) * 16);
-      uint4 b = *p;
-      uint32_t* u = reinterpret_cast<uint32_t*>(&b);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        u[j] = pack_bf16x2(__uint_as_float(v[8 * i + 2 * j]) + __uint_as_float(u[j] << 16),
-                           __uint_as_float(v[8 * i + 2 * j + 1]) + __uint_as_float(u[j] & 0xFFFF0000u));
-      *p = b;
-    }
-    tc_fence_before_sync();
-    __syncthreads();
-    const int e = column(q) + 8 * pc;
-    if (e < a.K) {
-#pragma unroll
-      for (int i = 0; i < kTcTile / kExpandRows; ++i) {
-        const int row = prow + kExpandRows * i;
-        if (row < tile.z)
-          *reinterpret_cast<uint4*>(a.y + token[row] * a.ldy + e) = *reinterpret_cast<const uint4*>(
-              ytile + row * 256 + ((pc ^ (row & 7)) << 4));
-      }
-    }
-    // the pieces that this thread copied out are those that it copies in
-    load_base(q + YB);
-  }
-  cp_async_wait<0>();
+  // (after a wait that ran out, MMAs may be under way: they are given their time)
+  if (*static_cast<volatile int*>(&ctl.abort) && warp == kFinishers)
+    mbar_wait(&ctl.sum_full[0], phase(n), nullptr, a.err, kWaitLimitNs);
   tc_end<2 * kCols>(tmem);
 }
 
@@ -1321,15 +1381,16 @@ __global__ void __launch_bounds__(kThreads) grad_tc_kernel(const __grid_constant
     __syncthreads();
     if (tid == 0) {
       tc_fence_after_sync();
-      const uint32_t st = ring + (ci % S) * kGradStage<RP>, su = st + kCt / 64 * kGradBlock;
+      const uint64_t x0 = desc_mn(ring + (ci % S) * kGradStage<RP>, kGradBlock);
+      const uint64_t u0 = x0 + kCt / 64 * kGradBlock / 16;
 #pragma unroll
       for (int ks = 0; ks < kGradTokens / 16; ++ks)
 #pragma unroll
         for (int m = 0; m < kCt / 128; ++m)
 #pragma unroll
           for (int q = 0; q < kMmas; ++q)
-            tc_mma_ss(tmem + m * kD + (ci & 1) * RP + q * kN, desc_mn(st + 2 * m * kGradBlock + ks * 2048, kGradBlock),
-                      desc_mn(su + q * (kN / 64) * kGradBlock + ks * 2048, kGradBlock), idesc, (ci | ks) != 0);
+            tc_mma_ss(tmem + m * kD + (ci & 1) * RP + q * kN, x0 + (2 * m * kGradBlock + ks * 2048) / 16,
+                      u0 + (q * (kN / 64) * kGradBlock + ks * 2048) / 16, idesc, (ci | ks) != 0);
       tc_commit(&bar[ci % S]);
     }
     if (ci + S - 1 < n) {
@@ -1385,6 +1446,7 @@ struct Plan {
   int tile, max_tiles, max_items, tokens_per_item;
   int splits_in, per_in, splits_out, per_out;   // shrink over K_in, over K_out
   size_t counts, perm, tiles, items, begin, v, du, v_terms, du_terms, part_a, part_b, total;
+  int cluster_in, cluster_out;                  // CTAs of a cluster of shrink, where tc
 };
 
 void cut(int64_t K, int tiles, int ctas, int most, int* splits, int* per) {
@@ -1397,6 +1459,15 @@ void cut(int64_t K, int tiles, int ctas, int most, int* splits, int* per) {
   *splits = (chunks + *per - 1) / *per;
 }
 
+// CTAs of a cluster of the tensor-core shrink: a power of two of at most eight, no
+// more than K has chunks, and no more clusters than the SMs hold at once.
+int cluster_of(int64_t K, int64_t r, int tiles) {
+  const int64_t chunks = (K + kChunk - 1) / kChunk, slots = (r > 64 ? 2 : 3) * device_sm_count();
+  int c = 1;
+  while (c < 8 && 2 * c <= chunks && 2 * c * tiles <= slots) c *= 2;
+  return c;
+}
+
 int64_t padded_rank(int64_t r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }
 
 Plan make_plan(int64_t T, int64_t n, int64_t r, int64_t K_in, int64_t K_out, bool backward, bool tc) {
@@ -1406,9 +1477,10 @@ Plan make_plan(int64_t T, int64_t n, int64_t r, int64_t K_in, int64_t K_out, boo
   const int64_t used = n < T ? n : T;
   p.max_tiles = static_cast<int>((T + p.tile - 1) / p.tile + used + 1);
   const int most = T <= 64 ? 32 : 8;
-  const int ctas = tc && r > 64 ? 1 : 3;   // of shrink, resident on an SM
-  cut(K_in, p.max_tiles, ctas, most, &p.splits_in, &p.per_in);
-  cut(K_out, p.max_tiles, ctas, most, &p.splits_out, &p.per_out);
+  cut(K_in, p.max_tiles, 3, most, &p.splits_in, &p.per_in);
+  cut(K_out, p.max_tiles, 3, most, &p.splits_out, &p.per_out);
+  p.cluster_in = cluster_of(K_in, r, p.max_tiles);
+  p.cluster_out = cluster_of(K_out, r, p.max_tiles);
   // grad: about two CTAs an SM over the columns of both gradients
   const int64_t ct = tc && r <= 64 ? 256 : kCols;
   const int64_t column_tiles = (K_in + ct - 1) / ct + (K_out + ct - 1) / ct;
@@ -1432,11 +1504,15 @@ Plan make_plan(int64_t T, int64_t n, int64_t r, int64_t K_in, int64_t K_out, boo
   p.begin = take(sizeof(int) * static_cast<size_t>(n + 1));
   const size_t row = sizeof(float) * static_cast<size_t>(T) * static_cast<size_t>(r);
   const size_t term = sizeof(__nv_bfloat16) * static_cast<size_t>(T * padded_rank(r));
-  p.v = take(row * p.splits_in);
-  if (tc) p.v_terms = take(term * (backward ? 3 : 2));
+  if (tc)
+    p.v_terms = take(term * (backward ? 3 : 2));
+  else
+    p.v = take(row * p.splits_in);
   if (backward) {
-    p.du = take(row * p.splits_out);
-    if (tc) p.du_terms = take(term * 3);
+    if (tc)
+      p.du_terms = take(term * 3);
+    else
+      p.du = take(row * p.splits_out);
     const size_t part = sizeof(float) * static_cast<size_t>(p.max_items) * static_cast<size_t>(r);
     p.part_a = take(part * static_cast<size_t>(K_in));
     p.part_b = take(part * static_cast<size_t>(K_out));
@@ -1475,7 +1551,8 @@ bool rows_aligned(const void* p, int64_t ld, int64_t K, size_t elem, size_t byte
 }
 
 cudaError_t run_route(const AdapterProblem& p, const Plan& pl, const Route& r, cudaStream_t s) {
-  const size_t smem = sizeof(int) * (32 * static_cast<size_t>(p.n + 1) + 3 * static_cast<size_t>(p.n + 2));
+  const size_t smem = sizeof(int) * (32 * static_cast<size_t>(p.n + 1) + 3 * static_cast<size_t>(p.n + 2) +
+                                     32 * static_cast<size_t>(kRouteKept));
   return go<route_kernel>(dim3(1), 1024, smem, s, p.ids, static_cast<int>(p.T),
             static_cast<int>(p.n), pl.tile, pl.tokens_per_item, r);
 }
@@ -1486,15 +1563,9 @@ cudaError_t run_shrink(const AdapterProblem& p, const Plan& pl, const Route& rou
   const int chunks = static_cast<int>((K + kChunk - 1) / kChunk);
   ShrinkArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, x,
                static_cast<const __nv_bfloat16*>(w), part, ldx, static_cast<int>(p.T),
-               static_cast<int>(K), chunks, per, splits, rows_aligned(x, ldx, K, dtype_size(dt), 16),
+               static_cast<int>(K), chunks, per, rows_aligned(x, ldx, K, dtype_size(dt), 16),
                rows_aligned(w, K, K, 2, 16)};
   const dim3 grid(pl.max_tiles, splits);
-  if (pl.tc)
-    return by_rank(p.r, [&](auto rp) {
-      constexpr int RP = decltype(rp)::value;
-      return go<shrink_tc_kernel<RP>>(dim3(pl.max_tiles * splits), kThreads, 1024 + kShrinkStages * kShrinkStage<RP>, s, a,
-                device_error_word());
-    });
   return by_rank(p.r, [&](auto rp) {
     constexpr int RP = decltype(rp)::value;
     const int terms = dt == TBN_BF16 ? 1 : 3;
@@ -1531,16 +1602,42 @@ cudaError_t run_expand(const AdapterProblem& p, const Plan& pl, const Route& rou
   });
 }
 
-// Low-rank activations as bf16 terms, of `kTerms` a value.
+// Low-rank activations of x as bf16 terms, kTerms a value (unless w is nullptr),
+// and (v_in) others that are there already.
 template <int kTerms>
-cudaError_t run_terms(const AdapterProblem& p, const Plan& pl, const Route& route,
-                      const TermsSide* sides, int count, cudaStream_t s) {
-  const TermsArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, {sides[0], sides[count - 1]}};
-  int parts = (2 * device_sm_count() + pl.max_tiles - 1) / pl.max_tiles;   // blocks of a tile
-  if (parts > 8) parts = 8;
+cudaError_t run_shrink_tc(const AdapterProblem& p, const Plan& pl, const Route& route, const void* x,
+                          int64_t ldx, const void* w, int64_t K, int cluster, __nv_bfloat16* terms,
+                          float* v_out, const float* v_in, __nv_bfloat16* v_terms, cudaStream_t s) {
+  // as many rows as L2 keeps beside the rest
+  const int64_t fit = w != nullptr ? kPrefetchBytes / (2 * K) : 0;
+  const int prefetch = static_cast<int>(fit < p.T ? fit : p.T);
+  const ShrinkTcArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)},
+                       static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(w), terms,
+                       v_out, ldx, static_cast<int>(K), static_cast<int>((K + kChunk - 1) / kChunk),
+                       cluster, w != nullptr ? pl.max_tiles : 0, prefetch, v_in, v_terms,
+                       device_error_word()};
   return by_rank(p.r, [&](auto rp) {
-    return go<terms_kernel<decltype(rp)::value, kTerms>>(dim3(pl.max_tiles, parts, count), kThreads, 0,
-                                                         s, a);
+    constexpr int RP = decltype(rp)::value;
+    static const cudaError_t allowed = cudaFuncSetAttribute(
+        reinterpret_cast<const void*>(shrink_tc_kernel<RP, kTerms>),
+        cudaFuncAttributeMaxDynamicSharedMemorySize, kShrinkSmem<RP>);
+    if (allowed != cudaSuccess) return allowed;
+    cudaLaunchConfig_t cfg{};
+    const int jobs = (w != nullptr ? 1 : 0) + (v_in != nullptr ? 1 : 0);
+    cfg.gridDim = dim3(static_cast<unsigned>(pl.max_tiles) * cluster * jobs);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kShrinkSmem<RP>;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, shrink_tc_kernel<RP, kTerms>, a);
   });
 }
 
@@ -1637,21 +1734,21 @@ tbn_status launch_adapter_fwd(const AdapterProblem& p, void* ws, cudaStream_t s)
   const Plan pl = make_plan(p.T, p.n, p.r, p.K_in, p.K_out, false, takes_tc(p, false));
   const Route route = route_at(pl, ws);
   uint8_t* b = static_cast<uint8_t*>(ws);
-  float* part = reinterpret_cast<float*>(b + pl.v);
   cudaError_t e = run_route(p, pl, route, s);
   if (e != cudaSuccess) return cuda_fail(e, "adapter route_kernel");
+  if (pl.tc) {
+    __nv_bfloat16* terms = reinterpret_cast<__nv_bfloat16*>(b + pl.v_terms);
+    e = run_shrink_tc<2>(p, pl, route, p.x, p.ldx, p.a, p.K_in, pl.cluster_in, terms, p.v_out, nullptr,
+                         nullptr, s);
+    if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_tc_kernel");
+    e = run_expand_tc(p, pl, route, terms, 2, p.b, p.K_out, p.base, p.ldbase, p.y, p.ldy, s);
+    return e == cudaSuccess ? TBN_OK : cuda_fail(e, "adapter expand_tc_kernel");
+  }
+  float* part = reinterpret_cast<float*>(b + pl.v);
   e = run_shrink(p, pl, route, p.x, p.xdt, p.ldx, p.a, p.K_in, pl.splits_in, pl.per_in, part, s);
   if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_kernel");
   const LowRank v{part, p.T * p.r, pl.splits_in, 0};
-  if (pl.tc) {
-    __nv_bfloat16* terms = reinterpret_cast<__nv_bfloat16*>(b + pl.v_terms);
-    const TermsSide side{v, terms, p.v_out};
-    e = run_terms<2>(p, pl, route, &side, 1, s);
-    if (e != cudaSuccess) return cuda_fail(e, "adapter terms_kernel");
-    e = run_expand_tc(p, pl, route, terms, 2, p.b, p.K_out, p.base, p.ldbase, p.y, p.ldy, s);
-  } else {
-    e = run_expand(p, pl, route, v, p.b, p.K_out, p.base, p.ldbase, p.y, p.ydt, p.ldy, p.v_out, s);
-  }
+  e = run_expand(p, pl, route, v, p.b, p.K_out, p.base, p.ldbase, p.y, p.ydt, p.ldy, p.v_out, s);
   return e == cudaSuccess ? TBN_OK : cuda_fail(e, "adapter expand_kernel");
 }
 
@@ -1668,7 +1765,17 @@ tbn_status launch_adapter_bwd(const AdapterProblem& p, void* ws, cudaStream_t s)
   if (e != cudaSuccess) return cuda_fail(e, "adapter route_kernel");
   LowRank v{p.v, 0, 1, 1};
   const LowRank u{dupart, p.T * p.r, pl.splits_out, 0};
-  if (p.T > 0) {
+  if (pl.tc) {
+    // du, and v's terms beside it; v itself first where it is not there
+    if (p.db != nullptr && p.v == nullptr)
+      e = run_shrink_tc<3>(p, pl, route, p.x, p.ldx, p.a, p.K_in, pl.cluster_in, v_terms, nullptr, nullptr,
+                           nullptr, s);
+    const float* v_in = p.db != nullptr ? p.v : nullptr;
+    if (e == cudaSuccess && (need_du || v_in != nullptr))
+      e = run_shrink_tc<3>(p, pl, route, p.dy, p.lddy, need_du ? p.b : nullptr, p.K_out, pl.cluster_out,
+                           du_terms, nullptr, v_in, v_terms, s);
+    if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_tc_kernel");
+  } else if (p.T > 0) {
     if (need_du) {
       e = run_shrink(p, pl, route, p.dy, p.ydt, p.lddy, p.b, p.K_out, pl.splits_out, pl.per_out,
                      dupart, s);
@@ -1678,14 +1785,6 @@ tbn_status launch_adapter_bwd(const AdapterProblem& p, void* ws, cudaStream_t s)
       e = run_shrink(p, pl, route, p.x, p.xdt, p.ldx, p.a, p.K_in, pl.splits_in, pl.per_in, vpart, s);
       if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_kernel");
       v = {vpart, p.T * p.r, pl.splits_in, 0};
-    }
-    if (pl.tc && (need_du || p.db != nullptr)) {
-      TermsSide both[2];
-      int many = 0;
-      if (need_du) both[many++] = {u, du_terms, nullptr};
-      if (p.db != nullptr) both[many++] = {v, v_terms, nullptr};
-      e = run_terms<3>(p, pl, route, both, many, s);
-      if (e != cudaSuccess) return cuda_fail(e, "adapter terms_kernel");
     }
   }
   GradSide sides[2];
@@ -1701,6 +1800,7 @@ tbn_status launch_adapter_bwd(const AdapterProblem& p, void* ws, cudaStream_t s)
     sides[count++] = grad_side(v, v_terms, p.dy, p.ydt, p.lddy, p.K_out,
                                reinterpret_cast<float*>(b + pl.part_b), p.db);
   }
+  e = cudaSuccess;
   if (pl.tc && count > 0) {
     e = run_grads_tc(p, pl, route, sides, count, s);
   } else if (p.T > 0) {
