@@ -795,8 +795,10 @@ __device__ __forceinline__ uint64_t desc_mn(uint32_t saddr, uint32_t block) {
   return d;
 }
 
-// What each tensor-core kernel begins and ends with: its tensor memory (kCols
-// columns) and `bars` barriers that one arrival completes.
+// What each tensor-core kernel begins and ends with: its tensor memory and `bars`
+// barriers that one arrival completes.  It begins before the dependency wait and
+// lets its dependents start behind it: a dependent that took tensor memory before
+// the kernel that it waits for has its own would wait for ever.
 template <int kTmemCols>
 __device__ __forceinline__ uint32_t tc_begin(uint32_t* slot, uint64_t* bar, int bars) {
   if (threadIdx.x < 32) {
@@ -897,6 +899,7 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const __grid_consta
   // nothing, so that it may stand before the wait)
   for (int i = blockIdx.x + gridDim.x * threadIdx.x; i < a.prefetch_rows; i += gridDim.x * kThreads)
     bulk_prefetch(a.x + i * a.ldx, a.K * 2);
+  const uint32_t tmem = tc_begin<kTmem>(&slot, bar, S);
   grid_dependency_wait();
   grid_dependents_launch();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, ch = tid & 7;
@@ -904,14 +907,15 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const __grid_consta
   int tile_id = blockIdx.x / a.splits;
   const bool second = tile_id >= a.max_tiles;
   if (second) tile_id -= a.max_tiles;
-  if (tile_id >= a.route.counts[0]) return;   // all CTAs of the cluster alike
+  // (all CTAs of the cluster alike)
+  if (tile_id >= a.route.counts[0]) return tc_end<kTmem>(tmem);
   const int4 tile = a.route.tiles[tile_id];
   const int r = a.ad.r;
   if (tile.x < 0) {
     if (a.v_out != nullptr && !second)
       for (int i = split * kThreads + tid; i < tile.z * r; i += a.splits * kThreads)
         a.v_out[static_cast<int64_t>(a.route.perm[tile.y + i / r]) * r + i % r] = 0.0f;
-    return;
+    return tc_end<kTmem>(tmem);
   }
   const int rank = a.ad.rank(tile.x);
   const float factor = a.ad.factor(tile.x);
@@ -926,9 +930,8 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const __grid_consta
         if (col + j < rank) v[j] = p[j];
       write_terms<RP, kTerms>(v, factor, col, rank, tile.y + m, a.v_terms);
     }
-    return;
+    return tc_end<kTmem>(tmem);
   }
-  const uint32_t tmem = tc_begin<kTmem>(&slot, bar, S);
   uint8_t* smem = align_1k(smem_raw);
   const uint32_t ring = smem_addr(smem);
   const int n = (a.chunks - split + a.splits - 1) / a.splits;   // chunks split, split + splits, ...
@@ -1085,7 +1088,8 @@ static_assert(sizeof(ExpandControl) <= 1024, "control");
 template <int RP>
 __global__ void __launch_bounds__(kExpandThreads, RP <= 64 ? 2 : 1)
     expand_tc_kernel(const __grid_constant__ ExpandTcArgs a) {
-  extern __shared__ __align__(1024) uint8_t smem[];
+  extern __shared__ __align__(1024) uint8_t expand_smem[];
+  uint8_t* smem = expand_smem;
   // without static variables the dynamic ones begin at a multiple of 1024 bytes;
   // the kilobyte behind the tiles holds the rest
   ExpandControl& ctl = *reinterpret_cast<ExpandControl*>(smem + kExpandSmem<RP> - 1024);
@@ -1094,20 +1098,30 @@ __global__ void __launch_bounds__(kExpandThreads, RP <= 64 ? 2 : 1)
     if (threadIdx.x == 0) raise_device_error(a.err, TBN_DEVERR_BAD_LAUNCH);
     return;
   }
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    ctl.abort = 0;
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&ctl.w_full[i], 32 * kLoaders);
+      mbar_init(&ctl.w_free[i], 1);
+      mbar_init(&ctl.sum_full[i], 1);
+      mbar_init(&ctl.sum_free[i], kFinishers);
+    }
+  }
+  const uint32_t tmem = tc_begin<2 * kCols>(&ctl.slot, nullptr, 0);
   grid_dependency_wait();
   grid_dependents_launch();
   // the tiles without adapter are the list's last and are copied here first, beside
   // the others' work
   const int tile_id = a.route.counts[0] - 1 - static_cast<int>(blockIdx.x / a.groups);
   const int group = blockIdx.x % a.groups;
-  if (tile_id < 0) return;
+  if (tile_id < 0) return tc_end<2 * kCols>(tmem);
   const int4 tile = a.route.tiles[tile_id];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   int* token = ctl.token;
   if (tid < kTcTile) token[tid] = tid < tile.z ? a.route.perm[tile.y + tid] : 0;
+  __syncthreads();
   if (tile.x < 0) {   // no adapter: the base, or zeros
-    if (a.base == a.y && a.ldbase == a.ldy) return;
-    __syncthreads();
+    if (a.base == a.y && a.ldbase == a.ldy) return tc_end<2 * kCols>(tmem);
     constexpr int kRows = kExpandThreads / 16, kOnce = 5;   // rows of a pass; passes at once
     for (int c = group * kCols + 8 * (tid & 15); c < a.K; c += a.groups * kCols)
       for (int m0 = tid >> 4; m0 < tile.z; m0 += kOnce * kRows) {
@@ -1125,18 +1139,8 @@ __global__ void __launch_bounds__(kExpandThreads, RP <= 64 ? 2 : 1)
           if (m < tile.z) *reinterpret_cast<uint4*>(a.y + token[m] * a.ldy + c) = d[i];
         }
       }
-    return;
+    return tc_end<2 * kCols>(tmem);
   }
-  if (tid == 0) {
-    ctl.abort = 0;
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&ctl.w_full[i], 32 * kLoaders);
-      mbar_init(&ctl.w_free[i], 1);
-      mbar_init(&ctl.sum_full[i], 1);
-      mbar_init(&ctl.sum_free[i], kFinishers);
-    }
-  }
-  const uint32_t tmem = tc_begin<2 * kCols>(&ctl.slot, nullptr, 0);
   uint8_t* ybuf = smem + kExpandV<RP> + WB * kExpandW<RP>;
   const uint32_t sv = smem_addr(smem), sw = sv + kExpandV<RP>;
   const int tiles = (a.K + kCols - 1) / kCols, n = (tiles - group + a.groups - 1) / a.groups;
@@ -1310,15 +1314,15 @@ __global__ void __launch_bounds__(kThreads) grad_tc_kernel(const __grid_constant
   constexpr int kXRows = kThreads / (kCt / 8), kXPasses = kGradTokens / kXRows;   // rows of a pass
   constexpr int kURow = N / 8;                                           // pieces of a row of u
   constexpr int kUPasses = (kGradTokens * kURow + kThreads - 1) / kThreads;
+  const uint32_t tmem = tc_begin<kTmem>(&slot, bar, S);
   grid_dependency_wait();
   grid_dependents_launch();
   const int item_id = blockIdx.x / a.tiles, column = blockIdx.x % a.tiles;
-  if (item_id >= a.route.counts[1]) return;
+  if (item_id >= a.route.counts[1]) return tc_end<kTmem>(tmem);
   const int4 item = a.route.items[item_id];
   const bool first = column < a.tiles0;
   const GradSide& sd = a.side[first ? 0 : 1];
   const int c0 = (first ? column : column - a.tiles0) * kCt;
-  const uint32_t tmem = tc_begin<kTmem>(&slot, bar, S);
   const uint32_t ring = smem_addr(align_1k(smem_raw));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   // the odd stages' leading sums begin in the middle of an MMA's columns: zeros
