@@ -768,7 +768,6 @@ __global__ void __launch_bounds__(256) grad_reduce_kernel(const __grid_constant_
 constexpr int kTcTile = 128;
 constexpr int64_t kTcFrom = 128;   // tokens
 constexpr int64_t kPrefetchBytes = int64_t(80) << 20;   // of the 129 MB of L2
-constexpr int kExpandCtas = 4;      // of expand, an SM and launch
 constexpr int kGradCtas = 2;        // of grad
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
 
@@ -1051,7 +1050,7 @@ struct ExpandTcArgs {
   const __nv_bfloat16* base;    // or nullptr
   __nv_bfloat16* y;
   int64_t ldbase, ldy;
-  int row_terms, K, groups;     // CTAs of a tile
+  int row_terms, K;
   uint32_t* err;
 };
 
@@ -1064,29 +1063,47 @@ template <int RP>
 constexpr int kExpandWs = RP == 64 ? 1 : 2;       // stages of w: as many as leave room for two CTAs
 template <int RP>
 constexpr int kExpandSmem = kExpandV<RP> + kExpandWs<RP> * kExpandW<RP> + 2 * kExpandY + 1024;
+template <int RP>
+constexpr int kExpandCtas = RP <= 64 ? 2 : 1;     // on an SM
 constexpr int kFinishers = 8;                     // warps
 constexpr int kLoaders = 4;                       // warps
 constexpr int kExpandThreads = 32 * (kFinishers + 1 + kLoaders);
 
-// CTA (tile, column tiles group, group + groups, ...), two on an SM up to rank
-// 64.  V is the K-major operand, w the other, ranks as steps.  Its warps wait for
-// one another only through barriers in shared memory: four load V and w, one
-// issues the MMAs into two sums in turn, and eight finish 32 tokens x 64 columns
-// each, by themselves: their part of the base comes by cp.async, a thread adds its
-// token's sums to it (16-byte chunk c of row m at c ^ (m & 7)), and the warp writes
-// it out in rows of 128 bytes.  (With block-wide barriers between these steps 60 us
-// at 8209 x 8192, rank 64, a third of it the steps' latencies; with rows read and
-// written by their own threads, a tag lookup a sector, 88.)
 struct ExpandControl {
   uint64_t w_full[2], w_free[2], sum_full[2], sum_free[2];
   uint32_t slot;
   int abort;
-  int token[kTcTile];
 };
 static_assert(sizeof(ExpandControl) <= 1024, "control");
 
+// A part of a CTA's share: column tiles [first, first + count) of a tile of tokens.
+struct Segment {
+  int4 tile;
+  int first, count;
+};
+
+// The share of a CTA in the launch's work, all column tiles of all token tiles in
+// order, cut evenly: the next segment from unit `u` on.
+__device__ __forceinline__ Segment next_segment(const Route& r, int columns, int64_t& u, int64_t end) {
+  const int id = static_cast<int>(u / columns), first = static_cast<int>(u - static_cast<int64_t>(id) * columns);
+  const int64_t left = end - u;
+  const int count = left < columns - first ? static_cast<int>(left) : columns - first;
+  u += count;
+  return {r.tiles[id], first, count};
+}
+
+// V is the K-major operand, w the other, ranks as steps.  As many CTAs as fit stay
+// and take an equal share of the work each (with a CTA for some columns of a token
+// tile the last wave of them left a tenth to a third of the machine idle).  A CTA's
+// warps wait for one another only through barriers in shared memory: four load V
+// and w, one issues the MMAs into two sums in turn, and eight finish 32 tokens x 64
+// columns each, by themselves: their part of the base comes by cp.async, a thread
+// adds its token's sums to it (16-byte chunk c of row m at c ^ (m & 7)), and the
+// warp writes it out in rows of 128 bytes.  (With block-wide barriers between these
+// steps 60 us at 8209 x 8192, rank 64, a third of it the steps' latencies; with rows
+// read and written by their own threads, a tag lookup a sector, 88.)
 template <int RP>
-__global__ void __launch_bounds__(kExpandThreads, RP <= 64 ? 2 : 1)
+__global__ void __launch_bounds__(kExpandThreads, kExpandCtas<RP>)
     expand_tc_kernel(const __grid_constant__ ExpandTcArgs a) {
   extern __shared__ __align__(1024) uint8_t expand_smem[];
   uint8_t* smem = expand_smem;
@@ -1111,42 +1128,14 @@ __global__ void __launch_bounds__(kExpandThreads, RP <= 64 ? 2 : 1)
   const uint32_t tmem = tc_begin<2 * kCols>(&ctl.slot, nullptr, 0);
   grid_dependency_wait();
   grid_dependents_launch();
-  // the tiles without adapter are the list's last and are copied here first, beside
-  // the others' work
-  const int tile_id = a.route.counts[0] - 1 - static_cast<int>(blockIdx.x / a.groups);
-  const int group = blockIdx.x % a.groups;
-  if (tile_id < 0) return tc_end<2 * kCols>(tmem);
-  const int4 tile = a.route.tiles[tile_id];
-  int* token = ctl.token;
-  if (tid < kTcTile) token[tid] = tid < tile.z ? a.route.perm[tile.y + tid] : 0;
-  __syncthreads();
-  if (tile.x < 0) {   // no adapter: the base, or zeros
-    if (a.base == a.y && a.ldbase == a.ldy) return tc_end<2 * kCols>(tmem);
-    constexpr int kRows = kExpandThreads / 16, kOnce = 5;   // rows of a pass; passes at once
-    for (int c = group * kCols + 8 * (tid & 15); c < a.K; c += a.groups * kCols)
-      for (int m0 = tid >> 4; m0 < tile.z; m0 += kOnce * kRows) {
-        uint4 d[kOnce];
-#pragma unroll
-        for (int i = 0; i < kOnce; ++i) {
-          const int m = m0 + i * kRows;
-          d[i] = make_uint4(0u, 0u, 0u, 0u);
-          if (a.base != nullptr && m < tile.z)
-            d[i] = *reinterpret_cast<const uint4*>(a.base + token[m] * a.ldbase + c);
-        }
-#pragma unroll
-        for (int i = 0; i < kOnce; ++i) {
-          const int m = m0 + i * kRows;
-          if (m < tile.z) *reinterpret_cast<uint4*>(a.y + token[m] * a.ldy + c) = d[i];
-        }
-      }
-    return tc_end<2 * kCols>(tmem);
-  }
   uint8_t* ybuf = smem + kExpandV<RP> + WB * kExpandW<RP>;
   const uint32_t sv = smem_addr(smem), sw = sv + kExpandV<RP>;
-  const int tiles = (a.K + kCols - 1) / kCols, n = (tiles - group + a.groups - 1) / a.groups;
-  const auto column = [&](int t) { return (group + t * a.groups) * kCols; };
-  // tile t is the (t / 2)-th use of its sums and the (t / WB)-th of its stage of w:
-  // the barriers' phases
+  const int columns = (a.K + kCols - 1) / kCols;
+  const int64_t all = static_cast<int64_t>(a.route.counts[0]) * columns;
+  int64_t u = all * blockIdx.x / gridDim.x;
+  const int64_t end = all * (blockIdx.x + 1) / gridDim.x;
+  int done = 0;   // column tiles multiplied so far, which the barriers' phases go by:
+  // tile t is the (t / 2)-th use of its sums and the (t / WB)-th of its stage of w
   const auto phase = [](int t) { return static_cast<uint32_t>(t >> 1) & 1u; };
   const auto w_phase = [](int t) { return static_cast<uint32_t>(t / WB) & 1u; };
   if (warp < kFinishers) {
@@ -1155,126 +1144,150 @@ __global__ void __launch_bounds__(kExpandThreads, RP <= 64 ? 2 : 1)
     uint8_t* mine = ybuf + warp * 4096;                 // of each buffer: 32 rows of 128 bytes
     const int pc = lane & 7, pr = lane >> 3;            // pieces: chunk pc of rows pr + 4 i
     const uint32_t acc = tmem + (static_cast<uint32_t>(r0) << 16) + c0;
-    const auto load_base = [&](int t) {
-      if (t < n) {
-        const int e = column(t) + c0 + 8 * pc;
-        const uint32_t to = smem_addr(mine) + (t % YB) * kExpandY;
+    while (u < end) {
+      const Segment sg = next_segment(a.route, columns, u, end);
+      const bool has = sg.tile.x >= 0;
+      if (!has && a.base == a.y && a.ldbase == a.ldy) continue;
+      const int my_token = r0 + lane < sg.tile.z ? a.route.perm[sg.tile.y + r0 + lane] : -1;
+      int token[8];   // of rows pr + 4 i, -1: none
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int m = pr + 4 * i;
-          const bool v = a.base != nullptr && r0 + m < tile.z && e < a.K;
-          cp_async16(to + tile_off(m, pc), v ? a.base + token[r0 + m] * a.ldbase + e : a.w, v);
-        }
-      }
-      cp_async_commit();
-    };
-    for (int t = 0; t < YB; ++t) load_base(t);
-    for (int t = 0; t < n; ++t) {
-      cp_async_wait<YB - 1>();
-      __syncwarp();
-      mbar_wait(&ctl.sum_full[t & 1], phase(t), &ctl.abort, a.err, kWaitLimitNs);
-      tc_fence_after_sync();
-      uint8_t* rows = mine + (t % YB) * kExpandY;
+      for (int i = 0; i < 8; ++i) token[i] = __shfl_sync(0xffffffffu, my_token, pr + 4 * i);
+      const auto load_base = [&](int t) {
+        if (t < sg.count) {
+          const int e = (sg.first + t) * kCols + c0 + 8 * pc;
+          const uint32_t to = smem_addr(mine) + (t % YB) * kExpandY;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t v[32];
-        tmem_ld_32x32b_x32(acc + (t & 1) * kCols + 32 * h, v);
-        tmem_wait_ld();
-        if (h == 1) {
-          tc_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&ctl.sum_free[t & 1]);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint4* p = reinterpret_cast<uint4*>(rows + tile_off(lane, 4 * h + i));
-          uint4 b = *p;
-          uint32_t* u = reinterpret_cast<uint32_t*>(&b);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint64_t f = add_f32x2(f32x2(v[8 * i + 2 * j], v[8 * i + 2 * j + 1]),
-                                         f32x2(u[j] << 16, u[j] & 0xFFFF0000u));
-            u[j] = pack_bf16x2(__uint_as_float(static_cast<uint32_t>(f)),
-                               __uint_as_float(static_cast<uint32_t>(f >> 32)));
+          for (int i = 0; i < 8; ++i) {
+            const bool v = a.base != nullptr && token[i] >= 0 && e < a.K;
+            cp_async16(to + tile_off(pr + 4 * i, pc), v ? a.base + token[i] * a.ldbase + e : a.w, v);
           }
-          *p = b;
         }
-      }
-      __syncwarp();
-      const int e = column(t) + c0 + 8 * pc;
-      if (e < a.K) {
+        cp_async_commit();
+      };
+      for (int t = 0; t < YB; ++t) load_base(t);
+      for (int t = 0; t < sg.count; ++t) {
+        cp_async_wait<YB - 1>();
+        __syncwarp();
+        uint8_t* rows = mine + (t % YB) * kExpandY;
+        if (has) {
+          const int d = done + t;
+          mbar_wait(&ctl.sum_full[d & 1], phase(d), &ctl.abort, a.err, kWaitLimitNs);
+          tc_fence_after_sync();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int m = pr + 4 * i;
-          if (r0 + m < tile.z)
-            *reinterpret_cast<uint4*>(a.y + token[r0 + m] * a.ldy + e) =
-                *reinterpret_cast<const uint4*>(rows + tile_off(m, pc));
+          for (int h = 0; h < 2; ++h) {
+            uint32_t v[32];
+            tmem_ld_32x32b_x32(acc + (d & 1) * kCols + 32 * h, v);
+            tmem_wait_ld();
+            if (h == 1) {
+              tc_fence_before_sync();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&ctl.sum_free[d & 1]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint4* p = reinterpret_cast<uint4*>(rows + tile_off(lane, 4 * h + i));
+              uint4 b = *p;
+              uint32_t* w = reinterpret_cast<uint32_t*>(&b);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const uint64_t f = add_f32x2(f32x2(v[8 * i + 2 * j], v[8 * i + 2 * j + 1]),
+                                             f32x2(w[j] << 16, w[j] & 0xFFFF0000u));
+                w[j] = pack_bf16x2(__uint_as_float(static_cast<uint32_t>(f)),
+                                   __uint_as_float(static_cast<uint32_t>(f >> 32)));
+              }
+              *p = b;
+            }
+          }
+          __syncwarp();
         }
+        const int e = (sg.first + t) * kCols + c0 + 8 * pc;
+        if (e < a.K) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (token[i] >= 0)
+              *reinterpret_cast<uint4*>(a.y + token[i] * a.ldy + e) =
+                  *reinterpret_cast<const uint4*>(rows + tile_off(pr + 4 * i, pc));
+        }
+        // the pieces that this lane copied out are those that it copies in
+        load_base(t + YB);
       }
-      // the pieces that this lane copied out are those that it copies in
-      load_base(t + YB);
+      cp_async_wait<0>();
+      if (has) done += sg.count;
     }
-    cp_async_wait<0>();
   } else if (warp == kFinishers) {
     // ---------------- MMA issue: the leading terms' ranks, then the second terms'
     constexpr uint32_t idesc = idesc_bf16_f32(128, kCols) | (1u << 16);   // w: columns contiguous
     const uint64_t v0 = smem_desc_sw128_kmajor(sv), w0 = desc_mn(sw, RP * 128);
-    for (int t = 0; t < n; ++t) {
-      bool ok = mbar_wait_warp(&ctl.w_full[t % WB], w_phase(t), &ctl.abort, a.err, kWaitLimitNs);
-      ok = mbar_wait_warp(&ctl.sum_free[t & 1], phase(t) ^ 1u, &ctl.abort, a.err, kWaitLimitNs) && ok;
-      if (!ok) break;
-      tc_fence_after_sync();
-      if (elect_one()) {
-        const uint64_t wt = w0 + (t % WB) * (kExpandW<RP> / 16);
+    bool ok = true;
+    while (u < end && ok) {
+      const Segment sg = next_segment(a.route, columns, u, end);
+      if (sg.tile.x < 0) continue;
+      for (int t = done; t < done + sg.count; ++t) {
+        ok = mbar_wait_warp(&ctl.w_full[t % WB], w_phase(t), &ctl.abort, a.err, kWaitLimitNs);
+        ok = mbar_wait_warp(&ctl.sum_free[t & 1], phase(t) ^ 1u, &ctl.abort, a.err, kWaitLimitNs) && ok;
+        if (!ok) break;
+        tc_fence_after_sync();
+        if (elect_one()) {
+          const uint64_t wt = w0 + (t % WB) * (kExpandW<RP> / 16);
 #pragma unroll
-        for (int k = 0; k < 2 * RP / 16; ++k)
-          tc_mma_ss(tmem + (t & 1) * kCols, v0 + ((k >> 2) * (kTcTile * 128 / 16) + 2 * (k & 3)),
-                    wt + (k % (RP / 16)) * 128, idesc, k != 0);
-        tc_commit(&ctl.w_free[t % WB]);
-        tc_commit(&ctl.sum_full[t & 1]);
+          for (int k = 0; k < 2 * RP / 16; ++k)
+            tc_mma_ss(tmem + (t & 1) * kCols, v0 + ((k >> 2) * (kTcTile * 128 / 16) + 2 * (k & 3)),
+                      wt + (k % (RP / 16)) * 128, idesc, k != 0);
+          tc_commit(&ctl.w_free[t % WB]);
+          tc_commit(&ctl.sum_full[t & 1]);
+        }
+        __syncwarp();
       }
-      __syncwarp();
+      done += sg.count;
     }
   } else {
-    // ---------------- V, and w ahead of the MMAs
+    // ---------------- a segment's V, and w ahead of the MMAs
     const int lt = tid - 32 * (kFinishers + 1);
     constexpr int kLt = 32 * kLoaders, kRow = 2 * RP / 8;   // threads; 16-byte pieces of a row of V
-    const int rank = a.ad.rank(tile.x);
-    const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * a.ad.r * a.K;
-    for (int p = lt; p < kTcTile * kRow; p += kLt) {
-      const int m = p / kRow, c = p % kRow;
-      const bool v = m < tile.z;
-      cp_async16(sv + (c >> 3) * (kTcTile * 128) + tile_off(m, c & 7),
-                 a.terms + static_cast<int64_t>(tile.y + (v ? m : 0)) * a.row_terms + 8 * c, v);
-    }
     const int pc = lt & 15, pr = lt >> 4;
-    // (with one stage each tile's copies are waited for at once, else a tile later)
-    for (int t = 0; t < n + WB - 1; ++t) {
-      if (t < n) {
-        // the stage's tile before, if any, has been multiplied
-        mbar_wait(&ctl.w_free[t % WB], w_phase(t) ^ 1u, &ctl.abort, a.err, kWaitLimitNs);
-        const int e = column(t) + 8 * pc;
+    while (u < end) {
+      const Segment sg = next_segment(a.route, columns, u, end);
+      if (sg.tile.x < 0) continue;
+      const int rank = a.ad.rank(sg.tile.x);
+      const __nv_bfloat16* w = a.w + static_cast<int64_t>(sg.tile.x) * a.ad.r * a.K;
+      // the segment before has been multiplied: its V may go
+      if (done > 0)
+        mbar_wait(&ctl.w_free[(done - 1) % WB], w_phase(done - 1), &ctl.abort, a.err, kWaitLimitNs);
+      for (int p = lt; p < kTcTile * kRow; p += kLt) {
+        const int m = p / kRow, c = p % kRow;
+        const bool v = m < sg.tile.z;
+        cp_async16(sv + (c >> 3) * (kTcTile * 128) + tile_off(m, c & 7),
+                   a.terms + static_cast<int64_t>(sg.tile.y + (v ? m : 0)) * a.row_terms + 8 * c, v);
+      }
+      // (with one stage each tile's copies are waited for at once, else a tile later)
+      for (int i = 0; i < sg.count + WB - 1; ++i) {
+        const int t = done + i;
+        if (i < sg.count) {
+          // the stage's tile before, if any, has been multiplied
+          mbar_wait(&ctl.w_free[t % WB], w_phase(t) ^ 1u, &ctl.abort, a.err, kWaitLimitNs);
+          const int e = (sg.first + i) * kCols + 8 * pc;
 #pragma unroll
-        for (int i = 0; i < RP * 16 / kLt; ++i) {
-          const int wr = pr + kLt / 16 * i;
-          const bool v = wr < rank && e < a.K;
-          cp_async16(sw + (t % WB) * kExpandW<RP> + (pc >> 3) * (RP * 128) + tile_off(wr, pc & 7),
-                     v ? w + static_cast<int64_t>(wr) * a.K + e : w, v);
+          for (int k = 0; k < RP * 16 / kLt; ++k) {
+            const int wr = pr + kLt / 16 * k;
+            const bool v = wr < rank && e < a.K;
+            cp_async16(sw + (t % WB) * kExpandW<RP> + (pc >> 3) * (RP * 128) + tile_off(wr, pc & 7),
+                       v ? w + static_cast<int64_t>(wr) * a.K + e : w, v);
+          }
+        }
+        cp_async_commit();
+        if (i >= WB - 1) {   // this tile (and V) has come
+          cp_async_wait<WB - 1>();
+          fence_proxy_async_smem();
+          mbar_arrive(&ctl.w_full[(t - (WB - 1)) % WB]);
         }
       }
-      cp_async_commit();
-      const int come = t - (WB - 1);   // this tile (and V) has come
-      if (come >= 0) {
-        cp_async_wait<WB - 1>();
-        fence_proxy_async_smem();
-        mbar_arrive(&ctl.w_full[come % WB]);
-      }
+      cp_async_wait<0>();
+      done += sg.count;
     }
-    cp_async_wait<0>();
   }
   // (after a wait that ran out, MMAs may be under way: they are given their time)
-  if (*static_cast<volatile int*>(&ctl.abort) && warp == kFinishers)
-    mbar_wait(&ctl.sum_full[0], phase(n), nullptr, a.err, kWaitLimitNs);
+  if (warp == kFinishers && *static_cast<volatile int*>(&ctl.abort))
+    mbar_wait(&ctl.sum_full[0], phase(done), nullptr, a.err, kWaitLimitNs);
   tc_end<2 * kCols>(tmem);
 }
 
@@ -1648,17 +1661,16 @@ cudaError_t run_shrink_tc(const AdapterProblem& p, const Plan& pl, const Route& 
 cudaError_t run_expand_tc(const AdapterProblem& p, const Plan& pl, const Route& route,
                           const __nv_bfloat16* terms, int terms_per, const void* w, int64_t K,
                           const void* base, int64_t ldbase, void* y, int64_t ldy, cudaStream_t s) {
-  const int tiles = static_cast<int>((K + kCols - 1) / kCols);
-  int groups = (kExpandCtas * device_sm_count() + pl.max_tiles - 1) / pl.max_tiles;
-  if (groups > tiles) groups = tiles;
+  const int64_t most = pl.max_tiles * ((K + kCols - 1) / kCols);   // units of work
   return by_rank(p.r, [&](auto rp) {
     constexpr int RP = decltype(rp)::value;
     const ExpandTcArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, terms,
                          static_cast<const __nv_bfloat16*>(w),
                          static_cast<const __nv_bfloat16*>(base), static_cast<__nv_bfloat16*>(y),
-                         ldbase, ldy, terms_per * RP, static_cast<int>(K), groups,
-                         device_error_word()};
-    return go<expand_tc_kernel<RP>>(dim3(pl.max_tiles * groups), kExpandThreads, kExpandSmem<RP>, s, a);
+                         ldbase, ldy, terms_per * RP, static_cast<int>(K), device_error_word()};
+    const int64_t stay = kExpandCtas<RP> * device_sm_count();
+    return go<expand_tc_kernel<RP>>(dim3(static_cast<unsigned>(most < stay ? most : stay)),
+                                    kExpandThreads, kExpandSmem<RP>, s, a);
   });
 }
 
