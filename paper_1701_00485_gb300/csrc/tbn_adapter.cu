@@ -61,6 +61,17 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
+               "r"(valid ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
 // The leading kTerms bf16 terms of v: all but the last cut off (so that no
 // finite value becomes infinite), the last rounded to nearest.  Infinities and
 // NaN go into the first term alone.
@@ -86,56 +97,76 @@ __device__ __forceinline__ void store_pair(uint8_t* tile, uint32_t stride, uint3
     *reinterpret_cast<uint32_t*>(tile + i * stride + off) = pack_bf16x2(a[i], b[i]);
 }
 
-// Sixteen consecutive elements of a row, held as they come.
-template <typename T>
-struct Piece;
-template <>
-struct Piece<__nv_bfloat16> {
-  uint4 q[2];
-};
-template <>
-struct Piece<float> {
-  float4 q[4];
-};
-
-// Elements [at, at + 16) of the row at p, of which K exist; zeros past the end
-// and for p = nullptr.
-__device__ __forceinline__ void load_piece(Piece<__nv_bfloat16>& d, const __nv_bfloat16* p, int at,
-                                           int K, bool aligned) {
+// The 16-byte words that hold elements [at, at + 16 kWords / sizeof(T)) of the row
+// at p, of which K exist; zeros past the end and for p = nullptr.  In a row that is
+// not aligned, words begin in front of `at` and there is one more of them; straighten
+// shifts them into place.  (Element by element an unaligned row took eight times as
+// many loads, and its lines were looked up for each of them.)
+template <int kWords, typename T>
+__device__ __forceinline__ void load_words(uint4 (&d)[kWords + 1], const T* p, int at, int K, bool aligned) {
+  constexpr int kPer = 16 / sizeof(T);
+  const int skew = aligned ? 0 : static_cast<int>((reinterpret_cast<uintptr_t>(p) + at * sizeof(T)) / sizeof(T) % kPer);
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int e = at + 8 * i;
-    d.q[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (p == nullptr || e >= K) continue;
-    if (aligned) {
-      d.q[i] = __ldg(reinterpret_cast<const uint4*>(p + e));
-    } else {
+  for (int i = 0; i < kWords + 1; ++i) {
+    const int e = at - skew + kPer * i;
+    d[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (p == nullptr || e >= K || (i == kWords && skew == 0)) continue;
+    if (e >= 0 && e + kPer <= K) {
+      d[i] = __ldg(reinterpret_cast<const uint4*>(p + e));
+    } else {   // it begins in front of the row or ends behind it
       uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (e + j < K)
-          w[j / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(p[e + j])) << (16 * (j % 2));
-      d.q[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int j = 0; j < kPer; ++j)
+        if (e + j >= 0 && e + j < K) {
+          if constexpr (sizeof(T) == 2)
+            w[j / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(p[e + j])) << (16 * (j % 2));
+          else
+            w[j] = __float_as_uint(p[e + j]);
+        }
+      d[i] = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
 }
 
-__device__ __forceinline__ void load_piece(Piece<float>& d, const float* p, int at, int K,
-                                           bool aligned) {
+// `from`: the address of the first element wanted.
+template <int kWords, typename T>
+__device__ __forceinline__ void straighten(uint4 (&d)[kWords + 1], const T* from) {
+  constexpr int N = 4 * (kWords + 1);
+  const uint32_t skew = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(from)) & 15u;
+  uint32_t w[N];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int e = at + 4 * i;
-    d.q[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (p == nullptr || e >= K) continue;
-    if (aligned) {
-      d.q[i] = __ldg(reinterpret_cast<const float4*>(p + e));
-    } else {
-      d.q[i].x = p[e];
-      if (e + 1 < K) d.q[i].y = p[e + 1];
-      if (e + 2 < K) d.q[i].z = p[e + 2];
-      if (e + 3 < K) d.q[i].w = p[e + 3];
-    }
+  for (int i = 0; i <= kWords; ++i) {
+    w[4 * i] = d[i].x;
+    w[4 * i + 1] = d[i].y;
+    w[4 * i + 2] = d[i].z;
+    w[4 * i + 3] = d[i].w;
   }
+#pragma unroll
+  for (int i = 0; i < N - 1; ++i) w[i] = skew & 4u ? w[i + 1] : w[i];
+#pragma unroll
+  for (int i = 0; i < N - 3; ++i) w[i] = skew & 8u ? w[i + 2] : w[i];
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < N - 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 8 * (skew & 2u));
+  }
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) d[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+}
+
+// Sixteen consecutive elements of a row, held as they come.
+template <typename T>
+constexpr int kPieceWords = static_cast<int>(sizeof(T));
+template <typename T>
+struct Piece {
+  uint4 q[kPieceWords<T> + 1];
+};
+
+// Eight consecutive elements of a row of a or b, at once in place.
+__device__ __forceinline__ uint4 load_w(const __nv_bfloat16* p, int at, int K, bool aligned) {
+  uint4 d[2];
+  load_words<1>(d, p, at, K, aligned);
+  if (!aligned) straighten<1>(d, p + at);
+  return d[0];
 }
 
 // Into chunks c and c + 1 of a row of the tile (fp32: of its three terms).
@@ -150,8 +181,8 @@ __device__ __forceinline__ void store_piece(uint8_t* tile, uint32_t stride, int 
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t off = tile_off(row, c + i / 2) + 8 * (i % 2);
-    store_pair<3>(tile, stride, off, d.q[i].x, d.q[i].y);
-    store_pair<3>(tile, stride, off + 4, d.q[i].z, d.q[i].w);
+    store_pair<3>(tile, stride, off, __uint_as_float(d.q[i].x), __uint_as_float(d.q[i].y));
+    store_pair<3>(tile, stride, off + 4, __uint_as_float(d.q[i].z), __uint_as_float(d.q[i].w));
   }
 }
 
@@ -295,61 +326,152 @@ struct Adapters {
   }
 };
 
+// ------------------------------------------------- the low-rank activations
+// Between two products they are kept as bf16 terms, scaled, by sorted position, a
+// token's terms side by side.
+__device__ __forceinline__ float4 load_cluster(uint32_t addr, int rank) {
+  float4 v;
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(at)
+               : "memory");
+  return v;
+}
+
+// Eight ranks from `col` on of the token at sorted position `at`, as terms.  Past
+// the rank they are zero, whatever v holds there.
+template <int RP, int kTerms>
+__device__ __forceinline__ void write_terms(const float (&v)[8], float factor, int col, int rank,
+                                            int64_t at, __nv_bfloat16* terms) {
+  float t[8][kTerms];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) split(col + j < rank ? v[j] * factor : 0.0f, t[j]);
+  __nv_bfloat16* out = terms + at * (kTerms * RP) + col;
+#pragma unroll
+  for (int k = 0; k < kTerms; ++k)
+    *reinterpret_cast<uint4*>(out + k * RP) =
+        make_uint4(pack_bf16x2(t[0][k], t[1][k]), pack_bf16x2(t[2][k], t[3][k]),
+                   pack_bf16x2(t[4][k], t[5][k]), pack_bf16x2(t[6][k], t[7][k]));
+}
+
+template <int RP>
+constexpr int kSumRow = RP + 4;   // floats: rows of neighbouring lanes in other banks
+
+// The part of a tile of kRows tokens that CTA `split` of a cluster finishes: the
+// CTAs' sums [kRows][kSumRow] at `sums_s` are added in order and written as they are
+// (v_out, by token) and as terms (2 or 3).
+template <int RP, int kRows>
+__device__ __forceinline__ void finish_shrink(uint32_t sums_s, const int4& tile, int split, int splits,
+                                              int rank, int r, float factor, const int* perm, float* v_out,
+                                              __nv_bfloat16* terms, int count) {
+  const int rows = kRows / splits;
+  for (int i = threadIdx.x; i < rows * (RP / 8); i += kThreads) {
+    const int m = split * rows + i / (RP / 8), col = 8 * (i % (RP / 8));
+    if (m >= tile.z) continue;
+    float v[8] = {};
+    for (int q = 0; q < splits; ++q) {
+      const uint32_t at = sums_s + (m * kSumRow<RP> + col) * 4;
+      const float4 x = load_cluster(at, q), y = load_cluster(at + 16, q);
+      v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+      v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+    }
+    if (v_out != nullptr) {
+      float* o = v_out + static_cast<int64_t>(perm[tile.y + m]) * r + col;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (col + j < r) o[j] = col + j < rank ? v[j] : 0.0f;
+    }
+    if (terms == nullptr) continue;
+    if (count == 2) write_terms<RP, 2>(v, factor, col, rank, tile.y + m, terms);
+    else write_terms<RP, 3>(v, factor, col, rank, tile.y + m, terms);
+  }
+}
+
+// Low-rank activations that are there already, by token, as terms.
+template <int RP, int kRows>
+__device__ __forceinline__ void terms_of(const float* v_in, const int4& tile, int split, int splits, int rank,
+                                         int r, float factor, const int* perm, __nv_bfloat16* terms) {
+  const int rows = kRows / splits;
+  for (int i = threadIdx.x; i < rows * (RP / 8); i += kThreads) {
+    const int m = split * rows + i / (RP / 8), col = 8 * (i % (RP / 8));
+    if (m >= tile.z) continue;
+    const float* p = v_in + static_cast<int64_t>(perm[tile.y + m]) * r + col;
+    float v[8] = {};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (col + j < rank) v[j] = p[j];
+    write_terms<RP, 3>(v, factor, col, rank, tile.y + m, terms);
+  }
+}
+
+// v_out of tokens without an adapter.
+__device__ __forceinline__ void zero_v(float* v_out, const int4& tile, int split, int splits, int r,
+                                       const int* perm) {
+  for (int i = split * kThreads + threadIdx.x; i < tile.z * r; i += splits * kThreads)
+    v_out[static_cast<int64_t>(perm[tile.y + i / r]) * r + i % r] = 0.0f;
+}
+
 // ----------------------------------------------------------------- shrink
 struct ShrinkArgs {
   Route route;
   Adapters ad;
   const void* x;
   const __nv_bfloat16* w;    // [n][r][K]
-  float* part;               // [splits][T][r], by sorted position
+  __nv_bfloat16* terms;      // or nullptr: [T][count RP]
+  float* v_out;              // or nullptr: [T][r] by token, unscaled
   int64_t ldx;
-  int T, K, chunks, chunks_per;
+  int K, chunks, splits, max_tiles, prefetch_rows, count;
+  // a second job, of the launch's clusters from max_tiles on (which may be 0: the
+  // only job): these low-rank activations [T][r], by token, as terms
+  const float* v_in;
+  __nv_bfloat16* v_terms;
   int x_aligned, w_aligned;
+  uint32_t* err;
 };
 
-// CTA (tile, split): 64 tokens x the ranks over a range of K.  Warp w takes 16
-// tokens and every other 32 of a chunk's 64 elements; the two halves are added
-// at the end.
+// A cluster of `splits` CTAs: 64 tokens x the ranks, a CTA every splits-th chunk of
+// K; their sums meet in distributed shared memory.  Warp w takes 16 tokens and every
+// other 32 of a chunk's 64 elements; the two halves are added at the end.
 template <typename T, int RP>
-__global__ void __launch_bounds__(kThreads) shrink_kernel(const ShrinkArgs a) {
+__global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant__ ShrinkArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   constexpr int kTerms = kTermsOf<T>;
   constexpr int kStage = kTerms * kHalf + RP * 128;
   constexpr int kPieces = (RP * 8 + kThreads - 1) / kThreads;   // 16-byte pieces of w a thread
   grid_dependency_wait();
   grid_dependents_launch();
-  if (static_cast<int>(blockIdx.x) >= a.route.counts[0]) return;
-  const int4 tile = a.route.tiles[blockIdx.x];
-  if (tile.x < 0) return;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int split = blockIdx.x % a.splits;
+  int tile_id = blockIdx.x / a.splits;
+  const bool second = tile_id >= a.max_tiles;
+  if (second) tile_id -= a.max_tiles;
+  // (all CTAs of the cluster alike)
+  if (tile_id >= a.route.counts[0]) return;
+  const int4 tile = a.route.tiles[tile_id];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = a.ad.r;
+  if (tile.x < 0) {
+    if (a.v_out != nullptr && !second) zero_v(a.v_out, tile, split, a.splits, r, a.route.perm);
+    return;
+  }
   const int rank = a.ad.rank(tile.x);
-  const int c0 = blockIdx.y * a.chunks_per, c1 = min(a.chunks, c0 + a.chunks_per);
+  const float factor = a.ad.factor(tile.x);
+  if (second)
+    return terms_of<RP, kTile>(a.v_in, tile, split, a.splits, rank, r, factor, a.route.perm, a.v_terms);
   const int row = tid >> 2, q = tid & 3;
   const T* xrow = nullptr;
   if (row < tile.z)
     xrow = static_cast<const T*>(a.x) + a.route.perm[tile.y + row] * a.ldx;
-  const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * a.ad.r * a.K;
+  const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * r * a.K;
   Piece<T> px;
   uint4 pw[kPieces];
   const auto load = [&](int c) {
-    load_piece(px, xrow, c * kChunk + 16 * q, a.K, a.x_aligned);
+    load_words<kPieceWords<T>>(px.q, xrow, c * kChunk + 16 * q, a.K, a.x_aligned);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int p = tid + i * kThreads, wr = p >> 3, e = c * kChunk + 8 * (p & 7);
-      pw[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (wr < rank && e < a.K) {
-        const __nv_bfloat16* src = w + static_cast<int64_t>(wr) * a.K + e;
-        if (a.w_aligned) {
-          pw[i] = __ldg(reinterpret_cast<const uint4*>(src));
-        } else {
-          uint32_t u[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (e + j < a.K)
-              u[j / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(src[j])) << (16 * (j % 2));
-          pw[i] = make_uint4(u[0], u[1], u[2], u[3]);
-        }
-      }
+      const int p = tid + i * kThreads, wr = p >> 3;
+      pw[i] = load_w(wr < rank ? w + static_cast<int64_t>(wr) * a.K : nullptr, c * kChunk + 8 * (p & 7), a.K,
+                     a.w_aligned);
     }
   };
   // with several terms the leading one's sum is apart from the others': the tensor
@@ -363,10 +485,12 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const ShrinkArgs a) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[q][i][j] = 0.0f;
   const int tg = 16 * (warp & 3), kh = warp >> 2, mi = lane >> 3, lr = lane & 7;
-  load(c0);
-  for (int c = c0; c < c1; ++c) {
-    uint8_t* st = smem + ((c - c0) & 1) * kStage;
+  load(split);
+  int turn = 0;
+  for (int c = split; c < a.chunks; c += a.splits, turn ^= 1) {
+    uint8_t* st = smem + turn * kStage;
     uint8_t* sw = st + kTerms * kHalf;
+    if (!a.x_aligned) straighten<kPieceWords<T>>(px.q, xrow + c * kChunk + 16 * q);
     store_piece(st, kHalf, row, 2 * q, px);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
@@ -374,7 +498,7 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const ShrinkArgs a) {
       if (p < RP * 8) *reinterpret_cast<uint4*>(sw + tile_off(p >> 3, p & 7)) = pw[i];
     }
     __syncthreads();   // two stages: the one written next was read before this
-    if (c + 1 < c1) load(c + 1);
+    if (c + a.splits < a.chunks) load(c + a.splits);
     const uint32_t sx = smem_addr(st), sww = smem_addr(sw);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -402,63 +526,48 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const ShrinkArgs a) {
       for (int j = 0; j < 4; ++j) acc[0][i][j] += acc[1][i][j];
   }
   __syncthreads();
-  float* sum = reinterpret_cast<float*>(smem);   // [64][RP]
+  float* sums = reinterpret_cast<float*>(smem);   // [64][kSumRow]
   const int g = lane >> 2, t2 = 2 * (lane & 3);
-  if (kh == 1) {
 #pragma unroll
-    for (int nt = 0; nt < RP / 8; ++nt)
+  for (int half = 1; half >= 0; --half) {
+    if (kh == half) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        sum[(tg + g + 8 * (i >> 1)) * RP + 8 * nt + t2 + (i & 1)] = acc[0][nt][i];
+      for (int nt = 0; nt < RP / 8; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+          float2* at = reinterpret_cast<float2*>(sums + (tg + g + 4 * i) * kSumRow<RP> + 8 * nt + t2);
+          const float2 other = half ? make_float2(0.0f, 0.0f) : *at;
+          *at = make_float2(acc[0][nt][i] + other.x, acc[0][nt][i + 1] + other.y);
+        }
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  if (kh == 0) {
-    float* part = a.part + (static_cast<int64_t>(blockIdx.y) * a.T + tile.y) * a.ad.r;
-#pragma unroll
-    for (int nt = 0; nt < RP / 8; ++nt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int m = tg + g + 8 * (i >> 1), col = 8 * nt + t2 + (i & 1);
-        if (m < tile.z && col < a.ad.r)
-          part[static_cast<int64_t>(m) * a.ad.r + col] = acc[0][nt][i] + sum[m * RP + col];
-      }
-  }
+  cluster_sync();
+  finish_shrink<RP, kTile>(smem_addr(sums), tile, split, a.splits, rank, r, factor, a.route.perm, a.v_out,
+                           a.terms, a.count);
+  cluster_sync();   // no CTA leaves while another reads its sums
 }
-
-// ------------------------------------------------- the low-rank activations
-// Where expand and grad find them: partial sums by sorted position, added in
-// order, or (by_token) one value by token.
-struct LowRank {
-  const float* p;
-  int64_t split_stride;
-  int splits, by_token;
-  __device__ __forceinline__ float get(int64_t row, int r, int col) const {
-    const float* s = p + row * r + col;
-    float v = *s;
-    for (int i = 1; i < splits; ++i) v += s[i * split_stride];
-    return v;
-  }
-};
 
 // ----------------------------------------------------------------- expand
 struct ExpandArgs {
   Route route;
   Adapters ad;
-  LowRank v;
+  const __nv_bfloat16* terms;
   const __nv_bfloat16* w;   // [n][r][K]
   const void* base;         // or nullptr
   void* y;
-  float* v_out;             // or nullptr: [T][r] by token, unscaled
   int64_t ldbase, ldy;
-  int K, cols_per;          // column tiles of a CTA
-  int y_bf16, w_aligned, y_aligned;
+  int terms_row, K, cols_per;   // elements of a token's terms; column tiles of a CTA
+  int w_aligned, y_aligned;
 };
 
 // CTA (tile, column group): 64 tokens x cols_per * 128 columns.  Warp w takes 16
 // tokens and 64 of the 128 columns; the sums leave through shared memory so that
-// a warp reads the base and writes the result in whole rows.
+// a warp reads the base and writes the result in whole rows, eight of them, whose
+// base is asked for before the product.  y has 16 bits with two terms, 32 with three.
 template <int RP, int kTerms>
-__global__ void __launch_bounds__(kThreads) expand_kernel(const ExpandArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) expand_kernel(const __grid_constant__ ExpandArgs a) {
+  using Y = typename std::conditional<kTerms == 2, __nv_bfloat16, float>::type;
   extern __shared__ __align__(128) uint8_t smem[];
   constexpr int kV = (RP + 63) / 64 * kHalf;          // bytes of one term of V
   constexpr int kW = RP * 128;                        // bytes of 64 columns of w
@@ -475,53 +584,69 @@ __global__ void __launch_bounds__(kThreads) expand_kernel(const ExpandArgs a) {
   const bool none = tile.x < 0;
   const int rank = none ? 0 : a.ad.rank(tile.x), r = a.ad.r;
   const __nv_bfloat16* w = a.w + static_cast<int64_t>(none ? 0 : tile.x) * r * a.K;
-  if (!none) {
-    const float factor = a.ad.factor(tile.x);
-    for (int i = tid; i < kTile * RP / 2; i += kThreads) {
-      const int m = i / (RP / 2), col = 2 * (i % (RP / 2));
-      float v[2] = {0.0f, 0.0f};
-      if (m < tile.z) {
-        const int64_t at = a.v.by_token ? a.route.perm[tile.y + m] : tile.y + m;
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          if (col + j < rank) v[j] = a.v.get(at, r, col + j);
-        if (a.v_out != nullptr && blockIdx.y == 0) {
-          float* o = a.v_out + static_cast<int64_t>(a.route.perm[tile.y + m]) * r;
-          if (col < r) o[col] = v[0];
-          if (col + 1 < r) o[col + 1] = v[1];
-        }
-      }
-      store_pair<kTerms>(sv, kV, (col >> 6) * kHalf + tile_off(m, (col & 63) >> 3) + 2 * (col & 7),
-                         v[0] * factor, v[1] * factor);
+  if (!none)
+    for (int i = tid; i < kTile * kTerms * (RP / 8); i += kThreads) {
+      const int m = i / (kTerms * (RP / 8)), c = i % (kTerms * (RP / 8)), t = c / (RP / 8), k = c % (RP / 8);
+      const bool v = m < tile.z;
+      cp_async16(smem_addr(sv) + t * kV + (k >> 3) * kHalf + tile_off(m, k & 7),
+                 a.terms + (v ? static_cast<int64_t>(tile.y + m) * a.terms_row + 8 * c : 0), v);
     }
-  } else if (a.v_out != nullptr && blockIdx.y == 0) {
-    for (int i = tid; i < tile.z * r; i += kThreads)
-      a.v_out[static_cast<int64_t>(a.route.perm[tile.y + i / r]) * r + i % r] = 0.0f;
-  }
+  cp_async_commit();
+  // the warp's tokens, one in each of eight lanes
+  const int mine = 8 * warp + lr < tile.z ? a.route.perm[tile.y + 8 * warp + lr] : -1;
   const uint32_t sv_s = smem_addr(sv), sw_s = smem_addr(sw);
   const int tg = 16 * (warp & 3), ch = warp >> 2;
   const int col_beg = blockIdx.y * a.cols_per * kCols;
   const int col_end = min(a.K, col_beg + a.cols_per * kCols);
   for (int c0 = col_beg; c0 < col_end; c0 += kCols) {
-    if (!none) {
-      for (int p = tid; p < RP * 16; p += kThreads) {
-        const int wr = p >> 4, pc = p & 15, e = c0 + 8 * pc;
-        uint32_t u[4] = {0u, 0u, 0u, 0u};
-        if (wr < rank && e < a.K) {
-          const __nv_bfloat16* src = w + static_cast<int64_t>(wr) * a.K + e;
-          if (a.w_aligned) {
-            const uint4 v4 = __ldg(reinterpret_cast<const uint4*>(src));
-            u[0] = v4.x; u[1] = v4.y; u[2] = v4.z; u[3] = v4.w;
-          } else {
+    // four columns a lane: side by side, or 32 apart in rows that are not aligned
+    const int e = a.y_aligned ? c0 + 4 * lane : c0 + lane;
+    uint32_t base[8][sizeof(Y) == 2 ? 2 : 4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (e + j < a.K)
-                u[j / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(src[j])) << (16 * (j % 2));
+    for (int j = 0; j < 8; ++j) {
+      const int token = __shfl_sync(0xffffffffu, mine, j);
+      const Y* p = static_cast<const Y*>(a.base) + token * a.ldbase + e;
+      const bool in = a.base != nullptr && token >= 0;
+      if constexpr (sizeof(Y) == 2) {
+        base[j][0] = base[j][1] = 0u;
+        if (a.y_aligned) {
+          if (in && e < a.K) {
+            const uint2 v = *reinterpret_cast<const uint2*>(p);
+            base[j][0] = v.x;
+            base[j][1] = v.y;
           }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (in && e + 32 * i < a.K)
+              base[j][i / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(p[32 * i])) << (16 * (i % 2));
         }
-        *reinterpret_cast<uint4*>(sw + (pc >> 3) * kW + tile_off(wr, pc & 7)) =
-            make_uint4(u[0], u[1], u[2], u[3]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) base[j][i] = 0u;
+        if (a.y_aligned) {
+          if (in && e < a.K) {
+            const uint4 v = *reinterpret_cast<const uint4*>(p);
+            base[j][0] = v.x;
+            base[j][1] = v.y;
+            base[j][2] = v.z;
+            base[j][3] = v.w;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (in && e + 32 * i < a.K) base[j][i] = __float_as_uint(p[32 * i]);
+        }
       }
+    }
+    if (!none) {
+#pragma unroll
+      for (int i = 0; i < RP * 16 / kThreads; ++i) {
+        const int p = tid + i * kThreads, wr = p >> 4, pc = p & 15;
+        *reinterpret_cast<uint4*>(sw + (pc >> 3) * kW + tile_off(wr, pc & 7)) =
+            load_w(wr < rank ? w + static_cast<int64_t>(wr) * a.K : nullptr, c0 + 8 * pc, a.K, a.w_aligned);
+      }
+      cp_async_wait<0>();
       __syncthreads();
       float acc[8][4];
 #pragma unroll
@@ -553,68 +678,46 @@ __global__ void __launch_bounds__(kThreads) expand_kernel(const ExpandArgs a) {
         for (int h = 0; h < 2; ++h)
           *reinterpret_cast<float2*>(out + (tg + g + 8 * h) * kStride + 64 * ch + 8 * nt + t2) =
               make_float2(acc[nt][2 * h], acc[nt][2 * h + 1]);
+      __syncthreads();
     }
-    __syncthreads();
-    // a warp: eight rows, four columns a lane
-    const int e = c0 + 4 * lane;
-    for (int j = 0; j < 8; ++j) {
-      const int m = 8 * warp + j;
-      if (m >= tile.z || e >= a.K) continue;
-      const int64_t token = a.route.perm[tile.y + m];
-      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      if (!none) v = *reinterpret_cast<const float4*>(out + m * kStride + 4 * lane);
-      if (a.y_aligned) {
-        if (a.y_bf16) {
-          if (a.base != nullptr) {
-            const uint2 b = *reinterpret_cast<const uint2*>(
-                static_cast<const __nv_bfloat16*>(a.base) + token * a.ldbase + e);
-            v.x += __uint_as_float(b.x << 16);
-            v.y += __uint_as_float(b.x & 0xFFFF0000u);
-            v.z += __uint_as_float(b.y << 16);
-            v.w += __uint_as_float(b.y & 0xFFFF0000u);
-          }
-          *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.y) + token * a.ldy + e) =
-              make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-        } else {
-          if (a.base != nullptr) {
-            const float4 b = *reinterpret_cast<const float4*>(
-                static_cast<const float*>(a.base) + token * a.ldbase + e);
-            v.x += b.x;
-            v.y += b.y;
-            v.z += b.z;
-            v.w += b.w;
-          }
-          *reinterpret_cast<float4*>(static_cast<float*>(a.y) + token * a.ldy + e) = v;
-        }
-      } else {
-        const float s[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (e + i >= a.K) break;
-          if (a.y_bf16) {
-            const float b = a.base == nullptr
-                                ? 0.0f
-                                : __bfloat162float(static_cast<const __nv_bfloat16*>(
-                                      a.base)[token * a.ldbase + e + i]);
-            static_cast<__nv_bfloat16*>(a.y)[token * a.ldy + e + i] = __float2bfloat16_rn(s[i] + b);
-          } else {
-            const float b = a.base == nullptr
-                                ? 0.0f
-                                : static_cast<const float*>(a.base)[token * a.ldbase + e + i];
-            static_cast<float*>(a.y)[token * a.ldy + e + i] = s[i] + b;
+    for (int j = 0; j < 8; ++j) {
+      const int token = __shfl_sync(0xffffffffu, mine, j);
+      if (token < 0 || e >= a.K) continue;
+      const float* sum = out + (8 * warp + j) * kStride + (e - c0);
+      Y* y = static_cast<Y*>(a.y) + token * a.ldy + e;
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(Y) == 2)
+          v[i] = __uint_as_float(i % 2 ? base[j][i / 2] & 0xFFFF0000u : base[j][i / 2] << 16);
+        else
+          v[i] = __uint_as_float(base[j][i]);
+        if (!none) v[i] += sum[a.y_aligned ? i : 32 * i];
+      }
+      if (a.y_aligned) {
+        if constexpr (sizeof(Y) == 2)
+          *reinterpret_cast<uint2*>(y) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        else
+          *reinterpret_cast<float4*>(y) = make_float4(v[0], v[1], v[2], v[3]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (e + 32 * i < a.K) {
+            if constexpr (sizeof(Y) == 2) y[32 * i] = __float2bfloat16_rn(v[i]);
+            else y[32 * i] = v[i];
           }
-        }
       }
     }
-    __syncthreads();
+    // (the next step's w and `out` are written behind what was read above: `sw` by
+    // the product, before the last barrier; `out` after the next one)
   }
 }
 
 // ------------------------------------------------------------------- grad
 // One of the two gradients.
 struct GradSide {
-  LowRank u;
-  const __nv_bfloat16* terms;   // tensor-core kernel: [T][3 RP] by sorted position
+  const __nv_bfloat16* terms;   // [T][3 RP] by sorted position
   const void* x;
   float* part;    // [items][r][K]
   float* out;     // [n][r][K]
@@ -625,19 +728,20 @@ struct GradSide {
 struct GradArgs {
   Route route;
   Adapters ad;
-  GradSide side;
+  GradSide side[2];
+  int tiles0;      // column tiles of side 0; those of side 1 follow
 };
 
 // CTA (item, 128 columns): the ranks x 128 columns of scale_i sum_t u_t x_t^T
 // over the item's tokens, in steps of 64.  Both operands come token by token and
-// are transposed by ldmatrix.  Warp w takes 16 columns.
+// are transposed by ldmatrix: u's terms by cp.async, a step ahead, x through
+// registers.  Warp w takes 16 columns.
 template <typename T, int RP>
-__global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
+__global__ void __launch_bounds__(kThreads) grad_kernel(const __grid_constant__ GradArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   constexpr int kTerms = kTermsOf<T>;
-  constexpr int kU = (RP + 63) / 64 * kHalf;    // bytes of one term of u
-  uint8_t* su = smem;                           // three terms
-  uint8_t* sx = smem + 3 * kU;                  // [terms][2 halves]
+  constexpr int kU = (3 * RP + 63) / 64 * kHalf;   // bytes of a stage of u
+  uint8_t* sx = smem + 2 * kU;                     // [terms][2 halves]
   grid_dependency_wait();
   grid_dependents_launch();
   if (static_cast<int>(blockIdx.x) >= a.route.counts[1]) return;
@@ -645,16 +749,29 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int mi = lane >> 3, lr = lane & 7, r = a.ad.r;
   const int rank = a.ad.rank(item.x);
-  const float factor = a.ad.factor(item.x);
-  const int c0 = blockIdx.y * kCols;
+  const bool first = static_cast<int>(blockIdx.y) < a.tiles0;
+  const GradSide& sd = a.side[first ? 0 : 1];
+  const int c0 = (first ? blockIdx.y : blockIdx.y - a.tiles0) * kCols;
   const int row = tid >> 2, q = tid & 3;
+  const uint32_t su_s = smem_addr(smem), sx_s = smem_addr(sx);
   Piece<T> px[2];
+  const T* at = nullptr;   // of the rows held
+  int token = row < item.z ? a.route.perm[item.y + row] : -1;
   const auto load = [&](int t0) {
-    const T* p = nullptr;
-    if (t0 + row < item.z)
-      p = static_cast<const T*>(a.side.x) + a.route.perm[item.y + t0 + row] * a.side.ldx;
+    at = token >= 0 ? static_cast<const T*>(sd.x) + token * sd.ldx : nullptr;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) load_piece(px[h], p, c0 + 64 * h + 16 * q, a.side.K, a.side.x_aligned);
+    for (int h = 0; h < 2; ++h)
+      load_words<kPieceWords<T>>(px[h].q, at, c0 + 64 * h + 16 * q, sd.K, sd.x_aligned);
+    const int next = t0 + kTile + row;
+    token = next < item.z ? a.route.perm[item.y + next] : -1;
+    const uint32_t su = su_s + (t0 / kTile & 1) * kU;
+    for (int i = tid; i < kTile * 3 * RP / 8; i += kThreads) {
+      const int m = i / (3 * RP / 8), c = i % (3 * RP / 8);
+      const bool v = t0 + m < item.z;
+      cp_async16(su + (c >> 3) * kHalf + tile_off(m, c & 7),
+                 sd.terms + (v ? static_cast<int64_t>(item.y + t0 + m) * (3 * RP) + 8 * c : 0), v);
+    }
+    cp_async_commit();
   };
   // the leading terms' sum, and the others'
   float acc[RP / 16][2][4], low[RP / 16][2][4];
@@ -664,26 +781,18 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int k = 0; k < 4; ++k) acc[i][j][k] = low[i][j][k] = 0.0f;
-  const uint32_t su_s = smem_addr(su), sx_s = smem_addr(sx);
   load(0);
   for (int t0 = 0; t0 < item.z; t0 += kTile) {
     __syncthreads();
 #pragma unroll
-    for (int h = 0; h < 2; ++h) store_piece(sx + h * kHalf, 2 * kHalf, row, 2 * q, px[h]);
-    for (int i = tid; i < kTile * RP / 2; i += kThreads) {
-      const int m = i / (RP / 2), col = 2 * (i % (RP / 2));
-      float v[2] = {0.0f, 0.0f};
-      if (t0 + m < item.z) {
-        const int64_t at = a.side.u.by_token ? a.route.perm[item.y + t0 + m] : item.y + t0 + m;
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          if (col + j < rank) v[j] = a.side.u.get(at, r, col + j) * factor;
-      }
-      store_pair<3>(su, kU, (col >> 6) * kHalf + tile_off(m, (col & 63) >> 3) + 2 * (col & 7), v[0],
-                    v[1]);
+    for (int h = 0; h < 2; ++h) {
+      if (!sd.x_aligned) straighten<kPieceWords<T>>(px[h].q, at + c0 + 64 * h + 16 * q);
+      store_piece(sx + h * kHalf, 2 * kHalf, row, 2 * q, px[h]);
     }
+    cp_async_wait<0>();
     __syncthreads();
     if (t0 + kTile < item.z) load(t0 + kTile);
+    const uint32_t su = su_s + (t0 / kTile & 1) * kU;
 #pragma unroll
     for (int ks = 0; ks < kTile / 16; ++ks) {
       uint32_t bf[kTerms][4];
@@ -696,8 +805,9 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
 #pragma unroll
         for (int tu = 0; tu < 3; ++tu) {
           uint32_t af[4];
-          ldsm4_trans(af, su_s + tu * kU + (mt >> 2) * kHalf +
-                              tile_off(16 * ks + 8 * (mi >> 1) + lr, 2 * (mt & 3) + (mi & 1)));
+          const int c = (tu * RP + 16 * mt) / 8;   // 16-byte chunk of a token's terms
+          ldsm4_trans(af, su + (c >> 3) * kHalf +
+                              tile_off(16 * ks + 8 * (mi >> 1) + lr, (c & 7) + (mi & 1)));
 #pragma unroll
           for (int t = 0; t < kTerms; ++t)
             if (tu + t <= 2) {   // what is left out is below 2^-24 of the product
@@ -708,8 +818,8 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
     }
   }
   const bool alone = a.route.item_begin[item.x + 1] - a.route.item_begin[item.x] == 1;
-  float* out = alone ? a.side.out + static_cast<int64_t>(item.x) * r * a.side.K
-                     : a.side.part + static_cast<int64_t>(blockIdx.x) * r * a.side.K;
+  float* out = alone ? sd.out + static_cast<int64_t>(item.x) * r * sd.K
+                     : sd.part + static_cast<int64_t>(blockIdx.x) * r * sd.K;
   const int g = lane >> 2, t2 = 2 * (lane & 3);
 #pragma unroll
   for (int mt = 0; mt < RP / 16; ++mt)
@@ -719,7 +829,7 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const GradArgs a) {
       for (int i = 0; i < 4; ++i) {
         const int m = 16 * mt + g + 8 * (i >> 1), e = c0 + 16 * warp + 8 * nt + t2 + (i & 1);
         // rows past the adapter's rank are zero whatever x holds
-        if (m < r && e < a.side.K) out[static_cast<int64_t>(m) * a.side.K + e] =
+        if (m < r && e < sd.K) out[static_cast<int64_t>(m) * sd.K + e] =
               m < rank ? acc[mt][nt][i] + low[mt][nt][i] : 0.0f;
       }
 }
@@ -770,17 +880,6 @@ constexpr int64_t kTcFrom = 128;   // tokens
 constexpr int64_t kPrefetchBytes = int64_t(80) << 20;   // of the 129 MB of L2
 constexpr int kGradCtas = 2;        // of grad
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
-
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
-               "r"(valid ? 16 : 0)
-               : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
 
 // Matrix descriptor of an operand whose rows are steps of the contraction and
 // whose 64-wide column blocks (128-byte swizzled rows) lie `block` bytes apart.
@@ -839,55 +938,10 @@ constexpr int kShrinkStages = 3;
 template <int RP>
 constexpr int kShrinkStage = kTcTile * 128 + RP * 128;
 template <int RP>
-constexpr int kSumRow = RP + 4;   // floats: rows of neighbouring lanes in other banks
-template <int RP>
 constexpr int kShrinkSmem = 1024 + kShrinkStages * kShrinkStage<RP>;
 
-struct ShrinkTcArgs {
-  Route route;
-  Adapters ad;
-  const __nv_bfloat16* x;
-  const __nv_bfloat16* w;   // [n][r][K]
-  __nv_bfloat16* terms;     // [T][kTerms RP], by sorted position
-  float* v_out;             // or nullptr: [T][r] by token, unscaled
-  int64_t ldx;
-  int K, chunks, splits, max_tiles, prefetch_rows;
-  // a second job, of the launch's clusters from max_tiles on (which may be 0: the
-  // only job): these low-rank activations [T][r], by token, as terms
-  const float* v_in;
-  __nv_bfloat16* v_terms;
-  uint32_t* err;
-};
-
-__device__ __forceinline__ float4 load_cluster(uint32_t addr, int rank) {
-  float4 v;
-  uint32_t at;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-               : "r"(at)
-               : "memory");
-  return v;
-}
-
-// Eight ranks from `col` on of the token at sorted position `at`, as terms.  Past
-// the rank they are zero, whatever v holds there.
-template <int RP, int kTerms>
-__device__ __forceinline__ void write_terms(const float (&v)[8], float factor, int col, int rank,
-                                            int64_t at, __nv_bfloat16* terms) {
-  float t[8][kTerms];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) split(col + j < rank ? v[j] * factor : 0.0f, t[j]);
-  __nv_bfloat16* out = terms + at * (kTerms * RP) + col;
-#pragma unroll
-  for (int k = 0; k < kTerms; ++k)
-    *reinterpret_cast<uint4*>(out + k * RP) =
-        make_uint4(pack_bf16x2(t[0][k], t[1][k]), pack_bf16x2(t[2][k], t[3][k]),
-                   pack_bf16x2(t[4][k], t[5][k]), pack_bf16x2(t[6][k], t[7][k]));
-}
-
-template <int RP, int kTerms>
-__global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const __grid_constant__ ShrinkTcArgs a) {
+template <int RP>
+__global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const __grid_constant__ ShrinkArgs a) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bar[kShrinkStages];
   __shared__ uint32_t slot;
@@ -896,13 +950,14 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const __grid_consta
   static_assert(kTcTile * kSumRow<RP> * 4 <= kShrinkStages * kShrinkStage<RP>, "sums in the ring");
   // while the tokens are being sorted: x is asked for in L2 (a hint that reads
   // nothing, so that it may stand before the wait)
+  const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(a.x);
   for (int i = blockIdx.x + gridDim.x * threadIdx.x; i < a.prefetch_rows; i += gridDim.x * kThreads)
-    bulk_prefetch(a.x + i * a.ldx, a.K * 2);
+    bulk_prefetch(x + i * a.ldx, a.K * 2);
   const uint32_t tmem = tc_begin<kTmem>(&slot, bar, S);
   grid_dependency_wait();
   grid_dependents_launch();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, ch = tid & 7;
-  const int split = blockIdx.x % a.splits, rows = kTcTile / a.splits;   // rows that a CTA finishes
+  const int split = blockIdx.x % a.splits;
   int tile_id = blockIdx.x / a.splits;
   const bool second = tile_id >= a.max_tiles;
   if (second) tile_id -= a.max_tiles;
@@ -911,24 +966,13 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const __grid_consta
   const int4 tile = a.route.tiles[tile_id];
   const int r = a.ad.r;
   if (tile.x < 0) {
-    if (a.v_out != nullptr && !second)
-      for (int i = split * kThreads + tid; i < tile.z * r; i += a.splits * kThreads)
-        a.v_out[static_cast<int64_t>(a.route.perm[tile.y + i / r]) * r + i % r] = 0.0f;
+    if (a.v_out != nullptr && !second) zero_v(a.v_out, tile, split, a.splits, r, a.route.perm);
     return tc_end<kTmem>(tmem);
   }
   const int rank = a.ad.rank(tile.x);
   const float factor = a.ad.factor(tile.x);
   if (second) {
-    for (int i = tid; i < rows * (RP / 8); i += kThreads) {
-      const int m = split * rows + i / (RP / 8), col = 8 * (i % (RP / 8));
-      if (m >= tile.z) continue;
-      const float* p = a.v_in + static_cast<int64_t>(a.route.perm[tile.y + m]) * r + col;
-      float v[8] = {};
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (col + j < rank) v[j] = p[j];
-      write_terms<RP, kTerms>(v, factor, col, rank, tile.y + m, a.v_terms);
-    }
+    terms_of<RP, kTcTile>(a.v_in, tile, split, a.splits, rank, r, factor, a.route.perm, a.v_terms);
     return tc_end<kTmem>(tmem);
   }
   uint8_t* smem = align_1k(smem_raw);
@@ -940,7 +984,7 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const __grid_consta
   for (int i = 0; i < 4; ++i) {
     const int row = (tid >> 3) + 32 * i;
     const bool v = row < tile.z;
-    xr[i] = a.x + (v ? a.route.perm[tile.y + row] * a.ldx : 0);
+    xr[i] = x + (v ? a.route.perm[tile.y + row] * a.ldx : 0);
     there |= static_cast<uint32_t>(v) << i;
   }
   const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * r * a.K;
@@ -1018,25 +1062,8 @@ __global__ void __launch_bounds__(kThreads) shrink_tc_kernel(const __grid_consta
     }
   }
   cluster_sync();
-  const uint32_t sums_s = smem_addr(sums);
-  for (int i = tid; i < rows * (RP / 8); i += kThreads) {
-    const int m = split * rows + i / (RP / 8), col = 8 * (i % (RP / 8));
-    if (m >= tile.z) continue;
-    float v[8] = {};
-    for (int q = 0; q < a.splits; ++q) {
-      const uint32_t at = sums_s + (m * kSumRow<RP> + col) * 4;
-      const float4 x = load_cluster(at, q), y = load_cluster(at + 16, q);
-      v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-      v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
-    }
-    if (a.v_out != nullptr) {
-      float* o = a.v_out + static_cast<int64_t>(a.route.perm[tile.y + m]) * r + col;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (col + j < r) o[j] = col + j < rank ? v[j] : 0.0f;
-    }
-    if (a.terms != nullptr) write_terms<RP, kTerms>(v, factor, col, rank, tile.y + m, a.terms);
-  }
+  finish_shrink<RP, kTcTile>(smem_addr(sums), tile, split, a.splits, rank, r, factor, a.route.perm, a.v_out,
+                             a.terms, a.count);
   cluster_sync();   // no CTA leaves while another reads its sums
   tc_end<kTmem>(tmem);
 }
@@ -1461,23 +1488,12 @@ size_t up(size_t n) { return (n + 255) / 256 * 256; }
 struct Plan {
   bool tc;
   int tile, max_tiles, max_items, tokens_per_item;
-  int splits_in, per_in, splits_out, per_out;   // shrink over K_in, over K_out
-  size_t counts, perm, tiles, items, begin, v, du, v_terms, du_terms, part_a, part_b, total;
-  int cluster_in, cluster_out;                  // CTAs of a cluster of shrink, where tc
+  int cluster_in, cluster_out;   // CTAs of a cluster of shrink, over K_in and over K_out
+  size_t counts, perm, tiles, items, begin, v_terms, du_terms, part_a, part_b, total;
 };
 
-void cut(int64_t K, int tiles, int ctas, int most, int* splits, int* per) {
-  const int chunks = static_cast<int>((K + kChunk - 1) / kChunk);
-  int want = ctas * device_sm_count() / tiles;   // not one more: they would be a second wave
-  if (want > most) want = most;
-  if (want > chunks) want = chunks;
-  if (want < 1) want = 1;
-  *per = (chunks + want - 1) / want;
-  *splits = (chunks + *per - 1) / *per;
-}
-
-// CTAs of a cluster of the tensor-core shrink: a power of two of at most eight, no
-// more than K has chunks, and no more clusters than the SMs hold at once.
+// CTAs of a cluster of shrink: a power of two of at most eight, no more than K has
+// chunks, and no more clusters than the SMs hold at once.
 int cluster_of(int64_t K, int64_t r, int tiles) {
   const int64_t chunks = (K + kChunk - 1) / kChunk, slots = (r > 64 ? 2 : 3) * device_sm_count();
   int c = 1;
@@ -1493,16 +1509,14 @@ Plan make_plan(int64_t T, int64_t n, int64_t r, int64_t K_in, int64_t K_out, boo
   p.tile = tc ? kTcTile : kTile;
   const int64_t used = n < T ? n : T;
   p.max_tiles = static_cast<int>((T + p.tile - 1) / p.tile + used + 1);
-  const int most = T <= 64 ? 32 : 8;
-  cut(K_in, p.max_tiles, 3, most, &p.splits_in, &p.per_in);
-  cut(K_out, p.max_tiles, 3, most, &p.splits_out, &p.per_out);
   p.cluster_in = cluster_of(K_in, r, p.max_tiles);
   p.cluster_out = cluster_of(K_out, r, p.max_tiles);
-  // grad: about two CTAs an SM over the columns of both gradients
+  // grad: about two CTAs an SM over the columns of both gradients, four without tc
   const int64_t ct = tc && r <= 64 ? 256 : kCols;
   const int64_t column_tiles = (K_in + ct - 1) / ct + (K_out + ct - 1) / ct;
   // (items of an adapter end unevenly: a little below two a slot is quickest)
-  const int64_t want = (kGradCtas * device_sm_count() * 4 / 5 + column_tiles - 1) / column_tiles;
+  const int64_t slots = tc ? kGradCtas * device_sm_count() * 4 / 5 : 4 * device_sm_count();
+  const int64_t want = (slots + column_tiles - 1) / column_tiles;
   int64_t per = (T + want - 1) / want;
   per = (per + kTile - 1) / kTile * kTile;
   if (per < kTile) per = kTile;
@@ -1519,17 +1533,10 @@ Plan make_plan(int64_t T, int64_t n, int64_t r, int64_t K_in, int64_t K_out, boo
   p.tiles = take(sizeof(int4) * static_cast<size_t>(p.max_tiles));
   p.items = take(sizeof(int4) * static_cast<size_t>(p.max_items));
   p.begin = take(sizeof(int) * static_cast<size_t>(n + 1));
-  const size_t row = sizeof(float) * static_cast<size_t>(T) * static_cast<size_t>(r);
   const size_t term = sizeof(__nv_bfloat16) * static_cast<size_t>(T * padded_rank(r));
-  if (tc)
-    p.v_terms = take(term * (backward ? 3 : 2));
-  else
-    p.v = take(row * p.splits_in);
+  p.v_terms = take(term * 3);
   if (backward) {
-    if (tc)
-      p.du_terms = take(term * 3);
-    else
-      p.du = take(row * p.splits_out);
+    p.du_terms = take(term * 3);
     const size_t part = sizeof(float) * static_cast<size_t>(p.max_items) * static_cast<size_t>(r);
     p.part_a = take(part * static_cast<size_t>(K_in));
     p.part_b = take(part * static_cast<size_t>(K_out));
@@ -1549,9 +1556,31 @@ Route route_at(const Plan& p, void* ws) {
 template <auto kKernel, typename... A>
 cudaError_t go(dim3 grid, int threads, size_t smem, cudaStream_t s, const A&... args) {
   static const cudaError_t allowed = cudaFuncSetAttribute(
-      reinterpret_cast<const void*>(kKernel), cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024);
+      reinterpret_cast<const void*>(kKernel), cudaFuncAttributeMaxDynamicSharedMemorySize, 222 * 1024);
   if (allowed != cudaSuccess) return allowed;
   return launch_dependent(kKernel, grid, dim3(threads), smem, s, args...);
+}
+
+template <auto kKernel, typename A>
+cudaError_t go_cluster(dim3 grid, int cluster, size_t smem, cudaStream_t s, const A& args) {
+  static const cudaError_t allowed = cudaFuncSetAttribute(
+      reinterpret_cast<const void*>(kKernel), cudaFuncAttributeMaxDynamicSharedMemorySize, 222 * 1024);
+  if (allowed != cudaSuccess) return allowed;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kKernel, args);
 }
 
 // f(std::integral_constant<int, RP>) for the padded rank of r.
@@ -1574,28 +1603,36 @@ cudaError_t run_route(const AdapterProblem& p, const Plan& pl, const Route& r, c
             static_cast<int>(p.n), pl.tile, pl.tokens_per_item, r);
 }
 
+// Low-rank activations of x as `count` bf16 terms a value (unless w is nullptr), and
+// (v_in) others that are there already, as three.
 cudaError_t run_shrink(const AdapterProblem& p, const Plan& pl, const Route& route, const void* x,
-                       tbn_dtype dt, int64_t ldx, const void* w, int64_t K, int splits, int per,
-                       float* part, cudaStream_t s) {
-  const int chunks = static_cast<int>((K + kChunk - 1) / kChunk);
-  ShrinkArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, x,
-               static_cast<const __nv_bfloat16*>(w), part, ldx, static_cast<int>(p.T),
-               static_cast<int>(K), chunks, per, rows_aligned(x, ldx, K, dtype_size(dt), 16),
-               rows_aligned(w, K, K, 2, 16)};
-  const dim3 grid(pl.max_tiles, splits);
+                       tbn_dtype dt, int64_t ldx, const void* w, int64_t K, int cluster,
+                       __nv_bfloat16* terms, int count, float* v_out, const float* v_in,
+                       __nv_bfloat16* v_terms, cudaStream_t s) {
+  // as many rows as L2 keeps beside the rest
+  const int64_t fit = pl.tc && w != nullptr ? kPrefetchBytes / (2 * K) : 0;
+  const ShrinkArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, x,
+                     static_cast<const __nv_bfloat16*>(w), terms, v_out, ldx, static_cast<int>(K),
+                     static_cast<int>((K + kChunk - 1) / kChunk), cluster, w != nullptr ? pl.max_tiles : 0,
+                     static_cast<int>(fit < p.T ? fit : p.T), count, v_in, v_terms,
+                     rows_aligned(x, ldx, K, dtype_size(dt), 16), rows_aligned(w, K, K, 2, 16),
+                     device_error_word()};
+  const int jobs = (w != nullptr ? 1 : 0) + (v_in != nullptr ? 1 : 0);
   return by_rank(p.r, [&](auto rp) {
     constexpr int RP = decltype(rp)::value;
-    const int terms = dt == TBN_BF16 ? 1 : 3;
-    size_t smem = 2 * (terms * static_cast<size_t>(kHalf) + RP * 128);
-    if (smem < sizeof(float) * kTile * RP) smem = sizeof(float) * kTile * RP;
-    if (dt == TBN_BF16) return go<shrink_kernel<__nv_bfloat16, RP>>(grid, kThreads, smem, s, a);
-    return go<shrink_kernel<float, RP>>(grid, kThreads, smem, s, a);
+    const dim3 grid(static_cast<unsigned>(pl.max_tiles) * cluster * jobs);
+    if (pl.tc) return go_cluster<shrink_tc_kernel<RP>>(grid, cluster, kShrinkSmem<RP>, s, a);
+    const int of_x = dt == TBN_BF16 ? 1 : 3;
+    size_t smem = 2 * (of_x * static_cast<size_t>(kHalf) + RP * 128);
+    if (smem < sizeof(float) * kTile * kSumRow<RP>) smem = sizeof(float) * kTile * kSumRow<RP>;
+    if (dt == TBN_BF16) return go_cluster<shrink_kernel<__nv_bfloat16, RP>>(grid, cluster, smem, s, a);
+    return go_cluster<shrink_kernel<float, RP>>(grid, cluster, smem, s, a);
   });
 }
 
 cudaError_t run_expand(const AdapterProblem& p, const Plan& pl, const Route& route,
-                       const LowRank& v, const void* w, int64_t K, const void* base,
-                       int64_t ldbase, void* y, tbn_dtype dt, int64_t ldy, float* v_out,
+                       const __nv_bfloat16* terms, int terms_per, const void* w, int64_t K,
+                       const void* base, int64_t ldbase, void* y, tbn_dtype dt, int64_t ldy,
                        cudaStream_t s) {
   const size_t e = dtype_size(dt);
   const int tiles = static_cast<int>((K + kCols - 1) / kCols);
@@ -1603,58 +1640,19 @@ cudaError_t run_expand(const AdapterProblem& p, const Plan& pl, const Route& rou
   if (groups > tiles) groups = tiles;
   const int per = (tiles + groups - 1) / groups;
   groups = (tiles + per - 1) / per;
-  ExpandArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, v,
-               static_cast<const __nv_bfloat16*>(w), base, y, v_out, ldbase, ldy,
-               static_cast<int>(K), per, dt == TBN_BF16, rows_aligned(w, K, K, 2, 16),
-               rows_aligned(y, ldy, K, e, 4 * e) &&
-                   (base == nullptr || rows_aligned(base, ldbase, K, e, 4 * e))};
   const dim3 grid(pl.max_tiles, groups);
   return by_rank(p.r, [&](auto rp) {
     constexpr int RP = decltype(rp)::value;
-    const int terms = dt == TBN_BF16 ? 2 : 3;
-    const size_t smem = static_cast<size_t>(terms) * ((RP + 63) / 64 * kHalf) + 2 * RP * 128 +
+    const ExpandArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, terms,
+                       static_cast<const __nv_bfloat16*>(w), base, y, ldbase, ldy, terms_per * RP,
+                       static_cast<int>(K), per, rows_aligned(w, K, K, 2, 16),
+                       rows_aligned(y, ldy, K, e, 4 * e) &&
+                           (base == nullptr || rows_aligned(base, ldbase, K, e, 4 * e))};
+    const int used = dt == TBN_BF16 ? 2 : 3;
+    const size_t smem = static_cast<size_t>(used) * ((RP + 63) / 64 * kHalf) + 2 * RP * 128 +
                         sizeof(float) * kTile * (kCols + 4);
     if (dt == TBN_BF16) return go<expand_kernel<RP, 2>>(grid, kThreads, smem, s, a);
     return go<expand_kernel<RP, 3>>(grid, kThreads, smem, s, a);
-  });
-}
-
-// Low-rank activations of x as bf16 terms, kTerms a value (unless w is nullptr),
-// and (v_in) others that are there already.
-template <int kTerms>
-cudaError_t run_shrink_tc(const AdapterProblem& p, const Plan& pl, const Route& route, const void* x,
-                          int64_t ldx, const void* w, int64_t K, int cluster, __nv_bfloat16* terms,
-                          float* v_out, const float* v_in, __nv_bfloat16* v_terms, cudaStream_t s) {
-  // as many rows as L2 keeps beside the rest
-  const int64_t fit = w != nullptr ? kPrefetchBytes / (2 * K) : 0;
-  const int prefetch = static_cast<int>(fit < p.T ? fit : p.T);
-  const ShrinkTcArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)},
-                       static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(w), terms,
-                       v_out, ldx, static_cast<int>(K), static_cast<int>((K + kChunk - 1) / kChunk),
-                       cluster, w != nullptr ? pl.max_tiles : 0, prefetch, v_in, v_terms,
-                       device_error_word()};
-  return by_rank(p.r, [&](auto rp) {
-    constexpr int RP = decltype(rp)::value;
-    static const cudaError_t allowed = cudaFuncSetAttribute(
-        reinterpret_cast<const void*>(shrink_tc_kernel<RP, kTerms>),
-        cudaFuncAttributeMaxDynamicSharedMemorySize, kShrinkSmem<RP>);
-    if (allowed != cudaSuccess) return allowed;
-    cudaLaunchConfig_t cfg{};
-    const int jobs = (w != nullptr ? 1 : 0) + (v_in != nullptr ? 1 : 0);
-    cfg.gridDim = dim3(static_cast<unsigned>(pl.max_tiles) * cluster * jobs);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kShrinkSmem<RP>;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, shrink_tc_kernel<RP, kTerms>, a);
   });
 }
 
@@ -1674,20 +1672,23 @@ cudaError_t run_expand_tc(const AdapterProblem& p, const Plan& pl, const Route& 
   });
 }
 
-GradSide grad_side(const LowRank& u, const __nv_bfloat16* terms, const void* x, tbn_dtype dt,
-                   int64_t ldx, int64_t K, float* part, float* out) {
-  return {u, terms, x, part, out, ldx, static_cast<int>(K),
+GradSide grad_side(const __nv_bfloat16* terms, const void* x, tbn_dtype dt, int64_t ldx, int64_t K,
+                   float* part, float* out) {
+  return {terms, x, part, out, ldx, static_cast<int>(K),
           rows_aligned(x, ldx, K, dtype_size(dt), 16)};
 }
 
-cudaError_t run_grad(const AdapterProblem& p, const Plan& pl, const Route& route,
-                     const GradSide& side, tbn_dtype dt, cudaStream_t s) {
-  const GradArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, side};
-  const dim3 grid(pl.max_items, static_cast<unsigned>((side.K + kCols - 1) / kCols));
+// One gradient, or both where x and dy have the same type.
+cudaError_t run_grads(const AdapterProblem& p, const Plan& pl, const Route& route,
+                      const GradSide* sides, int count, tbn_dtype dt, cudaStream_t s) {
+  const auto tiles = [](const GradSide& d) { return (d.K + kCols - 1) / kCols; };
+  const GradArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, {sides[0], sides[count - 1]},
+                   tiles(sides[0])};
+  const dim3 grid(pl.max_items, static_cast<unsigned>(tiles(sides[0]) + (count > 1 ? tiles(sides[1]) : 0)));
   return by_rank(p.r, [&](auto rp) {
     constexpr int RP = decltype(rp)::value;
     const int terms = dt == TBN_BF16 ? 1 : 3;
-    const size_t smem = 3 * static_cast<size_t>((RP + 63) / 64 * kHalf) + terms * 2 * kHalf;
+    const size_t smem = 2 * static_cast<size_t>((3 * RP + 63) / 64 * kHalf) + terms * 2 * kHalf;
     if (dt == TBN_BF16) return go<grad_kernel<__nv_bfloat16, RP>>(grid, kThreads, smem, s, a);
     return go<grad_kernel<float, RP>>(grid, kThreads, smem, s, a);
   });
@@ -1749,22 +1750,17 @@ tbn_status launch_adapter_fwd(const AdapterProblem& p, void* ws, cudaStream_t s)
   if (adapter_small_takes(p)) return launch_adapter_small(p, s);
   const Plan pl = make_plan(p.T, p.n, p.r, p.K_in, p.K_out, false, takes_tc(p, false));
   const Route route = route_at(pl, ws);
-  uint8_t* b = static_cast<uint8_t*>(ws);
+  __nv_bfloat16* terms = reinterpret_cast<__nv_bfloat16*>(static_cast<uint8_t*>(ws) + pl.v_terms);
+  const int count = p.ydt == TBN_BF16 ? 2 : 3;
   cudaError_t e = run_route(p, pl, route, s);
   if (e != cudaSuccess) return cuda_fail(e, "adapter route_kernel");
-  if (pl.tc) {
-    __nv_bfloat16* terms = reinterpret_cast<__nv_bfloat16*>(b + pl.v_terms);
-    e = run_shrink_tc<2>(p, pl, route, p.x, p.ldx, p.a, p.K_in, pl.cluster_in, terms, p.v_out, nullptr,
-                         nullptr, s);
-    if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_tc_kernel");
-    e = run_expand_tc(p, pl, route, terms, 2, p.b, p.K_out, p.base, p.ldbase, p.y, p.ldy, s);
-    return e == cudaSuccess ? TBN_OK : cuda_fail(e, "adapter expand_tc_kernel");
-  }
-  float* part = reinterpret_cast<float*>(b + pl.v);
-  e = run_shrink(p, pl, route, p.x, p.xdt, p.ldx, p.a, p.K_in, pl.splits_in, pl.per_in, part, s);
+  e = run_shrink(p, pl, route, p.x, p.xdt, p.ldx, p.a, p.K_in, pl.cluster_in, terms, count, p.v_out, nullptr,
+                 nullptr, s);
   if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_kernel");
-  const LowRank v{part, p.T * p.r, pl.splits_in, 0};
-  e = run_expand(p, pl, route, v, p.b, p.K_out, p.base, p.ldbase, p.y, p.ydt, p.ldy, p.v_out, s);
+  if (pl.tc)
+    e = run_expand_tc(p, pl, route, terms, count, p.b, p.K_out, p.base, p.ldbase, p.y, p.ldy, s);
+  else
+    e = run_expand(p, pl, route, terms, count, p.b, p.K_out, p.base, p.ldbase, p.y, p.ydt, p.ldy, s);
   return e == cudaSuccess ? TBN_OK : cuda_fail(e, "adapter expand_kernel");
 }
 
@@ -1772,64 +1768,52 @@ tbn_status launch_adapter_bwd(const AdapterProblem& p, void* ws, cudaStream_t s)
   const Plan pl = make_plan(p.T, p.n, p.r, p.K_in, p.K_out, true, takes_tc(p, true));
   const Route route = route_at(pl, ws);
   uint8_t* b = static_cast<uint8_t*>(ws);
-  float* vpart = reinterpret_cast<float*>(b + pl.v);
-  float* dupart = reinterpret_cast<float*>(b + pl.du);
   __nv_bfloat16* v_terms = reinterpret_cast<__nv_bfloat16*>(b + pl.v_terms);
   __nv_bfloat16* du_terms = reinterpret_cast<__nv_bfloat16*>(b + pl.du_terms);
   const bool need_du = p.dx != nullptr || p.da != nullptr;
   cudaError_t e = run_route(p, pl, route, s);
   if (e != cudaSuccess) return cuda_fail(e, "adapter route_kernel");
-  LowRank v{p.v, 0, 1, 1};
-  const LowRank u{dupart, p.T * p.r, pl.splits_out, 0};
-  if (pl.tc) {
+  if (p.T > 0) {
     // du, and v's terms beside it; v itself first where it is not there
     if (p.db != nullptr && p.v == nullptr)
-      e = run_shrink_tc<3>(p, pl, route, p.x, p.ldx, p.a, p.K_in, pl.cluster_in, v_terms, nullptr, nullptr,
-                           nullptr, s);
+      e = run_shrink(p, pl, route, p.x, p.xdt, p.ldx, p.a, p.K_in, pl.cluster_in, v_terms, 3, nullptr,
+                     nullptr, nullptr, s);
     const float* v_in = p.db != nullptr ? p.v : nullptr;
     if (e == cudaSuccess && (need_du || v_in != nullptr))
-      e = run_shrink_tc<3>(p, pl, route, p.dy, p.lddy, need_du ? p.b : nullptr, p.K_out, pl.cluster_out,
-                           du_terms, nullptr, v_in, v_terms, s);
-    if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_tc_kernel");
-  } else if (p.T > 0) {
-    if (need_du) {
-      e = run_shrink(p, pl, route, p.dy, p.ydt, p.lddy, p.b, p.K_out, pl.splits_out, pl.per_out,
-                     dupart, s);
-      if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_kernel");
-    }
-    if (p.db != nullptr && p.v == nullptr) {
-      e = run_shrink(p, pl, route, p.x, p.xdt, p.ldx, p.a, p.K_in, pl.splits_in, pl.per_in, vpart, s);
-      if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_kernel");
-      v = {vpart, p.T * p.r, pl.splits_in, 0};
-    }
+      e = run_shrink(p, pl, route, p.dy, p.ydt, p.lddy, need_du ? p.b : nullptr, p.K_out, pl.cluster_out,
+                     du_terms, 3, nullptr, v_in, v_terms, s);
+    if (e != cudaSuccess) return cuda_fail(e, "adapter shrink_kernel");
   }
   GradSide sides[2];
   tbn_dtype types[2];
   int count = 0;
   if (p.da != nullptr) {
     types[count] = p.xdt;
-    sides[count++] = grad_side(u, du_terms, p.x, p.xdt, p.ldx, p.K_in,
-                               reinterpret_cast<float*>(b + pl.part_a), p.da);
+    sides[count++] = grad_side(du_terms, p.x, p.xdt, p.ldx, p.K_in, reinterpret_cast<float*>(b + pl.part_a),
+                               p.da);
   }
   if (p.db != nullptr) {
     types[count] = p.ydt;
-    sides[count++] = grad_side(v, v_terms, p.dy, p.ydt, p.lddy, p.K_out,
-                               reinterpret_cast<float*>(b + pl.part_b), p.db);
+    sides[count++] = grad_side(v_terms, p.dy, p.ydt, p.lddy, p.K_out, reinterpret_cast<float*>(b + pl.part_b),
+                               p.db);
   }
-  e = cudaSuccess;
-  if (pl.tc && count > 0) {
-    e = run_grads_tc(p, pl, route, sides, count, s);
-  } else if (p.T > 0) {
-    for (int i = 0; i < count && e == cudaSuccess; ++i) e = run_grad(p, pl, route, sides[i], types[i], s);
+  if (count > 0) {
+    if (pl.tc) {
+      e = run_grads_tc(p, pl, route, sides, count, s);
+    } else if (p.T > 0) {
+      const bool together = count == 1 || types[0] == types[1];
+      e = run_grads(p, pl, route, sides, together ? count : 1, types[0], s);
+      if (!together && e == cudaSuccess) e = run_grads(p, pl, route, sides + 1, 1, types[1], s);
+    }
+    if (e == cudaSuccess) e = run_reduce(p, route, sides, count, s);
+    if (e != cudaSuccess) return cuda_fail(e, "adapter grad_kernel");
   }
-  if (count > 0 && e == cudaSuccess) e = run_reduce(p, route, sides, count, s);
-  if (e != cudaSuccess) return cuda_fail(e, "adapter grad_kernel");
   // last: dx may be written over x or over the base
   if (p.dx != nullptr && p.T > 0) {
     if (pl.tc)
       e = run_expand_tc(p, pl, route, du_terms, 3, p.a, p.K_in, p.base, p.ldbase, p.dx, p.lddx, s);
     else
-      e = run_expand(p, pl, route, u, p.a, p.K_in, p.base, p.ldbase, p.dx, p.xdt, p.lddx, nullptr, s);
+      e = run_expand(p, pl, route, du_terms, 3, p.a, p.K_in, p.base, p.ldbase, p.dx, p.xdt, p.lddx, s);
     if (e != cudaSuccess) return cuda_fail(e, "adapter expand_kernel");
   }
   return TBN_OK;
