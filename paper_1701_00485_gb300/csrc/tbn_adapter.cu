@@ -85,16 +85,16 @@ __device__ __forceinline__ void split(float v, float (&t)[kTerms]) {
   }
 }
 
-// Two neighbouring values into the kTerms tiles at `tile`, `stride` bytes apart.
+// Eight values as kTerms 16-byte chunks.
 template <int kTerms>
-__device__ __forceinline__ void store_pair(uint8_t* tile, uint32_t stride, uint32_t off, float v0,
-                                           float v1) {
-  float a[kTerms], b[kTerms];
-  split(v0, a);
-  split(v1, b);
+__device__ __forceinline__ void split8(const float (&v)[8], uint4 (&out)[kTerms]) {
+  float t[8][kTerms];
 #pragma unroll
-  for (int i = 0; i < kTerms; ++i)
-    *reinterpret_cast<uint32_t*>(tile + i * stride + off) = pack_bf16x2(a[i], b[i]);
+  for (int j = 0; j < 8; ++j) split(v[j], t[j]);
+#pragma unroll
+  for (int k = 0; k < kTerms; ++k)
+    out[k] = make_uint4(pack_bf16x2(t[0][k], t[1][k]), pack_bf16x2(t[2][k], t[3][k]),
+                        pack_bf16x2(t[4][k], t[5][k]), pack_bf16x2(t[6][k], t[7][k]));
 }
 
 // The 16-byte words that hold elements [at, at + 16 kWords / sizeof(T)) of the row
@@ -179,10 +179,14 @@ __device__ __forceinline__ void store_piece(uint8_t* tile, uint32_t, int row, in
 __device__ __forceinline__ void store_piece(uint8_t* tile, uint32_t stride, int row, int c,
                                             const Piece<float>& d) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t off = tile_off(row, c + i / 2) + 8 * (i % 2);
-    store_pair<3>(tile, stride, off, __uint_as_float(d.q[i].x), __uint_as_float(d.q[i].y));
-    store_pair<3>(tile, stride, off + 4, __uint_as_float(d.q[i].z), __uint_as_float(d.q[i].w));
+  for (int i = 0; i < 2; ++i) {
+    const uint4 &p = d.q[2 * i], &q = d.q[2 * i + 1];
+    const float v[8] = {__uint_as_float(p.x), __uint_as_float(p.y), __uint_as_float(p.z), __uint_as_float(p.w),
+                        __uint_as_float(q.x), __uint_as_float(q.y), __uint_as_float(q.z), __uint_as_float(q.w)};
+    uint4 t[3];
+    split8(v, t);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(tile + k * stride + tile_off(row, c + i)) = t[k];
   }
 }
 
@@ -345,15 +349,14 @@ __device__ __forceinline__ float4 load_cluster(uint32_t addr, int rank) {
 template <int RP, int kTerms>
 __device__ __forceinline__ void write_terms(const float (&v)[8], float factor, int col, int rank,
                                             int64_t at, __nv_bfloat16* terms) {
-  float t[8][kTerms];
+  float u[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) split(col + j < rank ? v[j] * factor : 0.0f, t[j]);
-  __nv_bfloat16* out = terms + at * (kTerms * RP) + col;
+  for (int j = 0; j < 8; ++j) u[j] = col + j < rank ? v[j] * factor : 0.0f;
+  uint4 t[kTerms];
+  split8(u, t);
 #pragma unroll
   for (int k = 0; k < kTerms; ++k)
-    *reinterpret_cast<uint4*>(out + k * RP) =
-        make_uint4(pack_bf16x2(t[0][k], t[1][k]), pack_bf16x2(t[2][k], t[3][k]),
-                   pack_bf16x2(t[4][k], t[5][k]), pack_bf16x2(t[6][k], t[7][k]));
+    *reinterpret_cast<uint4*>(terms + at * (kTerms * RP) + k * RP + col) = t[k];
 }
 
 template <int RP>
@@ -561,26 +564,34 @@ struct ExpandArgs {
   int w_aligned, y_aligned;
 };
 
-// CTA (tile, column group): 64 tokens x cols_per * 128 columns.  Warp w takes 16
-// tokens and 64 of the 128 columns; the sums leave through shared memory so that
-// a warp reads the base and writes the result in whole rows, eight of them, whose
-// base is asked for before the product.  y has 16 bits with two terms, 32 with three.
+constexpr int kOutRow = 72;   // floats of a row of 64 sums: the pairs of an MMA in other banks
 template <int RP, int kTerms>
-__global__ void __launch_bounds__(kThreads, 2) expand_kernel(const __grid_constant__ ExpandArgs a) {
+constexpr int kExpandPlainSmem =
+    kTerms * ((RP + 63) / 64 * kHalf) + 4 * RP * 128 + 8 * 16 * kOutRow * static_cast<int>(sizeof(float));
+
+// CTA (tile, column group): 64 tokens x cols_per * 128 columns.  Warp w takes 16
+// tokens and 64 of the 128 columns: its part of the base is in registers a step
+// ahead, goes to shared memory where the sums are added to it, and is written out in
+// rows.  y has 16 bits with two terms, 32 with three.
+template <int RP, int kTerms>
+__global__ void __launch_bounds__(kThreads, RP * kTerms > 256 ? 1 : 2) expand_kernel(const __grid_constant__ ExpandArgs a) {
   using Y = typename std::conditional<kTerms == 2, __nv_bfloat16, float>::type;
+  constexpr bool k16 = sizeof(Y) == 2;
   extern __shared__ __align__(128) uint8_t smem[];
   constexpr int kV = (RP + 63) / 64 * kHalf;          // bytes of one term of V
   constexpr int kW = RP * 128;                        // bytes of 64 columns of w
-  constexpr int kStride = kCols + 4;
+  constexpr int kLanes = k16 ? 8 : 16, kRows = 32 / kLanes, kPasses = 16 / kRows;   // aligned rows
+  constexpr int kWPieces = RP * 16 / kThreads;
   uint8_t* sv = smem;
-  uint8_t* sw = sv + kTerms * kV;
-  float* out = reinterpret_cast<float*>(sw + 2 * kW);  // [64][kStride]
+  uint8_t* sw = sv + kTerms * kV;                      // two stages
   grid_dependency_wait();
   grid_dependents_launch();
   if (static_cast<int>(blockIdx.x) >= a.route.counts[0]) return;
   const int4 tile = a.route.tiles[blockIdx.x];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int mi = lane >> 3, lr = lane & 7;
+  const int tg = 16 * (warp & 3), ch = warp >> 2;
+  float* out = reinterpret_cast<float*>(sw + 4 * kW) + warp * 16 * kOutRow;
   const bool none = tile.x < 0;
   const int rank = none ? 0 : a.ad.rank(tile.x), r = a.ad.r;
   const __nv_bfloat16* w = a.w + static_cast<int64_t>(none ? 0 : tile.x) * r * a.K;
@@ -592,62 +603,99 @@ __global__ void __launch_bounds__(kThreads, 2) expand_kernel(const __grid_consta
                  a.terms + (v ? static_cast<int64_t>(tile.y + m) * a.terms_row + 8 * c : 0), v);
     }
   cp_async_commit();
-  // the warp's tokens, one in each of eight lanes
-  const int mine = 8 * warp + lr < tile.z ? a.route.perm[tile.y + 8 * warp + lr] : -1;
-  const uint32_t sv_s = smem_addr(sv), sw_s = smem_addr(sw);
-  const int tg = 16 * (warp & 3), ch = warp >> 2;
-  const int col_beg = blockIdx.y * a.cols_per * kCols;
-  const int col_end = min(a.K, col_beg + a.cols_per * kCols);
-  for (int c0 = col_beg; c0 < col_end; c0 += kCols) {
-    // four columns a lane: side by side, or 32 apart in rows that are not aligned
-    const int e = a.y_aligned ? c0 + 4 * lane : c0 + lane;
-    uint32_t base[8][sizeof(Y) == 2 ? 2 : 4];
+  // the warp's tokens, one in each of sixteen lanes
+  const int mine = tg + (lane & 15) < tile.z ? a.route.perm[tile.y + tg + (lane & 15)] : -1;
+  const uint32_t sv_s = smem_addr(sv);
+  uint32_t base[k16 ? 16 : 32];
+  uint4 pw[kWPieces];
+  // the base of the warp's 64 columns from c on: in aligned rows a 16-byte word a
+  // lane, kRows rows at a time; else two elements a lane, 32 apart, row by row
+  const auto load = [&](int c) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int token = __shfl_sync(0xffffffffu, mine, j);
-      const Y* p = static_cast<const Y*>(a.base) + token * a.ldbase + e;
-      const bool in = a.base != nullptr && token >= 0;
-      if constexpr (sizeof(Y) == 2) {
-        base[j][0] = base[j][1] = 0u;
-        if (a.y_aligned) {
-          if (in && e < a.K) {
-            const uint2 v = *reinterpret_cast<const uint2*>(p);
-            base[j][0] = v.x;
-            base[j][1] = v.y;
+    for (int i = 0; i < (k16 ? 16 : 32); ++i) base[i] = 0u;
+    const Y* from = static_cast<const Y*>(a.base);
+    if (from != nullptr) {
+      if (a.y_aligned) {
+        const int e = c + lane % kLanes * (64 / kLanes);
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+          const int token = __shfl_sync(0xffffffffu, mine, kRows * i + lane / kLanes);
+          if (token >= 0 && e < a.K) {
+            const uint4 v = *reinterpret_cast<const uint4*>(from + token * a.ldbase + e);
+            base[4 * i] = v.x;
+            base[4 * i + 1] = v.y;
+            base[4 * i + 2] = v.z;
+            base[4 * i + 3] = v.w;
           }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (in && e + 32 * i < a.K)
-              base[j][i / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(p[32 * i])) << (16 * (i % 2));
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) base[j][i] = 0u;
-        if (a.y_aligned) {
-          if (in && e < a.K) {
-            const uint4 v = *reinterpret_cast<const uint4*>(p);
-            base[j][0] = v.x;
-            base[j][1] = v.y;
-            base[j][2] = v.z;
-            base[j][3] = v.w;
-          }
-        } else {
+        for (int m = 0; m < 16; ++m) {
+          const int token = __shfl_sync(0xffffffffu, mine, m);
+          const Y* p = from + token * a.ldbase + c + lane;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (in && e + 32 * i < a.K) base[j][i] = __float_as_uint(p[32 * i]);
+          for (int i = 0; i < 2; ++i)
+            if (token >= 0 && c + lane + 32 * i < a.K) {
+              if constexpr (k16)
+                base[m] |= static_cast<uint32_t>(__bfloat16_as_ushort(p[32 * i])) << (16 * i);
+              else
+                base[2 * m + i] = __float_as_uint(p[32 * i]);
+            }
         }
       }
     }
-    if (!none) {
+  };
+  const auto load_ws = [&](int c) {
 #pragma unroll
-      for (int i = 0; i < RP * 16 / kThreads; ++i) {
-        const int p = tid + i * kThreads, wr = p >> 4, pc = p & 15;
-        *reinterpret_cast<uint4*>(sw + (pc >> 3) * kW + tile_off(wr, pc & 7)) =
-            load_w(wr < rank ? w + static_cast<int64_t>(wr) * a.K : nullptr, c0 + 8 * pc, a.K, a.w_aligned);
+    for (int i = 0; i < kWPieces; ++i) {
+      const int p = tid + i * kThreads, wr = p >> 4;
+      pw[i] = load_w(wr < rank ? w + static_cast<int64_t>(wr) * a.K : nullptr, c + 8 * (p & 15), a.K,
+                     a.w_aligned);
+    }
+  };
+  const int col_beg = blockIdx.y * a.cols_per * kCols;
+  const int col_end = min(a.K, col_beg + a.cols_per * kCols);
+  load(col_beg + 64 * ch);
+  if (!none) load_ws(col_beg);
+  int turn = 0;
+  for (int c0 = col_beg; c0 < col_end; c0 += kCols, turn ^= 1) {
+    const int c = c0 + 64 * ch;
+    // the base, as fp32
+    if (a.y_aligned) {
+#pragma unroll
+      for (int i = 0; i < kPasses; ++i) {
+        float* to = out + (kRows * i + lane / kLanes) * kOutRow + lane % kLanes * (64 / kLanes);
+        const uint32_t* b = base + 4 * i;
+        if constexpr (k16) {
+#pragma unroll
+          for (int k = 0; k < 4; k += 2)
+            *reinterpret_cast<float4*>(to + 2 * k) =
+                make_float4(__uint_as_float(b[k] << 16), __uint_as_float(b[k] & 0xFFFF0000u),
+                            __uint_as_float(b[k + 1] << 16), __uint_as_float(b[k + 1] & 0xFFFF0000u));
+        } else {
+          *reinterpret_cast<uint4*>(to) = make_uint4(b[0], b[1], b[2], b[3]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < 16; ++m)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          out[m * kOutRow + lane + 32 * i] =
+              k16 ? __uint_as_float(i ? base[m] & 0xFFFF0000u : base[m] << 16) : __uint_as_float(base[2 * m + i]);
+    }
+    if (c0 + kCols < col_end) load(c + kCols);
+    if (!none) {
+      uint8_t* st = sw + turn * 2 * kW;
+#pragma unroll
+      for (int i = 0; i < kWPieces; ++i) {
+        const int p = tid + i * kThreads, pc = p & 15;
+        *reinterpret_cast<uint4*>(st + (pc >> 3) * kW + tile_off(p >> 4, pc & 7)) = pw[i];
       }
       cp_async_wait<0>();
-      __syncthreads();
+      __syncthreads();   // two stages: the one written next was read before this
+      if (c0 + kCols < col_end) load_ws(c0 + kCols);
+      const uint32_t sw_s = smem_addr(st) + ch * kW;
       float acc[8][4];
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -663,7 +711,7 @@ __global__ void __launch_bounds__(kThreads, 2) expand_kernel(const __grid_consta
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt) {
           uint32_t bf[4];
-          ldsm4_trans(bf, sw_s + ch * kW + tile_off(16 * ks + 8 * (mi & 1) + lr, 2 * nt + (mi >> 1)));
+          ldsm4_trans(bf, sw_s + tile_off(16 * ks + 8 * (mi & 1) + lr, 2 * nt + (mi >> 1)));
 #pragma unroll
           for (int t = 0; t < kTerms; ++t) {
             mma(acc[2 * nt], af[t], bf[0], bf[1]);
@@ -675,42 +723,42 @@ __global__ void __launch_bounds__(kThreads, 2) expand_kernel(const __grid_consta
 #pragma unroll
       for (int nt = 0; nt < 8; ++nt)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          *reinterpret_cast<float2*>(out + (tg + g + 8 * h) * kStride + 64 * ch + 8 * nt + t2) =
-              make_float2(acc[nt][2 * h], acc[nt][2 * h + 1]);
-      __syncthreads();
+        for (int h = 0; h < 2; ++h) {
+          float2* at = reinterpret_cast<float2*>(out + (g + 8 * h) * kOutRow + 8 * nt + t2);
+          *at = make_float2(at->x + acc[nt][2 * h], at->y + acc[nt][2 * h + 1]);
+        }
     }
+    __syncwarp();
+    if (a.y_aligned) {
+      const int e = c + lane % kLanes * (64 / kLanes);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int token = __shfl_sync(0xffffffffu, mine, j);
-      if (token < 0 || e >= a.K) continue;
-      const float* sum = out + (8 * warp + j) * kStride + (e - c0);
-      Y* y = static_cast<Y*>(a.y) + token * a.ldy + e;
-      float v[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(Y) == 2)
-          v[i] = __uint_as_float(i % 2 ? base[j][i / 2] & 0xFFFF0000u : base[j][i / 2] << 16);
+      for (int i = 0; i < kPasses; ++i) {
+        const int m = kRows * i + lane / kLanes, token = __shfl_sync(0xffffffffu, mine, m);
+        const float4* v = reinterpret_cast<const float4*>(out + m * kOutRow + lane % kLanes * (64 / kLanes));
+        if (token < 0 || e >= a.K) continue;
+        Y* y = static_cast<Y*>(a.y) + token * a.ldy + e;
+        if constexpr (k16)
+          *reinterpret_cast<uint4*>(y) =
+              make_uint4(pack_bf16x2(v[0].x, v[0].y), pack_bf16x2(v[0].z, v[0].w),
+                         pack_bf16x2(v[1].x, v[1].y), pack_bf16x2(v[1].z, v[1].w));
         else
-          v[i] = __uint_as_float(base[j][i]);
-        if (!none) v[i] += sum[a.y_aligned ? i : 32 * i];
+          *reinterpret_cast<float4*>(y) = v[0];
       }
-      if (a.y_aligned) {
-        if constexpr (sizeof(Y) == 2)
-          *reinterpret_cast<uint2*>(y) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-        else
-          *reinterpret_cast<float4*>(y) = make_float4(v[0], v[1], v[2], v[3]);
-      } else {
+    } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (e + 32 * i < a.K) {
-            if constexpr (sizeof(Y) == 2) y[32 * i] = __float2bfloat16_rn(v[i]);
-            else y[32 * i] = v[i];
+      for (int m = 0; m < 16; ++m) {
+        const int token = __shfl_sync(0xffffffffu, mine, m);
+        Y* y = static_cast<Y*>(a.y) + token * a.ldy + c + lane;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (token >= 0 && c + lane + 32 * i < a.K) {
+            const float v = out[m * kOutRow + lane + 32 * i];
+            if constexpr (k16) y[32 * i] = __float2bfloat16_rn(v);
+            else y[32 * i] = v;
           }
       }
     }
-    // (the next step's w and `out` are written behind what was read above: `sw` by
-    // the product, before the last barrier; `out` after the next one)
+    __syncwarp();
   }
 }
 
@@ -1646,13 +1694,10 @@ cudaError_t run_expand(const AdapterProblem& p, const Plan& pl, const Route& rou
     const ExpandArgs a{route, {p.ranks, p.scale, static_cast<int>(p.r)}, terms,
                        static_cast<const __nv_bfloat16*>(w), base, y, ldbase, ldy, terms_per * RP,
                        static_cast<int>(K), per, rows_aligned(w, K, K, 2, 16),
-                       rows_aligned(y, ldy, K, e, 4 * e) &&
-                           (base == nullptr || rows_aligned(base, ldbase, K, e, 4 * e))};
-    const int used = dt == TBN_BF16 ? 2 : 3;
-    const size_t smem = static_cast<size_t>(used) * ((RP + 63) / 64 * kHalf) + 2 * RP * 128 +
-                        sizeof(float) * kTile * (kCols + 4);
-    if (dt == TBN_BF16) return go<expand_kernel<RP, 2>>(grid, kThreads, smem, s, a);
-    return go<expand_kernel<RP, 3>>(grid, kThreads, smem, s, a);
+                       rows_aligned(y, ldy, K, e, 16) &&
+                           (base == nullptr || rows_aligned(base, ldbase, K, e, 16))};
+    if (dt == TBN_BF16) return go<expand_kernel<RP, 2>>(grid, kThreads, kExpandPlainSmem<RP, 2>, s, a);
+    return go<expand_kernel<RP, 3>>(grid, kThreads, kExpandPlainSmem<RP, 3>, s, a);
   });
 }
 
