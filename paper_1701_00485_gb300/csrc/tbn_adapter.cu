@@ -97,97 +97,141 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 (&out)[kTerms]
                         pack_bf16x2(t[4][k], t[5][k]), pack_bf16x2(t[6][k], t[7][k]));
 }
 
-// The 16-byte words that hold elements [at, at + 16 kWords / sizeof(T)) of the row
-// at p, of which K exist; zeros past the end and for p = nullptr.  In a row that is
-// not aligned, words begin in front of `at` and there is one more of them; straighten
-// shifts them into place.  (Element by element an unaligned row took eight times as
-// many loads, and its lines were looked up for each of them.)
-template <int kWords, typename T>
-__device__ __forceinline__ void load_words(uint4 (&d)[kWords + 1], const T* p, int at, int K, bool aligned) {
-  constexpr int kPer = 16 / sizeof(T);
-  const int skew = aligned ? 0 : static_cast<int>((reinterpret_cast<uintptr_t>(p) + at * sizeof(T)) / sizeof(T) % kPer);
+// Eight elements from e on of the row at p, of which those in [0, K) exist; the rest
+// are zeros.
+__device__ __forceinline__ uint4 word_at(const __nv_bfloat16* p, int e, int K) {
+  if (e >= 0 && e + 8 <= K) return __ldg(reinterpret_cast<const uint4*>(p + e));
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-  for (int i = 0; i < kWords + 1; ++i) {
-    const int e = at - skew + kPer * i;
-    d[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (p == nullptr || e >= K || (i == kWords && skew == 0)) continue;
-    if (e >= 0 && e + kPer <= K) {
-      d[i] = __ldg(reinterpret_cast<const uint4*>(p + e));
-    } else {   // it begins in front of the row or ends behind it
-      uint32_t w[4] = {0u, 0u, 0u, 0u};
+  for (int j = 0; j < 8; ++j)
+    if (e + j >= 0 && e + j < K)
+      w[j / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(p[e + j])) << (16 * (j % 2));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// 64 columns of a warp's eight rows of a tile, held as they come.  In aligned rows a
+// lane has 16-byte words and neighbouring lanes neighbouring ones.  In others it has
+// of bf16 the three aligned words that hold a quarter of a row, which begins `skew`
+// elements into them (4095 -> 4095, backward of 8192 tokens: element by element 278
+// us, so 231), and of fp32 two neighbouring elements of each row.
+template <typename T>
+struct Rows {
+  uint32_t w[sizeof(T) == 2 ? 12 : 16];
+  uint32_t skew;
+};
+template <typename T>
+constexpr int kRowLanes = 64 * static_cast<int>(sizeof(T)) / 16;   // of an aligned row
+
+// mine: the row of x that is row lane % 8, or -1.  From column c on; zeros past K.
+template <typename T>
+__device__ __forceinline__ void load_rows(Rows<T>& d, const T* x, int64_t ldx, int mine, int c, int K,
+                                          bool aligned) {
+  constexpr int L = kRowLanes<T>, kAtOnce = 32 / L;
+  const int lane = threadIdx.x & 31;
+  if (aligned) {
+    const int e = c + lane % L * (64 / L);
 #pragma unroll
-      for (int j = 0; j < kPer; ++j)
-        if (e + j >= 0 && e + j < K) {
-          if constexpr (sizeof(T) == 2)
-            w[j / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(p[e + j])) << (16 * (j % 2));
-          else
-            w[j] = __float_as_uint(p[e + j]);
-        }
-      d[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < 8 / kAtOnce; ++i) {
+      const int at = __shfl_sync(0xffffffffu, mine, kAtOnce * i + lane / L);
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (at >= 0 && e < K) v = __ldg(reinterpret_cast<const uint4*>(x + at * ldx + e));
+      d.w[4 * i] = v.x;
+      d.w[4 * i + 1] = v.y;
+      d.w[4 * i + 2] = v.z;
+      d.w[4 * i + 3] = v.w;
+    }
+  } else {
+    if constexpr (sizeof(T) == 2) {
+      const int at = __shfl_sync(0xffffffffu, mine, lane / 4);
+      const T* p = x + at * ldx;
+      d.skew = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p + c) / 2 % 8);
+      const int e = c + 16 * (lane % 4) - static_cast<int>(d.skew);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (at >= 0 && (i < 2 || d.skew != 0)) v = word_at(p, e + 8 * i, K);
+        d.w[4 * i] = v.x;
+        d.w[4 * i + 1] = v.y;
+        d.w[4 * i + 2] = v.z;
+        d.w[4 * i + 3] = v.w;
+      }
+    } else {
+      const int e = c + 2 * lane;
+#pragma unroll
+      for (int m = 0; m < 8; ++m) {
+        const int at = __shfl_sync(0xffffffffu, mine, m);
+        const T* p = x + at * ldx + e;
+        d.w[2 * m] = at >= 0 && e < K ? __float_as_uint(p[0]) : 0u;
+        d.w[2 * m + 1] = at >= 0 && e + 1 < K ? __float_as_uint(p[1]) : 0u;
+      }
     }
   }
 }
 
-// `from`: the address of the first element wanted.
-template <int kWords, typename T>
-__device__ __forceinline__ void straighten(uint4 (&d)[kWords + 1], const T* from) {
-  constexpr int N = 4 * (kWords + 1);
-  const uint32_t skew = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(from)) & 15u;
-  uint32_t w[N];
-#pragma unroll
-  for (int i = 0; i <= kWords; ++i) {
-    w[4 * i] = d[i].x;
-    w[4 * i + 1] = d[i].y;
-    w[4 * i + 2] = d[i].z;
-    w[4 * i + 3] = d[i].w;
-  }
-#pragma unroll
-  for (int i = 0; i < N - 1; ++i) w[i] = skew & 4u ? w[i + 1] : w[i];
-#pragma unroll
-  for (int i = 0; i < N - 3; ++i) w[i] = skew & 8u ? w[i + 2] : w[i];
-  if constexpr (sizeof(T) == 2) {
-#pragma unroll
-    for (int i = 0; i < N - 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 8 * (skew & 2u));
-  }
-#pragma unroll
-  for (int i = 0; i < kWords; ++i) d[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-}
-
-// Sixteen consecutive elements of a row, held as they come.
+// Into rows 8 warp .. of a tile, fp32 values into the three tiles of their terms,
+// `stride` bytes apart.
 template <typename T>
-constexpr int kPieceWords = static_cast<int>(sizeof(T));
-template <typename T>
-struct Piece {
-  uint4 q[kPieceWords<T> + 1];
-};
-
-// Eight consecutive elements of a row of a or b, at once in place.
-__device__ __forceinline__ uint4 load_w(const __nv_bfloat16* p, int at, int K, bool aligned) {
-  uint4 d[2];
-  load_words<1>(d, p, at, K, aligned);
-  if (!aligned) straighten<1>(d, p + at);
-  return d[0];
-}
-
-// Into chunks c and c + 1 of a row of the tile (fp32: of its three terms).
-__device__ __forceinline__ void store_piece(uint8_t* tile, uint32_t, int row, int c,
-                                            const Piece<__nv_bfloat16>& d) {
-  *reinterpret_cast<uint4*>(tile + tile_off(row, c)) = d.q[0];
-  *reinterpret_cast<uint4*>(tile + tile_off(row, c + 1)) = d.q[1];
-}
-
-__device__ __forceinline__ void store_piece(uint8_t* tile, uint32_t stride, int row, int c,
-                                            const Piece<float>& d) {
+__device__ __forceinline__ void store_rows(uint8_t* tile, uint32_t stride, const Rows<T>& d, bool aligned) {
+  constexpr int L = kRowLanes<T>, kAtOnce = 32 / L;
+  const int lane = threadIdx.x & 31, row0 = threadIdx.x >> 5 << 3;
+  if (aligned) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint4 &p = d.q[2 * i], &q = d.q[2 * i + 1];
-    const float v[8] = {__uint_as_float(p.x), __uint_as_float(p.y), __uint_as_float(p.z), __uint_as_float(p.w),
-                        __uint_as_float(q.x), __uint_as_float(q.y), __uint_as_float(q.z), __uint_as_float(q.w)};
-    uint4 t[3];
-    split8(v, t);
+    for (int i = 0; i < 8 / kAtOnce; ++i) {
+      const int row = row0 + kAtOnce * i + lane / L;
+      const uint32_t* v = d.w + 4 * i;
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<uint4*>(tile + tile_off(row, lane % L)) = make_uint4(v[0], v[1], v[2], v[3]);
+      } else {
+        float t[4][3];
 #pragma unroll
-    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(tile + k * stride + tile_off(row, c + i)) = t[k];
+        for (int j = 0; j < 4; ++j) split(__uint_as_float(v[j]), t[j]);
+        uint8_t* to = tile + tile_off(row, lane % L / 2) + 8 * (lane & 1);
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+          *reinterpret_cast<uint2*>(to + k * stride) =
+              make_uint2(pack_bf16x2(t[0][k], t[1][k]), pack_bf16x2(t[2][k], t[3][k]));
+      }
+    }
+  } else {
+    if constexpr (sizeof(T) == 2) {
+      uint32_t w[12];
+#pragma unroll
+      for (int k = 0; k < 12; ++k) w[k] = d.w[k];
+#pragma unroll
+      for (int k = 0; k < 11; ++k) w[k] = d.skew & 2u ? w[k + 1] : w[k];
+#pragma unroll
+      for (int k = 0; k < 9; ++k) w[k] = d.skew & 4u ? w[k + 2] : w[k];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16 * (d.skew & 1u));
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        *reinterpret_cast<uint4*>(tile + tile_off(row0 + lane / 4, 2 * (lane % 4) + k)) =
+            make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+    } else {
+#pragma unroll
+      for (int m = 0; m < 8; ++m) {
+        uint8_t* to = tile + tile_off(row0 + m, lane / 4) + 4 * (lane & 3);
+        float t[2][3];
+        split(__uint_as_float(d.w[2 * m]), t[0]);
+        split(__uint_as_float(d.w[2 * m + 1]), t[1]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+          *reinterpret_cast<uint32_t*>(to + k * stride) = pack_bf16x2(t[0][k], t[1][k]);
+      }
+    }
   }
+}
+
+// Eight elements from e on of a row of a or b, zeros past K and for p = nullptr.
+__device__ __forceinline__ uint4 load_w(const __nv_bfloat16* p, int e, int K, bool aligned) {
+  uint4 v = make_uint4(0u, 0u, 0u, 0u);
+  if (p == nullptr || e >= K) return v;
+  if (aligned) return __ldg(reinterpret_cast<const uint4*>(p + e));
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (e + j < K) w[j / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(p[e + j])) << (16 * (j % 2));
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 template <typename T>
@@ -461,15 +505,14 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
   const float factor = a.ad.factor(tile.x);
   if (second)
     return terms_of<RP, kTile>(a.v_in, tile, split, a.splits, rank, r, factor, a.route.perm, a.v_terms);
-  const int row = tid >> 2, q = tid & 3;
-  const T* xrow = nullptr;
-  if (row < tile.z)
-    xrow = static_cast<const T*>(a.x) + a.route.perm[tile.y + row] * a.ldx;
+  // the warp's tokens, one in each of eight lanes
+  const int mine = 8 * warp + (lane & 7) < tile.z ? a.route.perm[tile.y + 8 * warp + (lane & 7)] : -1;
+  const T* x = static_cast<const T*>(a.x);
   const __nv_bfloat16* w = a.w + static_cast<int64_t>(tile.x) * r * a.K;
-  Piece<T> px;
+  Rows<T> px;
   uint4 pw[kPieces];
   const auto load = [&](int c) {
-    load_words<kPieceWords<T>>(px.q, xrow, c * kChunk + 16 * q, a.K, a.x_aligned);
+    load_rows(px, x, a.ldx, mine, c * kChunk, a.K, a.x_aligned);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int p = tid + i * kThreads, wr = p >> 3;
@@ -493,8 +536,7 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
   for (int c = split; c < a.chunks; c += a.splits, turn ^= 1) {
     uint8_t* st = smem + turn * kStage;
     uint8_t* sw = st + kTerms * kHalf;
-    if (!a.x_aligned) straighten<kPieceWords<T>>(px.q, xrow + c * kChunk + 16 * q);
-    store_piece(st, kHalf, row, 2 * q, px);
+    store_rows(st, kHalf, px, a.x_aligned);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int p = tid + i * kThreads;
@@ -800,18 +842,16 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const __grid_constant__ 
   const bool first = static_cast<int>(blockIdx.y) < a.tiles0;
   const GradSide& sd = a.side[first ? 0 : 1];
   const int c0 = (first ? blockIdx.y : blockIdx.y - a.tiles0) * kCols;
-  const int row = tid >> 2, q = tid & 3;
   const uint32_t su_s = smem_addr(smem), sx_s = smem_addr(sx);
-  Piece<T> px[2];
-  const T* at = nullptr;   // of the rows held
-  int token = row < item.z ? a.route.perm[item.y + row] : -1;
+  Rows<T> px[2];
+  const int row = 8 * warp + (lane & 7);   // of a step
+  int mine = row < item.z ? a.route.perm[item.y + row] : -1;   // the token there in the next one
   const auto load = [&](int t0) {
-    at = token >= 0 ? static_cast<const T*>(sd.x) + token * sd.ldx : nullptr;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-      load_words<kPieceWords<T>>(px[h].q, at, c0 + 64 * h + 16 * q, sd.K, sd.x_aligned);
+      load_rows(px[h], static_cast<const T*>(sd.x), sd.ldx, mine, c0 + 64 * h, sd.K, sd.x_aligned);
     const int next = t0 + kTile + row;
-    token = next < item.z ? a.route.perm[item.y + next] : -1;
+    mine = next < item.z ? a.route.perm[item.y + next] : -1;
     const uint32_t su = su_s + (t0 / kTile & 1) * kU;
     for (int i = tid; i < kTile * 3 * RP / 8; i += kThreads) {
       const int m = i / (3 * RP / 8), c = i % (3 * RP / 8);
@@ -833,10 +873,7 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const __grid_constant__ 
   for (int t0 = 0; t0 < item.z; t0 += kTile) {
     __syncthreads();
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (!sd.x_aligned) straighten<kPieceWords<T>>(px[h].q, at + c0 + 64 * h + 16 * q);
-      store_piece(sx + h * kHalf, 2 * kHalf, row, 2 * q, px[h]);
-    }
+    for (int h = 0; h < 2; ++h) store_rows(sx + h * kHalf, 2 * kHalf, px[h], sd.x_aligned);
     cp_async_wait<0>();
     __syncthreads();
     if (t0 + kTile < item.z) load(t0 + kTile);
