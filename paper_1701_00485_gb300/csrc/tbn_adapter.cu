@@ -961,7 +961,11 @@ __global__ void __launch_bounds__(256) grad_reduce_kernel(const __grid_constant_
 // memory.  The low-rank activations between two products are kept as
 // bf16 terms.
 constexpr int kTcTile = 128;
-constexpr int64_t kTcFrom = 128;   // tokens
+// Tokens from which the tensor-core kernels are quicker.  4096 -> 4096, us with them
+// and with the others: forward rank 16 384 tokens 16.2 and 13.6, rank 64 512 tokens 19.1
+// and 18.2, 700 tokens 22.7 and 24.5; backward rank 32 320 tokens 25.6 and 24.2, rank
+// 64 384 tokens 35.4 and 36.8, rank 32 700 tokens 29.5 and 34.7.
+constexpr int64_t kTcFrom = 384;
 constexpr int64_t kPrefetchBytes = int64_t(80) << 20;   // of the 129 MB of L2
 constexpr int kGradCtas = 2;        // of grad
 constexpr uint64_t kWaitLimitNs = 1000000000ull;

@@ -295,10 +295,15 @@ cudaError_t launch(const SmallArgs& a, bool aligned, int groups, cudaStream_t s)
 
 }  // namespace
 
-// Every cluster reads its adapter from L2, so tokens that share one cost what
-// others do; past this much the tiled kernels are quicker.
+// Every cluster reads its adapter from L2, so tokens that share one cost what others
+// do, 0.6 us for 2^21 multiplications beside 8 for the launch; the tiled kernels take
+// about 15 us and 0.25 for each adapter in use, of which there are n at most.  4096 ->
+// 4096, us here and tiled: 64 tokens of 64 adapters, rank 16, 10.3 and 28.8, 256 of
+// 256 48.8 and 93.3, 32 of one, rank 64, 14.6 and 15.2; but 64 of one, rank 64, 18.9
+// and 16.0, 256 of one, rank 16, 25.1 and 15.1.
 bool adapter_small_takes(const AdapterProblem& p) {
-  return p.T <= kMaxTokens && p.T * p.r * (p.K_in + p.K_out) <= (int64_t(1) << 28);
+  const int64_t used = p.n < p.T ? p.n : p.T;
+  return p.T <= kMaxTokens && p.T * p.r * (p.K_in + p.K_out) <= (24 + 0.8 * used) * (int64_t(1) << 20);
 }
 
 tbn_status launch_adapter_small(const AdapterProblem& p, cudaStream_t s) {
