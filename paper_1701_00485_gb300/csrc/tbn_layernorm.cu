@@ -76,7 +76,11 @@ struct Row {
 #pragma unroll
         for (int k = 0; k < kVec; ++k) {
           const int e = slot<false>(j, k, t, threads);
-          w[j][k] = e < D ? __float_as_uint(static_cast<float>(p[e])) : 0u;
+          // (bf16 as its 16 bits: a conversion here would wait for the row)
+          if constexpr (sizeof(T) == 2)
+            w[j][k] = e < D ? __bfloat16_as_ushort(p[e]) : 0u;
+          else
+            w[j][k] = e < D ? __float_as_uint(p[e]) : 0u;
         }
       }
     }
@@ -100,6 +104,8 @@ struct Row {
   __device__ __forceinline__ uint64_t pair(int j, int i) const {
     if constexpr (kAligned && sizeof(T) == 2)
       return f32x2(w[j][i] << 16, w[j][i] & 0xFFFF0000u);
+    else if constexpr (sizeof(T) == 2)
+      return f32x2(w[j][2 * i] << 16, w[j][2 * i + 1] << 16);
     else
       return f32x2(w[j][2 * i], w[j][2 * i + 1]);
   }
