@@ -14,12 +14,12 @@
 // is held in 32 bits and taken in an order that depends on the sizes alone.
 //
 // Many aligned rows of 17 to 1024 vectors run on teams with rings of rows
-// (below); short rows by groups of lanes; few rows, rows of odd length or
-// alignment and longer ones by a block each.  Measured (GB300, HBM copy 6.8
-// TB/s), 16384 x 4096 bf16: forward 46.7 us (5.7 TB/s), backward with dres 82.2
-// us (6.5 TB/s); before the rings 58 and 113 us, where what the threads had
-// asked for did not cover the time until it came.  One row of 4096: 5.8 us a call
-// from Python, most of it the host's.
+// (below); short rows by groups of lanes; few rows and longer ones by a block each;
+// many rows of odd length or alignment by blocks that stay, element by element.
+// Measured (GB300, HBM copy 6.8 TB/s), 16384 x 4096 bf16: forward 46.7 us (5.7
+// TB/s), backward with dres 82.2 us (6.5 TB/s); before the rings 58 and 113 us, where
+// what the threads had asked for did not cover the time until it came.  One row of
+// 4096: 5.8 us a call from Python, most of it the host's.
 #include <cuda_bf16.h>
 
 #include "tbn_device.cuh"
@@ -329,6 +329,49 @@ __global__ void __launch_bounds__(G != 0 ? 256 : NV > 2 ? 512 : 1024)
       if (t == 0 && j == 0) write_statistics(a, st[q], at);
       write_vec<Row<T, kAligned, NV>, kAligned>(x[q], j, a, st[q], g, b, at, t, threads);
     }
+  }
+}
+
+// Many rows that are not aligned: blocks stay, gamma and beta are read once and the
+// next row is on its way while this one is reduced.  30000 x 1001 bf16 54 us (blocks
+// that take a row each 117), 66033 x 111 10 (13), 65536 x 511 59 (63); 5000 x 111
+// 3.0 (2.6).
+template <typename T, int G, int NV>
+__global__ void __launch_bounds__(G != 0 ? 256 : 512) layernorm_fwd_stay_kernel(const FwdArgs a) {
+  __shared__ float red[2][32];
+  constexpr int kGroups = G != 0 ? 256 / (G != 0 ? G : 1) : 1;
+  const int threads = G != 0 ? G : blockDim.x;
+  const int t = G != 0 ? threadIdx.x % (G != 0 ? G : 1) : threadIdx.x;
+  const int group = G != 0 ? threadIdx.x / (G != 0 ? G : 1) : 0;
+  grid_dependency_wait();
+  grid_dependents_launch();
+  uint64_t g[NV][kPairs], b[NV][kPairs];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    load_weight<false>(a.gamma, a.w_bf16, 1.0f, a.D, j, t, threads, g[j]);
+    load_weight<false>(a.beta, a.w_bf16, 0.0f, a.D, j, t, threads, b[j]);
+  }
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * kGroups;
+  const float n = static_cast<float>(a.D);
+  int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+  Row<T, false, NV> next;
+  const auto load = [&](int64_t at) {   // what lies past the last row is read as zeros
+    next.load(static_cast<const T*>(a.x) + (at < a.rows ? at : 0) * a.ldx, at < a.rows ? a.D : 0, t, threads);
+  };
+  load(row);
+  // a block's groups go on together
+  for (; row - group < a.rows; row += stride) {
+    const Row<T, false, NV> x = next;
+    if (row - group + stride < a.rows) load(row + stride);
+    float2 st;
+    st.x = row_sum1<G>(part_sum<Row<T, false, NV>, NV>(x), &red[0]) / n;
+    st.y = 1.0f / sqrtf(row_sum1<G>(part_squares<Row<T, false, NV>, false, NV>(x, st.x, a.D, t, threads),
+                                    &red[1]) / n + a.eps);
+    if (row >= a.rows) continue;
+    if (t == 0) write_statistics(a, st, row);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      write_vec<Row<T, false, NV>, false>(x, j, a, st, g[j], b[j], row, t, threads);
   }
 }
 
@@ -838,6 +881,7 @@ struct Spread {
 constexpr int64_t kFwdLongest = 512 * 4 * kVec;
 constexpr int64_t kFwdRingLongest = 512 * 2 * kVec;
 constexpr int64_t kBwdLongest = 512 * 2 * kVec;
+constexpr int64_t kStayFrom = int64_t(1) << 22;   // elements of unaligned rows, forward
 // What the rings of an SM's teams take of its shared memory: backward copies
 // three rows a turn, forward one and is no quicker with more (128 KB 47.8 us,
 // 200 KB 48.8 at 16384 x 4096).
@@ -954,6 +998,21 @@ cudaError_t launch_fwd(const FwdArgs& a, const Spread& sp, bool few, cudaStream_
   return go(layernorm_fwd_kernel<T, kAligned, 0, 4, 1>, 1);
 }
 
+template <typename T>
+cudaError_t launch_fwd_stay(const FwdArgs& a, cudaStream_t s) {
+  const Spread sp = bwd_spread(a.D);
+  const auto go = [&](auto kernel) {
+    const int grid = staying_blocks(a.rows, sp.G != 0 ? 256 / sp.G : 1,
+                                    (sp.G != 0 ? 768 : 512) / sp.threads);
+    return launch_dependent(kernel, dim3(grid), dim3(sp.threads), 0, s, a);
+  };
+  if (sp.G == 8) return go(layernorm_fwd_stay_kernel<T, 8, 1>);
+  if (sp.G == 16) return go(layernorm_fwd_stay_kernel<T, 16, 1>);
+  if (sp.G == 32) return go(layernorm_fwd_stay_kernel<T, 32, 1>);
+  if (sp.NV == 1) return go(layernorm_fwd_stay_kernel<T, 0, 1>);
+  return go(layernorm_fwd_stay_kernel<T, 0, 2>);
+}
+
 template <typename T, typename DY, bool kAligned>
 cudaError_t launch_bwd(const BwdArgs& a, const Spread& sp, int grid, cudaStream_t s) {
   const auto go = [&](auto kernel) {
@@ -1016,6 +1075,8 @@ tbn_status launch_layernorm_fwd(const LayerNormProblem& p, cudaStream_t s) {
     const Spread sp = fwd_spread(p.D, few);
     if (al && !few && p.D > 32 * kVec && p.D <= kFwdRingLongest)
       e = p.xdt == TBN_BF16 ? launch_fwd_ring<__nv_bfloat16>(a, s) : launch_fwd_ring<float>(a, s);
+    else if (!al && p.rows >= 32 * device_sm_count() && p.rows * p.D >= kStayFrom && p.D <= kBwdLongest)
+      e = p.xdt == TBN_BF16 ? launch_fwd_stay<__nv_bfloat16>(a, s) : launch_fwd_stay<float>(a, s);
     else if (p.xdt == TBN_BF16)
       e = al ? launch_fwd<__nv_bfloat16, true>(a, sp, few, s)
              : launch_fwd<__nv_bfloat16, false>(a, sp, few, s);

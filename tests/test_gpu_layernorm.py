@@ -106,6 +106,14 @@ def test_many_rows(rows, D, xdt, ydt, pad, offset):
     test_forward_and_backward(rows, D, xdt, ydt, pad, offset)
 
 
+# many rows that are not aligned, of each way to spread a row
+@pytest.mark.parametrize("rows,D", [(66001, 64), (38001, 111), (21001, 201), (14002, 300), (8501, 505),
+                                    (4871, 1001), (4870, 4095), (4871, 7777)])
+@pytest.mark.parametrize("xdt,ydt", [(BF16, BF16), (F32, F32), (F32, BF16)])
+def test_many_unaligned_rows(rows, D, xdt, ydt):
+    test_forward_and_backward(rows, D, xdt, ydt, 3, 1)
+
+
 def test_many_rows_in_place_and_equal_bits():
     rows, D = 4001, 1024
     x, dy = _inputs(rows, D, BF16, 21), _inputs(rows, D, BF16, 22)
