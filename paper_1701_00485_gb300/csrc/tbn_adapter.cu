@@ -616,7 +616,7 @@ constexpr int kExpandPlainSmem =
 // ahead, goes to shared memory where the sums are added to it, and is written out in
 // rows.  y has 16 bits with two terms, 32 with three.
 template <int RP, int kTerms>
-__global__ void __launch_bounds__(kThreads, RP * kTerms > 256 ? 1 : 2) expand_kernel(const __grid_constant__ ExpandArgs a) {
+__global__ void __launch_bounds__(kThreads, RP == 128 ? 1 : 2) expand_kernel(const __grid_constant__ ExpandArgs a) {
   using Y = typename std::conditional<kTerms == 2, __nv_bfloat16, float>::type;
   constexpr bool k16 = sizeof(Y) == 2;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -648,13 +648,13 @@ __global__ void __launch_bounds__(kThreads, RP * kTerms > 256 ? 1 : 2) expand_ke
   // the warp's tokens, one in each of sixteen lanes
   const int mine = tg + (lane & 15) < tile.z ? a.route.perm[tile.y + tg + (lane & 15)] : -1;
   const uint32_t sv_s = smem_addr(sv);
-  uint32_t base[k16 ? 16 : 32];
+  uint32_t base[32];
   uint4 pw[kWPieces];
   // the base of the warp's 64 columns from c on: in aligned rows a 16-byte word a
   // lane, kRows rows at a time; else two elements a lane, 32 apart, row by row
   const auto load = [&](int c) {
 #pragma unroll
-    for (int i = 0; i < (k16 ? 16 : 32); ++i) base[i] = 0u;
+    for (int i = 0; i < 32; ++i) base[i] = 0u;
     const Y* from = static_cast<const Y*>(a.base);
     if (from != nullptr) {
       if (a.y_aligned) {
@@ -678,8 +678,8 @@ __global__ void __launch_bounds__(kThreads, RP * kTerms > 256 ? 1 : 2) expand_ke
 #pragma unroll
           for (int i = 0; i < 2; ++i)
             if (token >= 0 && c + lane + 32 * i < a.K) {
-              if constexpr (k16)
-                base[m] |= static_cast<uint32_t>(__bfloat16_as_ushort(p[32 * i])) << (16 * i);
+              if constexpr (k16)   // as it comes: an operation here would wait for it
+                base[2 * m + i] = __bfloat16_as_ushort(p[32 * i]);
               else
                 base[2 * m + i] = __float_as_uint(p[32 * i]);
             }
@@ -724,7 +724,7 @@ __global__ void __launch_bounds__(kThreads, RP * kTerms > 256 ? 1 : 2) expand_ke
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           out[m * kOutRow + lane + 32 * i] =
-              k16 ? __uint_as_float(i ? base[m] & 0xFFFF0000u : base[m] << 16) : __uint_as_float(base[2 * m + i]);
+              __uint_as_float(k16 ? base[2 * m + i] << 16 : base[2 * m + i]);
     }
     if (c0 + kCols < col_end) load(c + kCols);
     if (!none) {
