@@ -1725,7 +1725,7 @@ cudaError_t run_expand(const AdapterProblem& p, const Plan& pl, const Route& rou
                        cudaStream_t s) {
   const size_t e = dtype_size(dt);
   const int tiles = static_cast<int>((K + kCols - 1) / kCols);
-  int groups = (4 * device_sm_count() + pl.max_tiles - 1) / pl.max_tiles;
+  int groups = (12 * device_sm_count() + pl.max_tiles - 1) / pl.max_tiles;
   if (groups > tiles) groups = tiles;
   const int per = (tiles + groups - 1) / groups;
   groups = (tiles + per - 1) / per;
