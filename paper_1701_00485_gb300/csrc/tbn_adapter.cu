@@ -1600,11 +1600,11 @@ Plan make_plan(int64_t T, int64_t n, int64_t r, int64_t K_in, int64_t K_out, boo
   p.max_tiles = static_cast<int>((T + p.tile - 1) / p.tile + used + 1);
   p.cluster_in = cluster_of(K_in, r, p.max_tiles);
   p.cluster_out = cluster_of(K_out, r, p.max_tiles);
-  // grad: about two CTAs an SM over the columns of both gradients, four without tc
+  // grad: about two CTAs an SM over the columns of both gradients, eight without tc
   const int64_t ct = tc && r <= 64 ? 256 : kCols;
   const int64_t column_tiles = (K_in + ct - 1) / ct + (K_out + ct - 1) / ct;
   // (items of an adapter end unevenly: a little below two a slot is quickest)
-  const int64_t slots = tc ? kGradCtas * device_sm_count() * 4 / 5 : 4 * device_sm_count();
+  const int64_t slots = tc ? kGradCtas * device_sm_count() * 4 / 5 : 8 * device_sm_count();
   const int64_t want = (slots + column_tiles - 1) / column_tiles;
   int64_t per = (T + want - 1) / want;
   per = (per + kTile - 1) / kTile * kTile;
