@@ -10,7 +10,10 @@
 // of the columns.  The loads of b_i are under way before that exchange.  With
 // few tokens several clusters share a token's columns, each with a whole v of
 // its own: reading a_i again from L2 is quicker than a second launch.  All in
-// 32 bits on the CUDA cores (products of bf16 values are exact).
+// 32 bits on the CUDA cores (products of bf16 values are exact).  Measured (GB300): 64
+// tokens of 64 adapters, rank 16, 4096 -> 4096, 10.3 us, of which the dependent loads
+// (ids, a, the exchange, b) are most; one token 8192 -> 8192 8.4 us a call from Python,
+// most of it the host's.
 #include <cuda_bf16.h>
 
 #include "tbn_device.cuh"
