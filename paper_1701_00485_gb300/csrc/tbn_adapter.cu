@@ -624,8 +624,8 @@ constexpr int kExpandPlainSmem =
 // CTA (tile, column group): 64 tokens x cols_per * 128 columns.  Warp w takes 16
 // tokens and 64 of the 128 columns: its part of the base is in registers a step
 // ahead, goes to shared memory where the sums are added to it, and is written out in
-// rows.  y has 16 bits with two terms, 32 with three.  8192 x 4096 fp32 rank 32 58 us
-// (4.6 TB/s with what stays in L2).
+// rows.  y has 16 bits with two terms, 32 with three.  8192 x 4096 fp32 rank 32 57 us
+// (4.8 TB/s with what stays in L2).
 template <int RP, int kTerms>
 __global__ void __launch_bounds__(kThreads, RP == 128 ? 1 : 2) expand_kernel(const __grid_constant__ ExpandArgs a) {
   using Y = typename std::conditional<kTerms == 2, __nv_bfloat16, float>::type;
@@ -836,8 +836,8 @@ struct GradArgs {
 // CTA (item, 128 columns): the ranks x 128 columns of scale_i sum_t u_t x_t^T
 // over the item's tokens, in steps of 64.  Both operands come token by token and
 // are transposed by ldmatrix: u's terms by cp.async, a step ahead, x through
-// registers.  Warp w takes 16 columns.  Both gradients of 8192 x 4096 fp32 rank 32 123
-// us (2.2 TB/s): six products a value on mma.sync (tensor pipe 43 %) take turns with
+// registers.  Warp w takes 16 columns.  Both gradients of 8192 x 4096 fp32 rank 32 110
+// us (2.6 TB/s): six products a value on mma.sync (tensor pipe 42 %) take turns with
 // the splitting of x (issue slots 49 %) in each of two CTAs an SM.
 template <typename T, int RP>
 __global__ void __launch_bounds__(kThreads) grad_kernel(const __grid_constant__ GradArgs a) {

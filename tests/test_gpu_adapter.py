@@ -311,6 +311,73 @@ def test_row_offsets_past_32_bits():
     assert g is not None
 
 
+@pytest.mark.parametrize("T,K_in,K_out,n,r", [(1, 200, 300, 2, 16), (150, 200, 304, 3, 100), (383, 256, 72, 5, 20),
+                                              (700, 512, 384, 4, 32), (900, 136, 1000, 30, 128)])
+@pytest.mark.parametrize("dt,pad", [(BF16, 0), (BF16, 3), (F32, 0), (F32, 3)])
+def test_workspaces_and_results_have_the_stated_sizes(T, K_in, K_out, n, r, dt, pad):
+    """What lies around the workspace, v, da and db stays as it is, and the
+    workspace's former contents do not matter."""
+    c = _case(T, K_in, K_out, n, r, dt, dt, pad, seed=T)
+    ad = {k: c[k] for k in ("ids", "scale", "ranks")}
+
+    def scratch(backward, fill):
+        size = tbn.tbn_adapter_workspace_bytes(T, K_in, K_out, n, r, backward=backward)
+        ws = torch.full((size + 512,), fill, dtype=torch.uint8, device="cuda")
+        return ws, ws[256:256 + size]
+
+    def whole(ws, fill):
+        return bool((ws[:256] == fill).all() and (ws[-256:] == fill).all())
+
+    out = []
+    for fill in (0x00, 0xFF):
+        guard, ws = scratch(False, fill)
+        v = torch.full((T * r + 128,), 7.0, device="cuda")
+        y = tbn.tbn_adapter_fwd(c["x"], c["a"], c["b"], base=c["base"], v=v[64:-64].view(T, r), workspace=ws, **ad)
+        assert whole(guard, fill) and (v[:64] == 7.0).all() and (v[-64:] == 7.0).all()
+        wide = [torch.full((n * r * K + 128,), 7.0, device="cuda") for K in (K_in, K_out)]
+        guard, ws = scratch(True, fill)
+        dx, da, db = tbn.tbn_adapter_bwd(c["dy"], c["x"], c["a"], c["b"], v=v[64:-64].view(T, r), base=c["dbase"],
+                                         da=wide[0][64:-64].view(n, r, K_in), db=wide[1][64:-64].view(n, r, K_out),
+                                         workspace=ws, **ad)
+        assert whole(guard, fill)
+        assert all((t[:64] == 7.0).all() and (t[-64:] == 7.0).all() for t in wide)
+        out.append((y, v[64:-64], dx, da, db))
+    assert all(torch.equal(p, q) for p, q in zip(*out))
+    assert tbn.tbn_device_error() == 0
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("T", [300, 1500])
+def test_as_many_adapters_as_there_may_be(T, dt):
+    test_forward(T, 72, 64, 1023, 4, dt, dt)
+    test_backward(T, 72, 64, 1023, 4, dt, dt)
+
+
+@pytest.mark.parametrize("dt,ld", [(BF16, 1 << 23), (BF16, (1 << 23) + 1), (F32, 1 << 23)])
+def test_tiles_of_rows_past_32_bits(dt, ld):
+    """520 rows, the last of which begins beyond element 2^32."""
+    T, K = 520, 128
+    c = _case(T, K, K, 2, 8, dt, dt, seed=19)
+    ad = {k: c[k] for k in ("ids", "scale", "ranks")}
+    pad = 1 if ld % 2 else 0   # the same kernels for the rows that stand together
+    near = {k: _rows(T, K, dt, torch.Generator(device="cuda").manual_seed(1), pad) for k in ("x", "dy", "base")}
+    store = torch.empty((T - 1) * ld + K, dtype=dt, device="cuda")
+    far = store.as_strided((T, K), (ld, 1))
+    for k in near:
+        near[k].copy_(c[k])
+    want = tbn.tbn_adapter_fwd(near["x"], c["a"], c["b"], base=near["base"], **ad)
+    far.copy_(near["x"])
+    assert torch.equal(tbn.tbn_adapter_fwd(far, c["a"], c["b"], base=near["base"], **ad), want)
+    grads = tbn.tbn_adapter_bwd(near["dy"], near["x"], c["a"], c["b"], base=near["base"], **ad)
+    got = tbn.tbn_adapter_bwd(near["dy"], far, c["a"], c["b"], base=near["base"], **ad)
+    assert all(torch.equal(p, q) for p, q in zip(got, grads))
+    far.copy_(near["base"])   # the base, overwritten by the result
+    tbn.tbn_adapter_fwd(near["x"], c["a"], c["b"], base=far, out=far, **ad)
+    assert torch.equal(far, want)
+    del store, far
+    torch.cuda.empty_cache()
+
+
 def test_on_another_stream():
     c = _case(500, 256, 256, 4, 16, seed=10)
     ad = {k: c[k] for k in ("ids", "scale", "ranks")}

@@ -215,6 +215,46 @@ def test_writes_stay_inside_the_rows():
     assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
+@pytest.mark.parametrize("rows,D", [(1, 64), (41, 300), (1300, 136), (1301, 4096), (5000, 505), (1217, 8200)])
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_workspaces_and_results_have_the_stated_sizes(rows, D, dt):
+    x, dy = _inputs(rows, D, dt, 31), _inputs(rows, D, dt, 32)
+    gamma = torch.randn(D, device="cuda")
+    size = tbn.tbn_layernorm_bwd_workspace_bytes(rows, D)
+    out = []
+    for fill in (0x00, 0xFF):
+        stats = [torch.full((rows + 128,), 7.0, device="cuda") for _ in range(2)]
+        y, mean, rstd = tbn.tbn_layernorm_fwd(x, gamma, mean=stats[0][64:-64], rstd=stats[1][64:-64])
+        ws = torch.full((size + 512,), fill, dtype=torch.uint8, device="cuda")
+        sums = [torch.full((D + 128,), 7.0, device="cuda") for _ in range(2)]
+        dx, dgamma, dbeta = tbn.tbn_layernorm_bwd(dy, x, mean, rstd, gamma, dgamma=sums[0][64:-64],
+                                                  dbeta=sums[1][64:-64], workspace=ws[256:256 + size])
+        assert (ws[:256] == fill).all() and (ws[-256:] == fill).all()
+        assert all((t[:64] == 7.0).all() and (t[-64:] == 7.0).all() for t in stats + sums)
+        out.append((y, dx, dgamma, dbeta))
+    assert all(torch.equal(p, q) for p, q in zip(*out))
+
+
+@pytest.mark.parametrize("dt,ld", [(BF16, 1 << 22), (BF16, (1 << 22) + 1), (F32, 1 << 22)])
+def test_many_rows_past_32_bits(dt, ld):
+    """1300 rows, the last of which begins beyond element 2^32."""
+    rows, D = 1300, 264
+    g = torch.Generator(device="cuda").manual_seed(5)
+    near = torch.empty((rows, D + (1 if ld % 2 else 0)), dtype=dt, device="cuda")[:, :D]
+    near.copy_(torch.empty((rows, D), device="cuda").normal_(generator=g))
+    store = torch.empty((rows - 1) * ld + D, dtype=dt, device="cuda")
+    far = store.as_strided((rows, D), (ld, 1))
+    far.copy_(near)
+    gamma = torch.randn(D, device="cuda")
+    y, mean, rstd = tbn.tbn_layernorm_fwd(near, gamma)
+    assert torch.equal(tbn.tbn_layernorm_fwd(far, gamma)[0], y)
+    want = tbn.tbn_layernorm_bwd(y, near, mean, rstd, gamma, dres=near)
+    got = tbn.tbn_layernorm_bwd(y, far, mean, rstd, gamma, dres=far, dx=far)
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    del store, far
+    torch.cuda.empty_cache()
+
+
 def test_refusals():
     x = torch.zeros(4, 64, device="cuda")
     with pytest.raises(ValueError):
